@@ -410,6 +410,98 @@ lpv_status lpv_add_layernorm(const void* x, const void* y, int64_t M, int64_t D,
 lpv_status lpv_attention(const void* qkv, int64_t n_seq, int32_t T, int32_t H, int32_t hd,
                          lpv_dtype dt, void* out, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Finetuning the pruned model (Fig. 1, Sec. 4) around the linear layers' backward:
+ * attention with a learned relative position bias, as the windows of Swin's encoder
+ * blocks have it, with its gradients.
+ * ------------------------------------------------------------------------ */
+
+/* A bucket index over the token pairs of a sequence.  Opaque; owns its device buffer;
+ * immutable, so calls on different streams may share it. */
+typedef struct lpv_relpos lpv_relpos;
+
+/*
+ * lpv_relpos_create -- the bucket index of a relative position bias: the bias of head h
+ * between query i and key j is table[index[i][j]][h].
+ * index  device, T x T int32, row-major: each pair's bucket in [0, n_buckets), or -1 for a
+ *        pair that takes no part (causal order, say).
+ * T in [1, 2048], n_buckets in [1, 65535].  *out receives the handle (release it with
+ * lpv_relpos_destroy), NULL on failure.  Copies the index to the host, checks every entry
+ * (INVALID_ARG names the first outside the range), sorts the pairs by bucket there, and
+ * allocates device memory (8 bytes a pair); waits on `stream` twice, like lpv_bsr_pack.
+ * index may be freed afterwards.
+ * Errors: INVALID_ARG, SHAPE, ALLOC, HIP.
+ */
+lpv_status lpv_relpos_create(const int32_t* index, int32_t T, int32_t n_buckets, void* stream,
+                             lpv_relpos** out);
+
+/* Release a handle.  NULL-safe.  The caller must make sure no enqueued work still uses it. */
+void lpv_relpos_destroy(lpv_relpos* p);
+
+/*
+ * lpv_relpos_workspace_size -- the workspace that lpv_relpos_attention (grad = 0) or
+ * lpv_relpos_attention_grad (grad != 0) needs for n_seq sequences and H heads.  Host only;
+ * writes *bytes.  Errors: INVALID_ARG, SHAPE.
+ */
+lpv_status lpv_relpos_workspace_size(const lpv_relpos* p, int64_t n_seq, int32_t H, int32_t grad,
+                                     size_t* bytes);
+
+/*
+ * lpv_relpos_attention -- multi-head self-attention with the bias, of n_seq sequences of
+ * the handle's T tokens (a window each, or a whole image):
+ *   s_ij = q_i . k_j / sqrt(hd) + table[index_ij][h],   out_h = softmax_j(s) V_h.
+ * table   device, n_buckets x H, row-major, of the element type.  A bias of -inf or of the
+ *         type's lowest finite value takes its pairs out.
+ * qkv     device, (n_seq T) x (3 H hd), row stride ldq; a row holds q, k, v, each H heads
+ *         of hd elements (as in lpv_attention).
+ * region  device, n_region x T int32, or NULL: sequence s has the labels of row
+ *         s % n_region.  Tokens attend to tokens of the same label only (the parts of a
+ *         shifted window); a token with a negative label is padding: it attends to
+ *         nothing, nothing attends to it, and its values are not used (they may be NaN).
+ * out     device, (n_seq T) x (H hd), row stride ldo; must not overlap qkv.  A row that
+ *         no pair is left for is zero.
+ * lse     device, n_seq x H x T float32, or NULL: receives log sum_j exp(s_ij) (-inf for a
+ *         row without pairs), for the gradient.
+ * workspace  device, 16-byte aligned, at least lpv_relpos_workspace_size bytes (may be
+ *         NULL if that is 0); owned by the caller, who must not reuse it before the call's
+ *         work has finished.  Needs no clearing.
+ * hd = 32 or 64, H in [1, 64], 16-bit element types; n_seq T and n_seq H below 2^31; ldq
+ * and ldo multiples of 16 bytes, at most 2^22 elements.  Scores, softmax and sums in
+ * float32; the weights are rounded once to the element type for the product with V.  Apart
+ * from padding tokens, non-finite values in qkv are outside the contract.  A call gives the
+ * same bits every time.  No allocation, no host synchronisation.
+ * Errors: INVALID_ARG, SHAPE, DTYPE, ALIAS, HIP.
+ */
+lpv_status lpv_relpos_attention(const lpv_relpos* p, const void* table, const void* qkv, int64_t ldq,
+                                int64_t n_seq, int32_t H, int32_t hd, lpv_dtype dt,
+                                const int32_t* region, int64_t n_region, void* out, int64_t ldo,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * lpv_relpos_attention_grad -- the gradients of lpv_relpos_attention: with P the softmax
+ * weights, dP = dout V^T and dS = P (dP - rowsum(P dP)),
+ *   dQ = dS K / sqrt(hd), dK = dS^T Q / sqrt(hd), dV = P^T dout,
+ *   dtable[b][h] = sum of dS_ij over the sequences and over the pairs with index_ij = b.
+ * table, qkv, region: as given to the forward call; out, lse: as it wrote them.
+ * dout    device, (n_seq T) x (H hd), row stride ldg: the gradient at out.  (A padding
+ *         token's rows of out and dout are not used.)
+ * dqkv    device, (n_seq T) x (3 H hd), row stride lddq: receives dQ, dK, dV in qkv's
+ *         layout (G of the qkv layer's backward).  Rows of padding tokens are zero.
+ * dtable  device, n_buckets x H: receives the bias's gradient (not added to; zero for
+ *         buckets without pairs and where n_seq = 0).
+ * dqkv and dtable overlap neither an input nor each other.  P and dS are rounded once to
+ * the element type for the products; the sums over sequences and pairs are float32 in a
+ * fixed order, rounded once.  Types, sizes, strides and workspace as above.  No allocation,
+ * no host synchronisation.
+ * Errors: INVALID_ARG, SHAPE, DTYPE, ALIAS, HIP.
+ */
+lpv_status lpv_relpos_attention_grad(const lpv_relpos* p, const void* table, const void* qkv,
+                                     int64_t ldq, int64_t n_seq, int32_t H, int32_t hd, lpv_dtype dt,
+                                     const int32_t* region, int64_t n_region, const void* out,
+                                     int64_t ldo, const float* lse, const void* dout, int64_t ldg,
+                                     void* dqkv, int64_t lddq, void* dtable, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

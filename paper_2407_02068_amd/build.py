@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblpv.so")
 SOURCES = ["api.hip", "pack.hip", "linear.hip", "mask.hip", "backward.hip", "delta.hip", "encoder.hip",
-           "stationary.hip"]
+           "stationary.hip", "relpos.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -27,7 +27,7 @@ FLAGS = [
 # register counts accumulators in AGPRs would be copied across every branch.
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 SOURCE_FLAGS = {"linear.hip": _VGPR_MFMA, "backward.hip": _VGPR_MFMA, "encoder.hip": _VGPR_MFMA,
-                "stationary.hip": _VGPR_MFMA}
+                "stationary.hip": _VGPR_MFMA, "relpos.hip": _VGPR_MFMA}
 BUILD_DIR = os.path.join(HERE, "_build")
 
 

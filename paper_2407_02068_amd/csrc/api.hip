@@ -831,3 +831,262 @@ lpv_status lpv_attention(const void* qkv, int64_t n_seq, int32_t T, int32_t H, i
     hipError_t e = lpv::launch_attention(qkv, n_seq, T, H, dt, out, (hipStream_t)stream);
     return e == hipSuccess ? LPV_OK : hip_fail(e, "attention launch");
 }
+
+namespace {
+
+// Host arrays of a bucket index while its handle is made.
+struct RelposHost {
+    int32_t *index = nullptr, *count = nullptr;
+    char* tables = nullptr;
+    ~RelposHost()
+    {
+        delete[] index;
+        delete[] count;
+        delete[] tables;
+    }
+};
+
+bool overlap(const void* a, int64_t an, const void* b, int64_t bn)
+{
+    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+    return a0 < b0 + (uintptr_t)bn && b0 < a0 + (uintptr_t)an;
+}
+
+// Shared checks of the position-biased attention calls: sizes, the labels and the matrices
+// every one of them reads.
+lpv_status check_relpos(const lpv_relpos* p, const void* table, const void* qkv, int64_t ldq,
+                        int64_t n_seq, int32_t H, int32_t hd, int dt, const int32_t* region,
+                        int64_t n_region, const void* out, int64_t ldo)
+{
+    if (!p)
+        return fail(LPV_ERR_INVALID_ARG, "handle must not be NULL");
+    if (dt != LPV_BF16 && dt != LPV_F16)
+        return fail(LPV_ERR_DTYPE, "relpos attention takes 16-bit element types only (got %d)", dt);
+    if (hd != 32 && hd != 64)
+        return fail(LPV_ERR_SHAPE, "head dimension %d is not supported (32 or 64)", hd);
+    if (H < 1 || H > 64)
+        return fail(LPV_ERR_SHAPE, "H = %d is out of range [1, 64]", H);
+    if (n_seq < 0 || n_seq >= MAX_M || n_seq * p->T >= MAX_M || n_seq * H >= MAX_M)
+        return fail(LPV_ERR_SHAPE, "n_seq = %lld is out of range", (long long)n_seq);
+    if (!table || (uintptr_t)table % 2)
+        return fail(LPV_ERR_INVALID_ARG, "table must be non-NULL and aligned to its element size");
+    if (region && (n_region < 1 || n_region >= MAX_M || (uintptr_t)region % 4))
+        return fail(LPV_ERR_INVALID_ARG, "region must be 4-byte aligned with n_region >= 1");
+    const int64_t D = (int64_t)H * hd;
+    if (ldq < 3 * D || ldq > MAX_LD || ldq % 8 || ldo < D || ldo > MAX_LD || ldo % 8)
+        return fail(LPV_ERR_INVALID_ARG, "row strides must cover the row, be multiples of 16 bytes "
+                                         "and at most 2^22");
+    if (n_seq > 0 && (!qkv || !out || !aligned16(qkv) || !aligned16(out)))
+        return fail(LPV_ERR_INVALID_ARG, "qkv and out must be non-NULL and 16-byte aligned");
+    return LPV_OK;
+}
+
+// The current device, and the workspace (after every other check).
+lpv_status check_relpos_device(const lpv_relpos* p, int64_t n_seq, int32_t H, bool grad,
+                               const void* ws, size_t ws_bytes)
+{
+    const size_t need = lpv::relpos_workspace_bytes(p, n_seq, H, grad);
+    if (need && (!ws || ws_bytes < need || !aligned16(ws)))
+        return fail(LPV_ERR_INVALID_ARG, "workspace: %zu bytes 16-byte aligned are needed", need);
+    int dev = -1;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess)
+        return hip_fail(e, "hipGetDevice");
+    if (dev != p->device)
+        return fail(LPV_ERR_INVALID_ARG, "handle lives on device %d, current device is %d", p->device,
+                    dev);
+    return LPV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lpv_status lpv_relpos_create(const int32_t* index, int32_t T, int32_t n_buckets, void* stream,
+                             lpv_relpos** out)
+{
+    g_err[0] = 0;
+    if (!out)
+        return fail(LPV_ERR_INVALID_ARG, "out must not be NULL");
+    *out = nullptr;
+    if (T < 1 || T > lpv::RELPOS_MAX_T)
+        return fail(LPV_ERR_SHAPE, "T = %d is out of range [1, %d]", T, lpv::RELPOS_MAX_T);
+    if (n_buckets < 1 || n_buckets > lpv::RELPOS_MAX_BUCKETS)
+        return fail(LPV_ERR_SHAPE, "n_buckets = %d is out of range [1, %d]", n_buckets,
+                    lpv::RELPOS_MAX_BUCKETS);
+    if (!index || (uintptr_t)index % 4)
+        return fail(LPV_ERR_INVALID_ARG, "index must be non-NULL and 4-byte aligned");
+    const hipStream_t s = (hipStream_t)stream;
+    RelposHost host;
+    host.index = new (std::nothrow) int32_t[(size_t)T * T];
+    host.count = new (std::nothrow) int32_t[n_buckets];
+    if (!host.index || !host.count)
+        return fail(LPV_ERR_ALLOC, "host allocation failed");
+    hipError_t e = hipMemcpyAsync(host.index, index, (size_t)T * T * 4, hipMemcpyDeviceToHost, s);
+    if (e == hipSuccess)
+        e = hipStreamSynchronize(s);
+    if (e != hipSuccess)
+        return hip_fail(e, "index copy");
+    const lpv::RelposSizes z = lpv::relpos_sizes(host.index, T, n_buckets, host.count);
+    if (z.bad >= 0)
+        return fail(LPV_ERR_INVALID_ARG, "index[%lld][%lld] = %d is outside [-1, %d)",
+                    (long long)(z.bad / T), (long long)(z.bad % T), host.index[z.bad], n_buckets);
+    const int32_t nt = (T + 31) / 32;
+    const size_t n_idx = (size_t)nt * nt * 1024;
+    const size_t words[3] = {(size_t)z.n_pairs, (size_t)z.n_segs + 1, (size_t)n_buckets + 1};
+    const size_t bytes = n_idx * 4 + (words[0] + words[1] + words[2]) * 4;
+    host.tables = new (std::nothrow) char[bytes];
+    lpv_relpos* h = new (std::nothrow) lpv_relpos();
+    if (!host.tables || !h) {
+        delete h;
+        return fail(LPV_ERR_ALLOC, "host allocation failed");
+    }
+    e = dmalloc(&h->mem, bytes);
+    if (e != hipSuccess) {
+        delete h;
+        return e == hipErrorOutOfMemory ? fail(LPV_ERR_ALLOC, "device allocation failed")
+                                        : hip_fail(e, "hipMalloc");
+    }
+    auto place = [&](lpv_relpos* at, char* mem) {
+        at->idx = (uint16_t*)mem;
+        at->idx_t = at->idx + n_idx;
+        at->order = (int32_t*)(at->idx_t + n_idx);
+        at->seg_ptr = at->order + words[0];
+        at->bucket_seg = at->seg_ptr + words[1];
+    };
+    lpv_relpos on_host = {};
+    place(&on_host, host.tables);
+    place(h, (char*)h->mem);
+    lpv::relpos_tables(host.index, T, n_buckets, nt, host.count, on_host.idx, on_host.idx_t,
+                       on_host.order, on_host.seg_ptr, on_host.bucket_seg);
+    h->T = T;
+    h->nt = nt;
+    h->n_buckets = n_buckets;
+    h->n_segs = z.n_segs;
+    e = hipGetDevice(&h->device);
+    if (e == hipSuccess)
+        e = hipMemcpyAsync(h->mem, host.tables, bytes, hipMemcpyHostToDevice, s);
+    if (e == hipSuccess)
+        e = hipStreamSynchronize(s);
+    if (e != hipSuccess) {
+        lpv_relpos_destroy(h);
+        return hip_fail(e, "index upload");
+    }
+    *out = h;
+    return LPV_OK;
+}
+
+void lpv_relpos_destroy(lpv_relpos* p)
+{
+    if (!p)
+        return;
+    (void)hipFree(p->mem);
+    delete p;
+}
+
+lpv_status lpv_relpos_workspace_size(const lpv_relpos* p, int64_t n_seq, int32_t H, int32_t grad,
+                                     size_t* bytes)
+{
+    if (!p || !bytes)
+        return fail(LPV_ERR_INVALID_ARG, "handle and bytes must not be NULL");
+    if (H < 1 || H > 64)
+        return fail(LPV_ERR_SHAPE, "H = %d is out of range [1, 64]", H);
+    if (n_seq < 0 || n_seq >= MAX_M || n_seq * p->T >= MAX_M || n_seq * H >= MAX_M)
+        return fail(LPV_ERR_SHAPE, "n_seq = %lld is out of range", (long long)n_seq);
+    *bytes = lpv::relpos_workspace_bytes(p, n_seq, H, grad != 0);
+    return LPV_OK;
+}
+
+lpv_status lpv_relpos_attention(const lpv_relpos* p, const void* table, const void* qkv, int64_t ldq,
+                                int64_t n_seq, int32_t H, int32_t hd, lpv_dtype dt,
+                                const int32_t* region, int64_t n_region, void* out, int64_t ldo,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream)
+{
+    lpv_status st = check_relpos(p, table, qkv, ldq, n_seq, H, hd, dt, region, n_region, out, ldo);
+    if (st != LPV_OK)
+        return st;
+    if (lse && (uintptr_t)lse % 4)
+        return fail(LPV_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+    if (n_seq == 0)
+        return LPV_OK;
+    const int64_t D = (int64_t)H * hd, M = n_seq * p->T;
+    const int64_t nq = ((M - 1) * ldq + 3 * D) * 2, no = ((M - 1) * ldo + D) * 2, nl = M * H * 4;
+    if (overlap(out, no, qkv, nq) || (lse && (overlap(lse, nl, qkv, nq) || overlap(lse, nl, out, no))))
+        return fail(LPV_ERR_ALIAS, "qkv, out and lse must not overlap");
+    st = check_relpos_device(p, n_seq, H, false, workspace, workspace_bytes);
+    if (st != LPV_OK)
+        return st;
+    lpv::RelposCall c = {};
+    c.table = table;
+    c.qkv = qkv;
+    c.ldq = ldq;
+    c.n_seq = n_seq;
+    c.H = H;
+    c.hd = hd;
+    c.dtype = dt;
+    c.region = region;
+    c.n_region = n_region;
+    c.out = out;
+    c.ldo = ldo;
+    c.lse = lse;
+    c.ws = workspace;
+    const hipError_t e = lpv::launch_relpos_attention(p, c, (hipStream_t)stream);
+    return e == hipSuccess ? LPV_OK : hip_fail(e, "relpos_attention launch");
+}
+
+lpv_status lpv_relpos_attention_grad(const lpv_relpos* p, const void* table, const void* qkv,
+                                     int64_t ldq, int64_t n_seq, int32_t H, int32_t hd, lpv_dtype dt,
+                                     const int32_t* region, int64_t n_region, const void* out,
+                                     int64_t ldo, const float* lse, const void* dout, int64_t ldg,
+                                     void* dqkv, int64_t lddq, void* dtable, void* workspace,
+                                     size_t workspace_bytes, void* stream)
+{
+    lpv_status st = check_relpos(p, table, qkv, ldq, n_seq, H, hd, dt, region, n_region, out, ldo);
+    if (st != LPV_OK)
+        return st;
+    const int64_t D = (int64_t)H * hd, M = n_seq * p->T;
+    if (ldg < D || ldg > MAX_LD || ldg % 8 || lddq < 3 * D || lddq > MAX_LD || lddq % 8)
+        return fail(LPV_ERR_INVALID_ARG, "row strides must cover the row, be multiples of 16 bytes "
+                                         "and at most 2^22");
+    if (!dtable || (uintptr_t)dtable % 2)
+        return fail(LPV_ERR_INVALID_ARG, "dtable must be non-NULL and aligned to its element size");
+    if (n_seq > 0) {
+        if (!lse || (uintptr_t)lse % 4 || !dout || !dqkv || !aligned16(dout) || !aligned16(dqkv))
+            return fail(LPV_ERR_INVALID_ARG, "lse, dout and dqkv must be non-NULL and aligned to 4, 16 "
+                                             "and 16 bytes");
+        const int64_t nq = ((M - 1) * ldq + 3 * D) * 2, no = ((M - 1) * ldo + D) * 2;
+        const int64_t ng = ((M - 1) * ldg + D) * 2, nd = ((M - 1) * lddq + 3 * D) * 2;
+        const int64_t nt = (int64_t)p->n_buckets * H * 2, nl = M * H * 4;
+        if (overlap(dqkv, nd, qkv, nq) || overlap(dqkv, nd, out, no) || overlap(dqkv, nd, dout, ng) ||
+            overlap(dqkv, nd, lse, nl) || overlap(dqkv, nd, table, nt) || overlap(dqkv, nd, dtable, nt) ||
+            overlap(dtable, nt, qkv, nq) || overlap(dtable, nt, out, no) || overlap(dtable, nt, dout, ng) ||
+            overlap(dtable, nt, lse, nl))
+            return fail(LPV_ERR_ALIAS, "dqkv and dtable must not overlap an input or each other");
+    }
+    st = check_relpos_device(p, n_seq, H, true, workspace, workspace_bytes);
+    if (st != LPV_OK)
+        return st;
+    lpv::RelposCall c = {};
+    c.table = table;
+    c.qkv = qkv;
+    c.ldq = ldq;
+    c.n_seq = n_seq;
+    c.H = H;
+    c.hd = hd;
+    c.dtype = dt;
+    c.region = region;
+    c.n_region = n_region;
+    c.out = (void*)out;
+    c.ldo = ldo;
+    c.lse = (float*)lse;
+    c.dout = dout;
+    c.ldg = ldg;
+    c.dqkv = dqkv;
+    c.lddq = lddq;
+    c.dtable = dtable;
+    c.ws = workspace;
+    const hipError_t e = lpv::launch_relpos_grad(p, c, (hipStream_t)stream);
+    return e == hipSuccess ? LPV_OK : hip_fail(e, "relpos_attention_grad launch");
+}
+
+}  // extern "C"

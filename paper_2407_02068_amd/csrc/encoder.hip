@@ -9,7 +9,7 @@
 // end on the GPU with the block-sparse layers in place.
 #include <math.h>
 
-#include "lpv_device.h"
+#include "lpv_attention.h"
 #include "lpv_grid.h"
 #include "lpv_internal.h"
 
@@ -130,32 +130,6 @@ __global__ __launch_bounds__(256) void k_add_layernorm(const uint16_t* x, const 
 // weighted mean of V with those weights.
 constexpr int ATT_RS = ATT_HD * 2 + 16;  // bytes per staged row
 static_assert(2 * ((ATT_MAX_T + 31) / 32 * 32) * ATT_RS <= 163840, "K and V of a head fit in LDS");
-
-typedef short att_v4s __attribute__((ext_vector_type(4)));
-
-__device__ inline uint2 att_tr_read(uint32_t addr)
-{
-    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                         (__attribute__((address_space(3))) att_v4s*)(uintptr_t)addr));
-}
-
-typedef unsigned int att_u4 __attribute__((ext_vector_type(4)));
-
-// c + the two 16-bit values packed in p (one dot product with (1, 1): the
-// products are exact, the sum is float32)
-template <int DT> __device__ inline float att_add2(uint32_t p, float c)
-{
-    if (DT == LPV_BF16)
-        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p),
-                                               __builtin_bit_cast(bf16x2, 0x3f803f80u), c, false);
-    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, p), __builtin_bit_cast(f16x2, 0x3c003c00u),
-                                  c, false);
-}
-
-__device__ inline uint4 att_read16(uint32_t addr)
-{
-    return __builtin_bit_cast(uint4, *(const __attribute__((address_space(3))) att_u4*)(uintptr_t)addr);
-}
 
 template <int DT, int NT>
 __global__ __launch_bounds__(NT) void k_attention(const uint16_t* __restrict__ qkv, int32_t heads,

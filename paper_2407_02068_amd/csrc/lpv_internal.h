@@ -69,6 +69,20 @@ struct lpv_bsr {
     mutable size_t gradw_ws_bytes;
 };
 
+// The bucket index of a position bias (lpv_relpos_create).
+struct lpv_relpos {
+    int32_t T, nt;  // tokens, and tiles of 32 of them
+    int32_t n_buckets, n_segs;
+    int32_t device;
+    void* mem;              // one allocation, the arrays below in it
+    uint16_t *idx, *idx_t;  // the index and its transpose, 32 nt x 32 nt, 0xffff: no pair
+    // the pairs by bucket (their places in a head's tiles), cut into segments of at most
+    // RELPOS_SEG; a bucket without pairs has one empty segment
+    int32_t* order;
+    int32_t* seg_ptr;     // n_segs + 1
+    int32_t* bucket_seg;  // n_buckets + 1
+};
+
 namespace lpv {
 
 struct PackArgs {
@@ -173,6 +187,40 @@ hipError_t launch_add_layernorm(const void* x, const void* y, int64_t M, int32_t
                                 hipStream_t s);
 hipError_t launch_attention(const void* qkv, int64_t n_seq, int32_t T, int32_t H, int dtype,
                             void* out, hipStream_t s);
+// relpos.hip
+constexpr int32_t RELPOS_MAX_T = 2048, RELPOS_MAX_BUCKETS = 65535, RELPOS_SEG = 2048;
+struct RelposCall {
+    const void* table;  // n_buckets x H
+    const void* qkv;
+    int64_t ldq, n_seq;
+    int32_t H, hd;
+    int dtype;
+    const int32_t* region;  // n_region x T, or NULL
+    int64_t n_region;
+    void* out;  // the gradient reads it
+    int64_t ldo;
+    float* lse;
+    const void* dout;  // gradient only, as are the next
+    int64_t ldg;
+    void* dqkv;
+    int64_t lddq;
+    void* dtable;
+    void* ws;
+};
+// The pairs and segments of an index, the pairs of each bucket (count), and the place of
+// the first entry outside [-1, n_buckets) (bad, -1 if there is none); host memory.
+struct RelposSizes {
+    int64_t bad, n_pairs;
+    int32_t n_segs;
+};
+RelposSizes relpos_sizes(const int32_t* index, int32_t T, int32_t n_buckets, int32_t* count);
+// The handle's arrays (host memory; count as relpos_sizes left it, overwritten).
+void relpos_tables(const int32_t* index, int32_t T, int32_t n_buckets, int32_t nt, int32_t* count,
+                   uint16_t* idx, uint16_t* idx_t, int32_t* order, int32_t* seg_ptr,
+                   int32_t* bucket_seg);
+size_t relpos_workspace_bytes(const lpv_relpos* h, int64_t n_seq, int32_t H, bool grad);
+hipError_t launch_relpos_attention(const lpv_relpos* h, const RelposCall& c, hipStream_t s);
+hipError_t launch_relpos_grad(const lpv_relpos* h, const RelposCall& c, hipStream_t s);
 hipError_t launch_bias_grad(const void* G, int64_t ldg, int64_t M, int64_t N, int dtype, void* db,
                             hipStream_t s);
 // The same with the partial sums in a fixed device array of this many floats

@@ -23,8 +23,9 @@ EXPORTED = ("lpv_bsr_pack", "lpv_bsr_info_get", "lpv_bsr_export", "lpv_bsr_sched
             "lpv_bsr_unpack", "lpv_bsr_linear", "lpv_dense_linear", "lpv_mask_topk",
             "lpv_bsr_transpose", "lpv_bsr_grad_w", "lpv_bias_grad", "lpv_bias_grad_noalloc",
             "lpv_delta_curve", "lpv_delta_curve_ws", "lpv_delta_curve_workspace_size",
-            "lpv_add_layernorm", "lpv_attention", "lpv_bsr_destroy", "lpv_status_str",
-            "lpv_last_error")
+            "lpv_add_layernorm", "lpv_attention", "lpv_relpos_create", "lpv_relpos_destroy",
+            "lpv_relpos_workspace_size", "lpv_relpos_attention", "lpv_relpos_attention_grad",
+            "lpv_bsr_destroy", "lpv_status_str", "lpv_last_error")
 
 
 class LpvError(RuntimeError):
@@ -78,14 +79,24 @@ def lib():
                                      i64, ctypes.c_double, vp, i32, vp, vp, ctypes.c_size_t, vp]
     L.lpv_delta_curve_workspace_size.argtypes = [i64, i64, i32, i32, i64, i32,
                                                  ctypes.POINTER(ctypes.c_size_t)]
+    size_p = ctypes.POINTER(ctypes.c_size_t)
+    L.lpv_relpos_create.argtypes = [vp, i32, i32, vp, ctypes.POINTER(vp)]
+    L.lpv_relpos_workspace_size.argtypes = [vp, i64, i32, i32, size_p]
+    L.lpv_relpos_attention.argtypes = [vp, vp, vp, i64, i64, i32, i32, i32, vp, i64, vp, i64, vp,
+                                       vp, ctypes.c_size_t, vp]
+    L.lpv_relpos_attention_grad.argtypes = [vp, vp, vp, i64, i64, i32, i32, i32, vp, i64, vp, i64,
+                                            vp, vp, i64, vp, i64, vp, vp, ctypes.c_size_t, vp]
     for f in ("lpv_bsr_pack", "lpv_bsr_info_get", "lpv_bsr_export", "lpv_bsr_schedule_export",
               "lpv_bsr_unpack", "lpv_bsr_linear", "lpv_dense_linear", "lpv_mask_topk",
               "lpv_bsr_transpose", "lpv_bsr_grad_w", "lpv_bias_grad", "lpv_bias_grad_noalloc",
               "lpv_delta_curve", "lpv_delta_curve_ws", "lpv_delta_curve_workspace_size",
-              "lpv_add_layernorm", "lpv_attention"):
+              "lpv_add_layernorm", "lpv_attention", "lpv_relpos_create",
+              "lpv_relpos_workspace_size", "lpv_relpos_attention", "lpv_relpos_attention_grad"):
         getattr(L, f).restype = i32
     L.lpv_bsr_destroy.argtypes = [vp]
     L.lpv_bsr_destroy.restype = None
+    L.lpv_relpos_destroy.argtypes = [vp]
+    L.lpv_relpos_destroy.restype = None
     L.lpv_status_str.argtypes = [i32]
     L.lpv_status_str.restype = ctypes.c_char_p
     L.lpv_last_error.argtypes = []
@@ -439,3 +450,156 @@ def attention(qkv, n_seq, T, H, out=None, stream=None, hd=64):
                                ctypes.c_void_p(out.data_ptr()), _stream(stream)), "lpv_attention")
     return out
 
+
+
+def _on_current(*tensors):
+    """Every tensor's device is the current one (the library works on that)."""
+    dev = torch.cuda.current_device()
+    for name, t in tensors:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise ValueError("%s must be a tensor on the GPU" % name)
+        if t.device.index != dev:
+            raise ValueError("%s lives on device %d, current device is %d" % (name, t.device.index, dev))
+
+
+def _rows(t, name, M, cols, dtype):
+    """(pointer, row stride) of an M x cols matrix of ``dtype``."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or tuple(t.shape) != (M, cols) \
+            or t.dtype != dtype:
+        raise ValueError("%s must be a %d x %d tensor of %s" % (name, M, cols, dtype))
+    if M == 0:  # (an empty tensor's strides say nothing)
+        return None, cols
+    return _mat(t, name)
+
+
+class RelPos:
+    """The bucket index of a relative position bias (owns an lpv_relpos handle)."""
+
+    def __init__(self, handle, T, n_buckets, device):
+        self._h = ctypes.c_void_p(handle)
+        self.T, self.n_buckets, self.device = T, n_buckets, device
+
+    @property
+    def handle(self):
+        return self._h
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            lib().lpv_relpos_destroy(self._h)
+            self._h = ctypes.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def relpos(index, n_buckets, stream=None):
+    """lpv_relpos_create: a T x T int32 bucket index (device; -1: the pair takes no part)
+    -> RelPos.  Waits for the copy."""
+    if not isinstance(index, torch.Tensor) or index.dim() != 2 or index.dtype != torch.int32 \
+            or index.shape[0] != index.shape[1] or not index.is_contiguous():
+        raise ValueError("index must be a contiguous T x T int32 tensor")
+    _on_current(("index", index))
+    out = ctypes.c_void_p()
+    _check(lib().lpv_relpos_create(ctypes.c_void_p(index.data_ptr()), index.shape[0], n_buckets,
+                                   _stream(stream), ctypes.byref(out)), "lpv_relpos_create")
+    return RelPos(out.value, index.shape[0], n_buckets, index.device)
+
+
+def relpos_workspace_size(rp, n_seq, H, grad=False):
+    """lpv_relpos_workspace_size: bytes of the workspace of ``relpos_attention`` or, with
+    ``grad``, of ``relpos_attention_grad``."""
+    nbytes = ctypes.c_size_t(0)
+    _check(lib().lpv_relpos_workspace_size(rp.handle, n_seq, H, int(grad), ctypes.byref(nbytes)),
+           "lpv_relpos_workspace_size")
+    return nbytes.value
+
+
+def _workspace(workspace, nbytes, device, stream):
+    """(pointer, bytes, tensor) of the caller's workspace, or of one from torch's
+    allocator (on the current stream only: that is what its reuse is ordered by)."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, 0, None
+        if stream is not None and _stream(stream).value != _stream(None).value:
+            raise ValueError("a call on a stream that is not the current one takes a workspace")
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    elif not isinstance(workspace, torch.Tensor) or not workspace.is_cuda \
+            or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor")
+    return (ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size(),
+            workspace)
+
+
+def _relpos_args(rp, table, qkv, n_seq, H, hd, region):
+    """The leading arguments that both position-biased attention calls share."""
+    if not isinstance(table, torch.Tensor) or table.dtype not in DTYPES \
+            or tuple(table.shape) != (rp.n_buckets, H) or not table.is_contiguous():
+        raise ValueError("table must be a contiguous %d x %d tensor" % (rp.n_buckets, H))
+    qp, ldq = _rows(qkv, "qkv", n_seq * rp.T, 3 * H * hd, table.dtype)
+    n_region = 0
+    if region is not None:
+        if not isinstance(region, torch.Tensor) or region.dim() != 2 or region.shape[1] != rp.T \
+                or region.dtype != torch.int32 or not region.is_contiguous():
+            raise ValueError("region must be a contiguous n x %d int32 tensor" % rp.T)
+        n_region = region.shape[0]
+    return (rp.handle, ctypes.c_void_p(table.data_ptr()), qp, ldq, n_seq, H, hd,
+            DTYPES[table.dtype], ctypes.c_void_p(region.data_ptr() if region is not None else 0),
+            n_region)
+
+
+def _lse(lse, n_seq, H, T):
+    if not isinstance(lse, torch.Tensor) or lse.dtype != torch.float32 \
+            or lse.numel() != n_seq * H * T or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 tensor of n_seq x H x T elements")
+    return ctypes.c_void_p(lse.data_ptr())
+
+
+def relpos_attention(rp, table, qkv, n_seq, H, region=None, out=None, lse=None, workspace=None,
+                     stream=None, hd=64):
+    """lpv_relpos_attention: multi-head self-attention of n_seq sequences of rp.T tokens with
+    the position bias table[index] (table: n_buckets x H); region: n x T int32 labels
+    (tokens attend within their label, negative: padding).  Returns (n_seq T) x (H hd);
+    ``lse`` (float32, n_seq x H x T), when given, receives the rows' log-sum-exp."""
+    args = _relpos_args(rp, table, qkv, n_seq, H, hd, region)
+    if out is None:
+        out = torch.empty((n_seq * rp.T, H * hd), dtype=qkv.dtype, device=qkv.device)
+    op, ldo = _rows(out, "out", n_seq * rp.T, H * hd, qkv.dtype)
+    lp = _lse(lse, n_seq, H, rp.T) if lse is not None else None
+    _on_current(("table", table), ("qkv", qkv), ("region", region), ("out", out), ("lse", lse),
+                ("workspace", workspace))
+    wp, nbytes, keep = _workspace(workspace, relpos_workspace_size(rp, n_seq, H), qkv.device, stream)
+    _check(lib().lpv_relpos_attention(*args, op, ldo, lp, wp, nbytes, _stream(stream)),
+           "lpv_relpos_attention")
+    return out
+
+
+def relpos_attention_grad(rp, table, qkv, out, lse, dout, n_seq, H, region=None, dqkv=None,
+                          dtable=None, workspace=None, stream=None, hd=64):
+    """lpv_relpos_attention_grad: (dqkv, dtable) from the gradient ``dout`` at the output;
+    ``out`` and ``lse`` as ``relpos_attention`` wrote them."""
+    args = _relpos_args(rp, table, qkv, n_seq, H, hd, region)
+    M = n_seq * rp.T
+    if dqkv is None:
+        dqkv = torch.empty((M, 3 * H * hd), dtype=qkv.dtype, device=qkv.device)
+    if dtable is None:
+        dtable = torch.empty_like(table)
+    if tuple(dtable.shape) != tuple(table.shape) or dtable.dtype != table.dtype \
+            or not dtable.is_contiguous():
+        raise ValueError("dtable must be a contiguous tensor shaped and typed like table")
+    op, ldo = _rows(out, "out", M, H * hd, qkv.dtype)
+    gp, ldg = _rows(dout, "dout", M, H * hd, qkv.dtype)
+    dp, ldd = _rows(dqkv, "dqkv", M, 3 * H * hd, qkv.dtype)
+    lp = _lse(lse, n_seq, H, rp.T)
+    _on_current(("table", table), ("qkv", qkv), ("region", region), ("out", out), ("lse", lse),
+                ("dout", dout), ("dqkv", dqkv), ("dtable", dtable), ("workspace", workspace))
+    wp, nbytes, keep = _workspace(workspace, relpos_workspace_size(rp, n_seq, H, True), qkv.device,
+                                  stream)
+    _check(lib().lpv_relpos_attention_grad(*args, op, ldo, lp, gp, ldg, dp, ldd,
+                                           ctypes.c_void_p(dtable.data_ptr()), wp, nbytes,
+                                           _stream(stream)), "lpv_relpos_attention_grad")
+    return dqkv, dtable
