@@ -413,7 +413,8 @@ lpv_status lpv_attention(const void* qkv, int64_t n_seq, int32_t T, int32_t H, i
 /* ------------------------------------------------------------------------
  * Finetuning the pruned model (Fig. 1, Sec. 4) around the linear layers' backward:
  * attention with a learned relative position bias, as the windows of Swin's encoder
- * blocks have it, with its gradients.
+ * blocks have it, with its gradients; and the loss that the head's gradient starts from, a
+ * distillation from the unpruned model's top logits.
  * ------------------------------------------------------------------------ */
 
 /* A bucket index over the token pairs of a sequence.  Opaque; owns its device buffer;
@@ -501,6 +502,45 @@ lpv_status lpv_relpos_attention_grad(const lpv_relpos* p, const void* table, con
                                      int64_t ldo, const float* lse, const void* dout, int64_t ldg,
                                      void* dqkv, int64_t lddq, void* dtable, void* workspace,
                                      size_t workspace_bytes, void* stream);
+
+/*
+ * lpv_distill -- the distillation loss of M rows from a teacher's top logits, and its
+ * gradient.  With the student's logits z of a row, the teacher's logits t at the classes
+ * ids, and the temperature tau:
+ *   p = softmax(z / tau) over the V classes, q = softmax(t / tau) over the row's entries,
+ *   loss = tau^2 sum_j q_j (log q_j - log p[ids_j]),
+ *   dlogits = dloss tau (p - q), q taken to its entries' classes (a class named by several
+ *             entries has the sum of their q).
+ * logits   device, M x V, row stride ldz: the head's output (lpv_dense_linear's with its N
+ *          padded to 16, of which the first V columns are classes).  -inf is allowed (a
+ *          class left out), unless a whole row is.
+ * ids, teacher  device, M x k int32 and float32, row stride ldt in elements: the entries.
+ *          An entry with an id outside [0, V) or a logit of -inf is not used (rows with
+ *          fewer than k); a row without entries has loss 0 and gradient 0.
+ * temperature  in [1e-3, 1e3].
+ * dloss    device, M float32: the gradient at each row's loss; NULL: 1.
+ * loss     device, M float32.
+ * dlogits  device, M x Vd (V <= Vd <= ldd), row stride ldd, the logits' type; NULL: the loss
+ *          alone.  Columns from V on receive zero (the head's padding), those from Vd on are
+ *          left as they were.  May be logits itself (ldd = ldz); else must not overlap it.
+ *          It is G of the head's backward.
+ * workspace  device, 16-byte aligned, at least lpv_distill_workspace_size bytes (may be NULL
+ *          if that is 0); owned by the caller, who must not reuse it before the call's work
+ *          has finished.  Needs no clearing.
+ * Every element type; float32 inside, dlogits rounded once.  k in [1, 1024], V in
+ * [1, 2^22], ldz, ldd multiples of 16 bytes and at most 2^22 elements, as is ldt.  Apart
+ * from the above, non-finite inputs are outside the contract.  A call gives the same bits
+ * every time.  No allocation, no host synchronisation.  M = 0 is a no-op.
+ * Errors: INVALID_ARG, SHAPE, DTYPE, ALIAS, HIP.
+ */
+lpv_status lpv_distill(const void* logits, int64_t ldz, int64_t M, int64_t V, lpv_dtype dt,
+                       const int32_t* ids, const float* teacher, int64_t ldt, int32_t k,
+                       double temperature, const float* dloss, float* loss, void* dlogits, int64_t ldd,
+                       int64_t Vd, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The workspace lpv_distill needs (with or without dlogits).  Host only; writes *bytes.
+ * Errors: INVALID_ARG, SHAPE, DTYPE. */
+lpv_status lpv_distill_workspace_size(int64_t M, int64_t V, int32_t k, lpv_dtype dt, size_t* bytes);
 
 #ifdef __cplusplus
 }

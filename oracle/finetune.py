@@ -69,13 +69,13 @@ def relpos_attention(qkv, table, index, n_seq, H, hd, region=None, dout=None, lo
 
 def distill(logits, ids, teacher, temperature, dloss=None):
     """loss = t^2 sum_j q_j (log q_j - log p[id_j]) per row, p = softmax(logits / t), q the
-    softmax of teacher / t over the row's entries with an id in [0, V); 0 for a row without
-    any.  With dloss, also dlogits = dloss t (p - the q of each class)."""
+    softmax of teacher / t over the row's entries with an id in [0, V) (and a logit above
+    -inf); 0 for a row without any.  With dloss, also dlogits = dloss t (p - the q of each class)."""
     z = np.asarray(logits, np.float64) / temperature
     M, V = z.shape
     loss, grad = np.zeros(M), np.zeros((M, V))
     for r in range(M):
-        use = np.flatnonzero((ids[r] >= 0) & (ids[r] < V))
+        use = np.flatnonzero((ids[r] >= 0) & (ids[r] < V) & (teacher[r] > -np.inf))
         if not len(use):
             continue
         at, t = ids[r, use], np.asarray(teacher[r, use], np.float64) / temperature

@@ -1090,3 +1090,78 @@ lpv_status lpv_relpos_attention_grad(const lpv_relpos* p, const void* table, con
 }
 
 }  // extern "C"
+
+namespace {
+
+lpv_status check_distill_sizes(int64_t M, int64_t V, int32_t k, int dt)
+{
+    if (!elem_size(dt))
+        return fail(LPV_ERR_DTYPE, "unknown element type %d", dt);
+    if (M < 0 || M >= MAX_M)
+        return fail(LPV_ERR_SHAPE, "M = %lld is out of range [0, 2^31)", (long long)M);
+    if (V < 1 || V > MAX_LD)
+        return fail(LPV_ERR_SHAPE, "V = %lld is out of range [1, %lld]", (long long)V, (long long)MAX_LD);
+    if (k < 1 || k > lpv::DISTILL_MAX_K)
+        return fail(LPV_ERR_SHAPE, "k = %d is out of range [1, %d]", k, lpv::DISTILL_MAX_K);
+    return LPV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lpv_status lpv_distill_workspace_size(int64_t M, int64_t V, int32_t k, lpv_dtype dt, size_t* bytes)
+{
+    if (!bytes)
+        return fail(LPV_ERR_INVALID_ARG, "bytes must not be NULL");
+    const lpv_status st = check_distill_sizes(M, V, k, dt);
+    if (st != LPV_OK)
+        return st;
+    *bytes = lpv::distill_workspace_bytes(M, V, k, dt);
+    return LPV_OK;
+}
+
+lpv_status lpv_distill(const void* logits, int64_t ldz, int64_t M, int64_t V, lpv_dtype dt,
+                       const int32_t* ids, const float* teacher, int64_t ldt, int32_t k,
+                       double temperature, const float* dloss, float* loss, void* dlogits, int64_t ldd,
+                       int64_t Vd, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const lpv_status st = check_distill_sizes(M, V, k, dt);
+    if (st != LPV_OK)
+        return st;
+    const int es = elem_size(dt);
+    if (!(temperature >= 1e-3) || !(temperature <= 1e3))
+        return fail(LPV_ERR_INVALID_ARG, "temperature must be in [1e-3, 1e3]");
+    if (ldz < V || ldz > MAX_LD || (ldz * es) % 16)
+        return fail(LPV_ERR_INVALID_ARG, "ldz must be in [V, 2^22] and a multiple of 16 bytes");
+    if (dlogits && (Vd < V || ldd < Vd || ldd > MAX_LD || (ldd * es) % 16))
+        return fail(LPV_ERR_INVALID_ARG, "V <= Vd <= ldd <= 2^22 is needed, ldd a multiple of 16 bytes");
+    if (ldt < k || ldt > MAX_LD)
+        return fail(LPV_ERR_INVALID_ARG, "ldt must be in [k, 2^22]");
+    if (M == 0)
+        return LPV_OK;
+    if (!logits || !aligned16(logits) || !aligned16(dlogits))
+        return fail(LPV_ERR_INVALID_ARG, "logits must be non-NULL, and logits and dlogits 16-byte aligned");
+    if (!ids || !teacher || !loss || (uintptr_t)ids % 4 || (uintptr_t)teacher % 4 || (uintptr_t)loss % 4 ||
+        (uintptr_t)dloss % 4)
+        return fail(LPV_ERR_INVALID_ARG, "ids, teacher and loss must be non-NULL, and they and dloss "
+                                         "4-byte aligned");
+    const int64_t nz = ((M - 1) * ldz + V) * es, nd = dlogits ? ((M - 1) * ldd + Vd) * es : 0;
+    const int64_t ne = ((M - 1) * ldt + k) * 4;
+    if (dlogits && !(dlogits == logits && ldd == ldz) && overlap(dlogits, nd, logits, nz))
+        return fail(LPV_ERR_ALIAS, "dlogits may be logits itself, or not overlap it");
+    if (overlap(loss, M * 4, logits, nz) || overlap(loss, M * 4, ids, ne) ||
+        overlap(loss, M * 4, teacher, ne) || (dloss && overlap(loss, M * 4, dloss, M * 4)) ||
+        (dlogits && (overlap(dlogits, nd, loss, M * 4) || overlap(dlogits, nd, ids, ne) ||
+                     overlap(dlogits, nd, teacher, ne) || (dloss && overlap(dlogits, nd, dloss, M * 4)))))
+        return fail(LPV_ERR_ALIAS, "loss and dlogits must not overlap the other inputs or each other");
+    const size_t need = lpv::distill_workspace_bytes(M, V, k, dt);
+    if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+        return fail(LPV_ERR_INVALID_ARG, "workspace: %zu bytes 16-byte aligned are needed", need);
+    const lpv::DistillCall c = {logits, ldz, M, V, (int)dt, ids, teacher, ldt, k, temperature, dloss, loss,
+                                dlogits, ldd, Vd, workspace};
+    const hipError_t e = lpv::launch_distill(c, (hipStream_t)stream);
+    return e == hipSuccess ? LPV_OK : hip_fail(e, "distill launch");
+}
+
+}  // extern "C"

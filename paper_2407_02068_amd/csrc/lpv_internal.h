@@ -221,6 +221,25 @@ void relpos_tables(const int32_t* index, int32_t T, int32_t n_buckets, int32_t n
 size_t relpos_workspace_bytes(const lpv_relpos* h, int64_t n_seq, int32_t H, bool grad);
 hipError_t launch_relpos_attention(const lpv_relpos* h, const RelposCall& c, hipStream_t s);
 hipError_t launch_relpos_grad(const lpv_relpos* h, const RelposCall& c, hipStream_t s);
+// distill.hip
+constexpr int32_t DISTILL_MAX_K = 1024;
+struct DistillCall {
+    const void* logits;  // M x V, row stride ldz
+    int64_t ldz, M, V;
+    int dtype;
+    const int32_t* ids;  // M x k, row stride ldt, as is teacher
+    const float* teacher;
+    int64_t ldt;
+    int32_t k;
+    double temperature;
+    const float* dloss;  // M, or NULL: 1
+    float* loss;         // M
+    void* dlogits;       // M x Vd, row stride ldd, or NULL
+    int64_t ldd, Vd;
+    void* ws;
+};
+size_t distill_workspace_bytes(int64_t M, int64_t V, int32_t k, int dtype);
+hipError_t launch_distill(const DistillCall& c, hipStream_t s);
 hipError_t launch_bias_grad(const void* G, int64_t ldg, int64_t M, int64_t N, int dtype, void* db,
                             hipStream_t s);
 // The same with the partial sums in a fixed device array of this many floats

@@ -25,7 +25,8 @@ EXPORTED = ("lpv_bsr_pack", "lpv_bsr_info_get", "lpv_bsr_export", "lpv_bsr_sched
             "lpv_delta_curve", "lpv_delta_curve_ws", "lpv_delta_curve_workspace_size",
             "lpv_add_layernorm", "lpv_attention", "lpv_relpos_create", "lpv_relpos_destroy",
             "lpv_relpos_workspace_size", "lpv_relpos_attention", "lpv_relpos_attention_grad",
-            "lpv_bsr_destroy", "lpv_status_str", "lpv_last_error")
+            "lpv_distill", "lpv_distill_workspace_size", "lpv_bsr_destroy", "lpv_status_str",
+            "lpv_last_error")
 
 
 class LpvError(RuntimeError):
@@ -86,12 +87,16 @@ def lib():
                                        vp, ctypes.c_size_t, vp]
     L.lpv_relpos_attention_grad.argtypes = [vp, vp, vp, i64, i64, i32, i32, i32, vp, i64, vp, i64,
                                             vp, vp, i64, vp, i64, vp, vp, ctypes.c_size_t, vp]
+    L.lpv_distill.argtypes = [vp, i64, i64, i64, i32, vp, vp, i64, i32, ctypes.c_double, vp, vp, vp,
+                              i64, i64, vp, ctypes.c_size_t, vp]
+    L.lpv_distill_workspace_size.argtypes = [i64, i64, i32, i32, size_p]
     for f in ("lpv_bsr_pack", "lpv_bsr_info_get", "lpv_bsr_export", "lpv_bsr_schedule_export",
               "lpv_bsr_unpack", "lpv_bsr_linear", "lpv_dense_linear", "lpv_mask_topk",
               "lpv_bsr_transpose", "lpv_bsr_grad_w", "lpv_bias_grad", "lpv_bias_grad_noalloc",
               "lpv_delta_curve", "lpv_delta_curve_ws", "lpv_delta_curve_workspace_size",
               "lpv_add_layernorm", "lpv_attention", "lpv_relpos_create",
-              "lpv_relpos_workspace_size", "lpv_relpos_attention", "lpv_relpos_attention_grad"):
+              "lpv_relpos_workspace_size", "lpv_relpos_attention", "lpv_relpos_attention_grad",
+              "lpv_distill", "lpv_distill_workspace_size"):
         getattr(L, f).restype = i32
     L.lpv_bsr_destroy.argtypes = [vp]
     L.lpv_bsr_destroy.restype = None
@@ -603,3 +608,69 @@ def relpos_attention_grad(rp, table, qkv, out, lse, dout, n_seq, H, region=None,
                                            ctypes.c_void_p(dtable.data_ptr()), wp, nbytes,
                                            _stream(stream)), "lpv_relpos_attention_grad")
     return dqkv, dtable
+
+
+def distill_workspace_size(M, V, k, dtype):
+    """lpv_distill_workspace_size: bytes of the workspace of ``distill_loss`` and
+    ``distill_grad``."""
+    nbytes = ctypes.c_size_t(0)
+    _check(lib().lpv_distill_workspace_size(M, V, k, DTYPES[dtype], ctypes.byref(nbytes)),
+           "lpv_distill_workspace_size")
+    return nbytes.value
+
+
+def _distill(logits, ids, teacher, temperature, dloss, loss, dlogits, Vd, workspace, stream):
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in DTYPES:
+        raise ValueError("logits must be a 2-D tensor of float32, float16 or bfloat16")
+    M, V = logits.shape
+    for t, name, dtype in ((ids, "ids", torch.int32), (teacher, "teacher", torch.float32)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != dtype \
+                or t.shape[0] != M or t.shape != ids.shape or (t.shape[1] > 1 and M and t.stride(1) != 1):
+            raise ValueError("%s must be an M x k tensor of %s with unit column stride" % (name, dtype))
+    k = ids.shape[1]
+    ldt = ids.stride(0) if M > 1 else k
+    if M > 1 and teacher.stride(0) != ldt:
+        raise ValueError("ids and teacher must have the same row stride")
+    if loss is None:
+        loss = torch.empty(M, dtype=torch.float32, device=logits.device)
+    for t, name in ((loss, "loss"), (dloss, "dloss")):
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (M,) or not t.is_contiguous()):
+            raise ValueError("%s must be a contiguous float32 tensor of M elements" % name)
+    _on_current(("logits", logits), ("ids", ids), ("teacher", teacher), ("dloss", dloss),
+                ("loss", loss), ("dlogits", dlogits), ("workspace", workspace))
+    pad = 16 // logits.element_size()
+
+    def rows(t, name, cols):
+        p, ld = _rows(t, name, M, V, logits.dtype)
+        # (one row's stride says nothing: any that covers it)
+        return p, ld if M > 1 else (cols + pad - 1) // pad * pad
+    zp, ldz = rows(logits, "logits", V)
+    dp, ldd = rows(dlogits, "dlogits", Vd) if dlogits is not None else (None, 0)
+    wp, nbytes, keep = _workspace(workspace, distill_workspace_size(M, V, k, logits.dtype), logits.device,
+                                  stream)
+    vec = lambda t: ctypes.c_void_p(t.data_ptr() if t is not None else 0)
+    _check(lib().lpv_distill(zp, ldz, M, V, DTYPES[logits.dtype], vec(ids), vec(teacher), ldt, k,
+                             float(temperature), vec(dloss), vec(loss), dp, ldd, Vd, wp, nbytes,
+                             _stream(stream)), "lpv_distill")
+    return loss
+
+
+def distill_loss(logits, ids, teacher, temperature, loss=None, workspace=None, stream=None):
+    """lpv_distill without a gradient: the distillation loss of each row of the logits (M x V)
+    from a teacher's top logits (ids int32 and teacher float32, M x k; an id outside [0, V):
+    no entry).  Returns M float32."""
+    return _distill(logits, ids, teacher, temperature, None, loss, None, 0, workspace, stream)
+
+
+def distill_grad(logits, ids, teacher, temperature, dloss=None, loss=None, dlogits=None,
+                 workspace=None, stream=None):
+    """lpv_distill: (loss, dlogits), for the gradient ``dloss`` at each row's loss (M float32;
+    None: 1).  dlogits is allocated in rows padded to 16 columns, the padding zero, as the
+    linear calls take it; it may be given, and may be the logits themselves."""
+    Vd = logits.shape[1]
+    if dlogits is None:
+        Vd = (Vd + 15) // 16 * 16
+        wide = torch.empty((logits.shape[0], Vd), dtype=logits.dtype, device=logits.device)
+        dlogits = wide[:, :logits.shape[1]]
+    loss = _distill(logits, ids, teacher, temperature, dloss, loss, dlogits, Vd, workspace, stream)
+    return loss, dlogits

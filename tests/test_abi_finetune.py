@@ -106,3 +106,42 @@ def grad(L, p=H_PTR, table=FAKE, qkv=FAKE + G, ldq=288, n=4, H=3, hd=32, dt=2, r
 def test_relpos_grad_refuses(L, kw, want):
     assert grad(L, **kw) == want
     assert L.lpv_last_error().decode() != ""
+
+
+def distill(L, z=FAKE, ldz=1008, M=10, V=1000, dt=2, ids=FAKE + G, t=FAKE + 2 * G, ldt=16, k=16, tau=1.0,
+            g=0, loss=FAKE + 3 * G, d=FAKE + 4 * G, ldd=1008, Vd=1008, ws=0, wsb=0):
+    return L.lpv_distill(z, ldz, M, V, dt, ids, t, ldt, k, ctypes.c_double(tau), g, loss, d, ldd, Vd, ws,
+                         wsb, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(dt=3), DTYPE), (dict(dt=-1), DTYPE), (dict(M=-1), SHAPE), (dict(M=1 << 31), SHAPE),
+    (dict(V=0), SHAPE), (dict(V=(1 << 22) + 1), SHAPE), (dict(k=0), SHAPE), (dict(k=1025), SHAPE),
+    (dict(tau=0.0), INVALID), (dict(tau=-1.0), INVALID), (dict(tau=float("nan")), INVALID),
+    (dict(tau=1e4), INVALID), (dict(tau=float("inf")), INVALID), (dict(ldz=999), INVALID),
+    (dict(ldz=1004), INVALID), (dict(ldz=(1 << 22) + 8), INVALID), (dict(ldd=1000), INVALID),
+    (dict(ldd=1012), INVALID), (dict(Vd=999), INVALID), (dict(ldt=15), INVALID), (dict(z=0), INVALID),
+    (dict(z=FAKE + 8), INVALID), (dict(d=FAKE + 4 * G + 8), INVALID), (dict(ids=0), INVALID),
+    (dict(t=0), INVALID), (dict(loss=0), INVALID), (dict(loss=FAKE + 3 * G + 2), INVALID),
+    (dict(g=FAKE + 5 * G + 1), INVALID), (dict(ids=FAKE + G + 3), INVALID), (dict(d=FAKE + 16), ALIAS),
+    (dict(d=FAKE, ldd=1016), ALIAS), (dict(loss=FAKE + 64), ALIAS), (dict(loss=FAKE + G + 4), ALIAS),
+    (dict(loss=FAKE + 4 * G), ALIAS), (dict(d=FAKE + 2 * G - 16), ALIAS),
+    (dict(g=FAKE + 3 * G + 4), ALIAS), (dict(g=FAKE + 4 * G + 400), ALIAS),
+    # few long rows need a workspace
+    (dict(M=2, V=100000, ldz=100000, ldd=100000, Vd=100000), INVALID),
+    (dict(M=2, V=100000, ldz=100000, ldd=100000, Vd=100000, ws=FAKE + 6 * G, wsb=8), INVALID),
+    (dict(M=2, V=100000, ldz=100000, ldd=100000, Vd=100000, ws=FAKE + 6 * G + 8, wsb=1 << 20), INVALID)])
+def test_distill_refuses(L, kw, want):
+    assert distill(L, **kw) == want
+    assert L.lpv_last_error().decode() != ""
+
+
+def test_distill_without_rows_and_its_workspace(L):
+    assert distill(L, M=0, z=0, ids=0, t=0, loss=0, d=0) == OK
+    b = ctypes.c_size_t(0)
+    size = lambda M, V, k=16, dt=2: L.lpv_distill_workspace_size(M, V, k, dt, ctypes.byref(b))
+    assert size(256, 1000) == OK and b.value == 0
+    assert size(2, 100000) == OK and 0 < b.value <= 2 * (100000 // 8 // 256 * 8 + 4)
+    assert size(0, 100000) == OK and b.value == 0
+    assert size(2, 0) == SHAPE and size(-1, 5) == SHAPE and size(2, 5, 0) == SHAPE and size(2, 5, 4, 7) == DTYPE
+    assert L.lpv_distill_workspace_size(2, 5, 4, 2, None) == INVALID
