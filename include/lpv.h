@@ -466,8 +466,8 @@ lpv_status lpv_relpos_workspace_size(const lpv_relpos* p, int64_t n_seq, int32_t
  * workspace  device, 16-byte aligned, at least lpv_relpos_workspace_size bytes (may be
  *         NULL if that is 0); owned by the caller, who must not reuse it before the call's
  *         work has finished.  Needs no clearing.
- * hd = 32 or 64, H in [1, 64], 16-bit element types; n_seq T and n_seq H below 2^31; ldq
- * and ldo multiples of 16 bytes, at most 2^22 elements.  Scores, softmax and sums in
+ * hd = 32 or 64, H in [1, 64], 16-bit element types; n_seq T and n_seq H ceil(T / 32)
+ * below 2^31; ldq and ldo multiples of 16 bytes, at most 2^22 elements.  Scores, softmax and sums in
  * float32; the weights are rounded once to the element type for the product with V.  Apart
  * from padding tokens, non-finite values in qkv are outside the contract.  A call gives the
  * same bits every time.  No allocation, no host synchronisation.

@@ -27,7 +27,9 @@ FLAGS = [
 # register counts accumulators in AGPRs would be copied across every branch.
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 SOURCE_FLAGS = {"linear.hip": _VGPR_MFMA, "backward.hip": _VGPR_MFMA, "encoder.hip": _VGPR_MFMA,
-                "stationary.hip": _VGPR_MFMA, "relpos.hip": _VGPR_MFMA}
+                "stationary.hip": _VGPR_MFMA,
+                # (a maximum then takes its operands as they are, without quieting NaNs first)
+                "relpos.hip": _VGPR_MFMA + ["-fno-honor-nans"]}
 BUILD_DIR = os.path.join(HERE, "_build")
 
 

@@ -866,7 +866,7 @@ lpv_status check_relpos(const lpv_relpos* p, const void* table, const void* qkv,
         return fail(LPV_ERR_SHAPE, "head dimension %d is not supported (32 or 64)", hd);
     if (H < 1 || H > 64)
         return fail(LPV_ERR_SHAPE, "H = %d is out of range [1, 64]", H);
-    if (n_seq < 0 || n_seq >= MAX_M || n_seq * p->T >= MAX_M || n_seq * H >= MAX_M)
+    if (n_seq < 0 || n_seq >= MAX_M || n_seq * p->T >= MAX_M || n_seq * p->nt * H >= MAX_M)
         return fail(LPV_ERR_SHAPE, "n_seq = %lld is out of range", (long long)n_seq);
     if (!table || (uintptr_t)table % 2)
         return fail(LPV_ERR_INVALID_ARG, "table must be non-NULL and aligned to its element size");
@@ -991,7 +991,7 @@ lpv_status lpv_relpos_workspace_size(const lpv_relpos* p, int64_t n_seq, int32_t
         return fail(LPV_ERR_INVALID_ARG, "handle and bytes must not be NULL");
     if (H < 1 || H > 64)
         return fail(LPV_ERR_SHAPE, "H = %d is out of range [1, 64]", H);
-    if (n_seq < 0 || n_seq >= MAX_M || n_seq * p->T >= MAX_M || n_seq * H >= MAX_M)
+    if (n_seq < 0 || n_seq >= MAX_M || n_seq * p->T >= MAX_M || n_seq * p->nt * H >= MAX_M)
         return fail(LPV_ERR_SHAPE, "n_seq = %lld is out of range", (long long)n_seq);
     *bytes = lpv::relpos_workspace_bytes(p, n_seq, H, grad != 0);
     return LPV_OK;

@@ -11,6 +11,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "lpv_attention.h"
 #include "lpv_grid.h"
 #include "lpv_internal.h"
@@ -18,7 +20,7 @@
 namespace lpv {
 namespace {
 
-constexpr int BLK = 64;  // rows of a staged block
+constexpr float LAZY = 8.0f;
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // What the kernels read: qkv rows of the framework's layout, region labels.
@@ -31,6 +33,12 @@ struct Rp {
     const float* bias;  // tiles of the bias (k_relpos_bias)
 };
 
+// The labels of a sequence (n_seq and n_region are below 2^31).
+__device__ inline const int32_t* labels(const Rp& p, int64_t seq)
+{
+    return p.region + (int64_t)((uint32_t)seq % (uint32_t)p.n_region) * p.T;
+}
+
 template <int HD> struct Row {
     static constexpr int KS = HD / 16;     // 16-dimension steps of a product over the head
     static constexpr int DT = HD / 32;     // 32-dimension tiles of an output
@@ -38,15 +46,40 @@ template <int HD> struct Row {
                                            // 16-byte column sit in distinct banks
 };
 
+// The wave's number in the workgroup, as the uniform value that it is.
+__device__ inline int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
 __device__ inline uint32_t lds32(const void* p)
 {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
 
-// The tile's bias in matrix-core accumulator order, times sqrt(hd) (so that it is the
+// A tile's bias in matrix-core accumulator order, times sqrt(hd) (so that it is the
 // accumulator's start value), -inf where the pair takes no part.  idx: Tp x Tp, -1 past T.
 // Tile (a, b): rows 32 a of idx, columns 32 b; lane l holds row l % 32 and, in element r,
-// column 8 (r / 4) + 4 (l / 32) + r % 4.
+// column 8 (r / 4) + 4 (l / 32) + r % 4; in memory [r / 4][lane][r % 4], so that a wave's
+// loads and stores are whole lines.
+
+// Elements 4 g .. 4 g + 3 of this lane.
+template <int DT>
+__device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, int g, int lane,
+                                     const uint16_t* table, int H, int h, float root)
+{
+    constexpr uint16_t LOWEST = DT == LPV_BF16 ? 0xff7f : 0xfbff, NEG_INF = DT == LPV_BF16 ? 0xff80 : 0xfc00;
+    const uint2 v = *(const uint2*)(idx + ((int64_t)a * 32 + (lane & 31)) * (nt * 32) + b * 32 + 4 * (lane >> 5) + 8 * g);
+    const uint16_t* e = (const uint16_t*)&v;
+    float4 o;
+    float* of = (float*)&o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint16_t t = e[j] == 0xffff ? NEG_INF : table[(int64_t)e[j] * H + h];
+        // (a finite bias stays finite: the product's overflow would mask the pair)
+        const float f = fminf(fmaxf(Elem<DT>::to_f32(t) * root, -3e38f), 3e38f);
+        of[j] = t == LOWEST || t == NEG_INF ? -INFINITY : f;
+    }
+    return o;
+}
+
 template <int DT>
 __global__ __launch_bounds__(256) void k_relpos_bias(const uint16_t* __restrict__ idx, int32_t nt,
                                                      const uint16_t* __restrict__ table, int32_t H,
@@ -58,24 +91,10 @@ __global__ __launch_bounds__(256) void k_relpos_bias(const uint16_t* __restrict_
     if (tile >= n_tiles)
         return;
     const int a = (int)(tile / nt), b = (int)(tile - (int64_t)a * nt);
-    const uint16_t* src = idx + ((int64_t)a * 32 + (lane & 31)) * (nt * 32) + b * 32 + 4 * (lane >> 5);
-    float* dst = bias + ((int64_t)h * n_tiles + tile) * 1024 + lane * 16;
-    constexpr uint16_t LOWEST = DT == LPV_BF16 ? 0xff7f : 0xfbff, NEG_INF = DT == LPV_BF16 ? 0xff80 : 0xfc00;
+    float* dst = bias + ((int64_t)h * n_tiles + tile) * 1024 + lane * 4;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        const uint2 v = *(const uint2*)(src + 8 * g);
-        const uint16_t* e = (const uint16_t*)&v;
-        float4 o;
-        float* of = (float*)&o;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint16_t t = e[j] == 0xffff ? NEG_INF : table[(int64_t)e[j] * H + h];
-            // (a finite bias stays finite: the product's overflow would mask the pair)
-            const float f = fminf(fmaxf(Elem<DT>::to_f32(t) * root, -3e38f), 3e38f);
-            of[j] = t == LOWEST || t == NEG_INF ? -INFINITY : f;
-        }
-        *(float4*)(dst + 4 * g) = o;
-    }
+    for (int g = 0; g < 4; ++g)
+        *(float4*)(dst + 256 * g) = gather_bias<DT>(idx, nt, a, b, g, lane, table, H, h, root);
 }
 
 __device__ inline f32x16 load_bias(const float* p)
@@ -83,7 +102,7 @@ __device__ inline f32x16 load_bias(const float* p)
     f32x16 s;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        const float4 v = *(const float4*)(p + 4 * g);
+        const float4 v = *(const float4*)(p + 256 * g);
         s[4 * g] = v.x;
         s[4 * g + 1] = v.y;
         s[4 * g + 2] = v.z;
@@ -92,11 +111,11 @@ __device__ inline f32x16 load_bias(const float* p)
     return s;
 }
 
-// BLK rows of a head's slices of two matrices, from global memory through registers into
+// ROWS rows of a head's slices of two matrices, from global memory through registers into
 // LDS, zero past T and for padding tokens (whose values, NaN too, then reach nothing).
-template <int HD, int NT, bool REG> struct Stage {
+template <int HD, int NT, int ROWS, bool REG> struct Stage {
     static constexpr int CH = HD / 8;                    // 16-byte chunks per row
-    static constexpr int N = (BLK * CH + NT - 1) / NT;   // chunks per thread and matrix
+    static constexpr int N = (ROWS * CH + NT - 1) / NT;   // chunks per thread and matrix
     uint4 a[N], b[N];
     __device__ inline void load(const uint16_t* pa, int64_t lda, const uint16_t* pb, int64_t ldb,
                                 int row0, int T, const int32_t* reg)
@@ -106,7 +125,7 @@ template <int HD, int NT, bool REG> struct Stage {
             const int c = threadIdx.x + i * NT, r = row0 + c / CH, k = c % CH;
             a[i] = uint4{0u, 0u, 0u, 0u};
             b[i] = uint4{0u, 0u, 0u, 0u};
-            bool ok = r < T && c < BLK * CH;
+            bool ok = r < T && c < ROWS * CH;
             if (REG && ok)
                 ok = reg[r] >= 0;
             if (ok) {
@@ -120,7 +139,7 @@ template <int HD, int NT, bool REG> struct Stage {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = threadIdx.x + i * NT;
-            if (BLK * CH % NT == 0 || c < BLK * CH) {
+            if (ROWS * CH % NT == 0 || c < ROWS * CH) {
                 *(uint4*)(la + c / CH * Row<HD>::RS + 16 * (c % CH)) = a[i];
                 *(uint4*)(lb + c / CH * Row<HD>::RS + 16 * (c % CH)) = b[i];
             }
@@ -153,6 +172,20 @@ template <typename F, int HD> __device__ inline F tr_frag(uint32_t base, int row
     return as_frag<F>(uint4{lo.x, lo.y, hi.x, hi.y});
 }
 
+// The maximum, or sum, of a value in lanes l and l ^ 32.
+__device__ inline float half_max(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float half_add(float v)
+{
+    const uint32_t u = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // s = -inf where the labels of this lane's token and of the element's differ.
 __device__ inline void mask_region(f32x16& s, int mine, const int32_t* lab, int half)
 {
@@ -171,18 +204,34 @@ __device__ inline void mask_region(f32x16& s, int mine, const int32_t* lab, int 
 constexpr int32_t NO_LABEL = INT32_MIN;
 
 // 32 rows of an output whose accumulators hold one row per lane (l % 32), dimensions
-// 8 (r / 4) + 4 half + r % 4 of each 32-dimension tile.
+// 8 (r / 4) + 4 half + r % 4 of each 32-dimension tile: lanes l and l ^ 32 swap halves, so
+// that each stores 16 bytes at a time.
 template <int DT, int HD>
 __device__ inline void store_rows(uint16_t* row, const f32x16* o, float f, int half)
 {
 #pragma unroll
     for (int dt = 0; dt < HD / 32; ++dt)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
-            *(uint2*)(row + 32 * dt + 8 * g + 4 * half) =
-                uint2{pack2<DT>(o[dt][4 * g] * f, o[dt][4 * g + 1] * f),
-                      pack2<DT>(o[dt][4 * g + 2] * f, o[dt][4 * g + 3] * f)};
+        for (int g = 0; g < 4; g += 2) {
+            uint32_t w[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    w[i][j] = pack2<DT>(o[dt][4 * (g + i) + 2 * j] * f, o[dt][4 * (g + i) + 2 * j + 1] * f);
+            const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+            const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+            *(uint4*)(row + 32 * dt + 8 * g + 8 * half) = uint4{x[0], y[0], x[1], y[1]};
+        }
 }
+
+// How a workgroup of the general kernels is laid out: QW 32-row tiles of one sequence and
+// head, KS waves to each; the other side's rows pass in blocks of B, of which a wave takes
+// NI 32-row tiles.
+template <int QW_, int KS_> struct Shape {
+    static constexpr int QW = QW_, KS = KS_, NW = QW_ * KS_, NT = 64 * NW;
+    static constexpr int NI = KS_ == 1 ? 2 : 1, B = 32 * NI * KS_;
+};
 
 // Workgroup -> (sequence, head, block of row tiles).
 struct Place {
@@ -192,111 +241,177 @@ struct Place {
 };
 __device__ inline Place place(const Rp& p, int n_blk)
 {
-    const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int64_t u = id / p.n_seq;  // the sequences of one head's block follow each other
-    return {id - u * p.n_seq, (int)(u / n_blk), (int)(u % n_blk), u < (int64_t)p.H * n_blk};
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;  // (below 2^31 + 2^20)
+    const uint32_t u = id / (uint32_t)p.n_seq;  // the sequences of one head's block follow each other
+    const uint32_t h = u / (uint32_t)n_blk;
+    return {(int64_t)(id - u * (uint32_t)p.n_seq), (int)h, (int)(u - h * (uint32_t)n_blk), h < (uint32_t)p.H};
+}
+
+// The label of a token that attends (mine) or is attended (theirs); 0 without labels.
+template <bool REG> __device__ inline int label_mine(const int32_t* reg, int i)
+{
+    return !REG ? 0 : reg[i] < 0 ? NO_LABEL : reg[i];
+}
+
+// The pipeline of a general kernel: the next block's rows in flight while a block is worked
+// on, and the bias tiles of the next step.  step(nj, first row of the step in the block, the
+// block's rows in LDS, block % 2, the tiles' bias) takes J tiles at once (fewer at the end).
+// A step's bias is asked for before the rows that are asked for in the same block, so that
+// its wait is not for them too.
+template <int HD, typename Sh, bool REG, int J, typename LoadMore, typename StoreMore, typename Step>
+__device__ inline void pass_blocks(const Rp& p, const uint16_t* a, int64_t lda, const uint16_t* b,
+                                   int64_t ldb, const int32_t* reg, const float* bias, bool busy, int part,
+                                   char* buf, LoadMore&& load_more, StoreMore&& store_more, Step&& step)
+{
+    constexpr int HALF = Sh::B * Row<HD>::RS;  // buf: [2][2][HALF]
+    constexpr int NI = Sh::NI;
+    static_assert(J == 1 || J == NI, "a step is a tile or the wave's part of a block");
+    const int n_b = (p.T + Sh::B - 1) / Sh::B;
+    Stage<HD, Sh::NT, Sh::B, REG> st;
+    auto load_tiles = [&](f32x16* t, int blk, int i) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            t[j] = load_bias(bias + (int64_t)min(blk * NI * Sh::KS + part + i + j, p.nt - 1) * 1024);
+    };
+    f32x16 next[J];
+    load_tiles(next, 0, 0);
+    st.load(a, lda, b, ldb, 0, p.T, reg);
+    load_more(0);
+    st.store(buf, buf + HALF);
+    store_more(0);
+    __syncthreads();
+    for (int blk = 0; blk < n_b; ++blk) {
+        char* at = buf + (blk & 1) * 2 * HALF;
+        char* to = buf + (~blk & 1) * 2 * HALF;
+        const bool more = blk + 1 < n_b;
+#pragma unroll
+        for (int i = 0; i < NI; i += J) {
+            f32x16 cur[J];
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                cur[j] = next[j];
+            if (i + J < NI)
+                load_tiles(next, blk, i + J);
+            else
+                load_tiles(next, blk + 1, 0);
+            if (i == 0 && more) {
+                st.load(a, lda, b, ldb, (blk + 1) * Sh::B, p.T, reg);
+                load_more(blk + 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const int t = blk * NI * Sh::KS + part + i;
+            if (busy && t < p.nt) {
+                if (J == 1 || t + 1 < p.nt)
+                    step(std::integral_constant<int, J>(), 32 * (part + i), at, at + HALF, blk & 1, cur);
+                else
+                    step(std::integral_constant<int, 1>(), 32 * (part + i), at, at + HALF, blk & 1, cur);
+            }
+        }
+        if (more) {
+            st.store(to, to + HALF);
+            store_more(~blk & 1);
+        }
+        __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------- forward
 
-// A workgroup of NW waves takes NW 32-query tiles of one sequence and head, a wave one of
-// them; the keys pass in blocks of 64 through a double buffer in LDS, the next block's
-// loads in flight meanwhile.  S^T = K Q^T starts from the bias in the accumulator, so a row
-// of the softmax lives in lanes l and l ^ 32; the weights, rounded once to the element
-// type, are then the B operand of O^T = V^T P^T (V^T by transposing LDS reads).  The
-// row's sum adds the weights before that rounding, so that lse is exact to float32.
-template <int DT, int HD, int NW, bool REG>
-__global__ __launch_bounds__(64 * NW) void k_relpos_fwd(Rp p, uint16_t* __restrict__ out, int64_t ldo,
-                                                        float* __restrict__ lse, float scale)
+// A wave holds a 32-query tile; the keys pass in blocks through a double buffer in LDS.
+// S^T = K Q^T starts from the bias in the accumulator, so a row of the softmax lives in
+// lanes l and l ^ 32; the weights, rounded once to the element type, are then the B operand
+// of O^T = V^T P^T (V^T by transposing LDS reads).  The row's sum adds the weights before
+// that rounding, so that lse is exact to float32; each lane adds its own, the two of a row
+// meet at the end.  With KS = 2 two waves share a tile's keys and join their rows in LDS.
+template <int DT, int HD, typename Sh, bool REG>
+__global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, uint16_t* __restrict__ out, int64_t ldo,
+                                                       float* __restrict__ lse, float scale)
 {
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT;
-    __shared__ __attribute__((aligned(16))) char kv[2][2][BLK * RS];
-    __shared__ __attribute__((aligned(16))) int32_t lab[2][BLK];
-    const int T = p.T, n_blk = (p.nt + NW - 1) / NW;
-    const Place at = place(p, n_blk);
+    __shared__ __attribute__((aligned(16))) char kv[4 * Sh::B * RS];
+    __shared__ __attribute__((aligned(16))) int32_t lab[2][Sh::B];
+    const int T = p.T;
+    const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
     if (!at.ok)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     const uint16_t* base = p.qkv + at.seq * T * ldq + at.h * HD;
-    const int32_t* reg = REG ? p.region + at.seq % p.n_region * T : nullptr;
-    const int qt = at.blk * NW + wave, q = qt * 32 + l32;
+    const int32_t* reg = REG ? labels(p, at.seq) : nullptr;
+    const int part = wave % Sh::KS, qt = at.blk * Sh::QW + wave / Sh::KS, q = qt * 32 + l32;
     const bool busy = qt < p.nt;
+    const int mine = label_mine<REG>(reg, min(q, T - 1));
     F qf[KS];
-    load_frags<F, HD>(qf, base + (int64_t)min(q, T - 1) * ldq, half, busy);
-    int mine = 0;
-    if (REG) {
-        mine = reg[min(q, T - 1)];
-        mine = mine < 0 ? NO_LABEL : mine;
-    }
-    Stage<HD, 64 * NW, REG> st;
-    auto load_labels = [&](int b) {
-        int32_t v = -1;
-        const int r = b * BLK + threadIdx.x;
-        if (REG && threadIdx.x < BLK && r < T)
-            v = max(reg[r], -1);
-        return v;
-    };
-    st.load(base + hw, ldq, base + 2 * hw, ldq, 0, T, reg);
-    int32_t lv = load_labels(0);
-    const int n_kb = (T + BLK - 1) / BLK;
-    const float* bt = p.bias + (((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt) * 1024 + lane * 16;
-    f32x16 bn = load_bias(bt);
-    st.store(kv[0][0], kv[0][1]);
-    if (REG && threadIdx.x < BLK)
-        lab[0][threadIdx.x] = lv;
-    __syncthreads();
+    load_frags<F, HD>(qf, base + (int64_t)min(q, T - 1) * ldq, half, busy && mine != NO_LABEL);
     f32x16 o[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
         o[d] = f32x16{};
     float m = -INFINITY, l = 0.0f;
-    for (int b = 0; b < n_kb; ++b) {
-        const int cur = b & 1;
-        if (b + 1 < n_kb) {
-            st.load(base + hw, ldq, base + 2 * hw, ldq, (b + 1) * BLK, T, reg);
-            lv = load_labels(b + 1);
-        }
-        if (busy) {
-            const uint32_t ka = lds32(kv[cur][0]) + l32 * RS + half * 16;
-            const uint32_t va = tr_base<HD>(kv[cur][1], lane);
-            for (int i = 0; i < 2; ++i) {
-                const int kt = 2 * b + i;
-                if (kt >= p.nt)
-                    break;
-                f32x16 s = bn;
-                bn = load_bias(bt + (int64_t)min(kt + 1, p.nt - 1) * 1024);
+    int32_t lv = -1;
+    pass_blocks<HD, Sh, REG, 1>(
+        p, base + hw, ldq, base + 2 * hw, ldq, reg,
+        p.bias + ((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, kv,
+        [&](int blk) {
+            const int r = blk * Sh::B + threadIdx.x;
+            if (REG && threadIdx.x < Sh::B)
+                lv = r < T ? max(reg[r], -1) : -1;
+        },
+        [&](int b) {
+            if (REG && threadIdx.x < Sh::B)
+                lab[b][threadIdx.x] = lv;
+        },
+        [&](auto ni, int row0, const char* kb, const char* vb, int b, const f32x16* bias) {
+            constexpr int NI = decltype(ni)::value;
+            const uint32_t ka = lds32(kb) + (row0 + l32) * RS + half * 16;
+            const uint32_t va = tr_base<HD>(vb, lane) + row0 * RS;
+            f32x16 s[NI];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    s = E::mma(as_frag<F>(att_read16(ka + i * 32 * RS + 32 * ks)), qf[ks], s);
+            for (int i = 0; i < NI; ++i)
+                s[i] = bias[i];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+                    s[i] = E::mma(as_frag<F>(att_read16(ka + i * 32 * RS + 32 * ks)), qf[ks], s[i]);
+            float mt = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
                 if (REG)
-                    mask_region(s, mine, lab[cur] + 32 * i, half);
-                float mt = s[0];
+                    mask_region(s[i], mine, lab[b] + row0 + 32 * i, half);
+                float t[4];
 #pragma unroll
-                for (int r = 1; r < 16; ++r)
-                    mt = fmaxf(mt, s[r]);
-                mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-                const float mn = fmaxf(m, mt);
-                const float ref = mn == -INFINITY ? 0.0f : mn;  // (nothing yet: all weights 0)
-                const float nms = -ref * scale;
-                const float alpha = __builtin_amdgcn_exp2f((m - ref) * scale);
-                float ps = 0.0f;
-                uint32_t pb[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * j], scale, nms));
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], scale, nms));
-                    ps += e0 + e1;
-                    pb[j] = pack2<DT>(e0, e1);
-                }
-                ps += __shfl_xor(ps, 32, 64);
-                l = l * alpha + ps;
-                m = mn;
+                for (int j = 0; j < 4; ++j)
+                    t[j] = fmaxf(fmaxf(s[i][j], s[i][j + 4]), fmaxf(s[i][j + 8], s[i][j + 12]));
+                mt = fmaxf(mt, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
+            }
+            mt = half_max(mt);
+            // the weights' reference m follows a row's maximum when that is over 2^8 weights
+            // above it: most tiles then need no rescaling (each row by its own scores)
+            const bool far = mt > m + LAZY / scale;
+            if (__any(far)) {
+                const float alpha = far ? __builtin_amdgcn_exp2f((m - mt) * scale) : 1.0f;
+                m = far ? mt : m;
+                l *= alpha;
 #pragma unroll
                 for (int d = 0; d < ND; ++d)
                     o[d] *= alpha;
+            }
+            const float nms = m == -INFINITY ? 0.0f : -m * scale;  // (nothing yet: all weights 0)
+            float ps[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                uint32_t pb[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j], scale, nms));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j + 1], scale, nms));
+                    ps[0] += e0;
+                    ps[1] += e1;
+                    pb[j] = pack2<DT>(e0, e1);
+                }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const F pf = as_frag<F>(uint4{pb[4 * t], pb[4 * t + 1], pb[4 * t + 2], pb[4 * t + 3]});
@@ -305,142 +420,174 @@ __global__ __launch_bounds__(64 * NW) void k_relpos_fwd(Rp p, uint16_t* __restri
                         o[d] = E::mma(tr_frag<F, HD>(va, 32 * i + 16 * t, d), pf, o[d]);
                 }
             }
-        }
-        if (b + 1 < n_kb) {
-            st.store(kv[1 - cur][0], kv[1 - cur][1]);
-            if (REG && threadIdx.x < BLK)
-                lab[1 - cur][threadIdx.x] = lv;
+            l += ps[0] + ps[1];
+        });
+    l = half_add(l);
+    if constexpr (Sh::KS == 2) {  // (every wave has left the blocks)
+        float* j = (float*)kv + (wave / 2) * (ND * 16 + 2) * 64 + lane;
+        static_assert(Sh::QW * (ND * 16 + 2) * 256 <= (int)sizeof(kv), "the joined rows fit");
+        if (part == 1) {
+            j[0] = m;
+            j[64] = l;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    j[64 * (2 + 16 * d + r)] = o[d][r];
         }
         __syncthreads();
+        if (part == 1)
+            return;
+        const float m1 = j[0], mn = fmaxf(m, m1), ref = mn == -INFINITY ? 0.0f : mn;
+        const float a0 = __builtin_amdgcn_exp2f((m - ref) * scale), a1 = __builtin_amdgcn_exp2f((m1 - ref) * scale);
+        m = mn;
+        l = l * a0 + j[64] * a1;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                o[d][r] = o[d][r] * a0 + j[64 * (2 + 16 * d + r)] * a1;
     }
     if (busy && q < T) {
         store_rows<DT, HD>(out + (at.seq * T + q) * ldo + at.h * HD, o, l > 0.0f ? 1.0f / l : 0.0f, half);
         if (lse && half == 0)
-            lse[(at.seq * p.H + at.h) * T + q] =
-                l > 0.0f ? LN2 * (m * scale + __log2f(l)) : -INFINITY;
+            lse[(at.seq * p.H + at.h) * T + q] = l > 0.0f ? LN2 * (m * scale + __log2f(l)) : -INFINITY;
     }
 }
 
 // ---------------------------------------------------------------- gradients
 
+// Adds the accumulators of the second of two waves to the first's; false for the second.
+template <int N> __device__ inline bool join_sums(char* buf, f32x16* o, int wave)
+{
+    float* j = (float*)buf + (wave / 2) * N * 1024 + (threadIdx.x & 63);
+    if (wave % 2) {
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                j[64 * (16 * d + r)] = o[d][r];
+    }
+    __syncthreads();
+    if (wave % 2)
+        return false;
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            o[d][r] += j[64 * (16 * d + r)];
+    return true;
+}
+
 // dQ, tiled as the forward: the weights come back from lse, dP^T = V dO^T, and dS^T,
 // rounded once, is the B operand of dQ^T = K^T dS^T.  D = dO . O is formed first and kept
 // for the next kernel.
-template <int DT, int HD, int NW, bool REG>
-__global__ __launch_bounds__(64 * NW) void k_relpos_dq(Rp p, const uint16_t* __restrict__ out,
-                                                       int64_t ldo, const float* __restrict__ lse,
-                                                       const uint16_t* __restrict__ dout, int64_t ldg,
-                                                       float* __restrict__ Dv,
-                                                       uint16_t* __restrict__ dqkv, int64_t lddq,
-                                                       float scale, float rroot)
+template <int DT, int HD, typename Sh, bool REG>
+__global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __restrict__ out, int64_t ldo,
+                                                      const float* __restrict__ lse,
+                                                      const uint16_t* __restrict__ dout, int64_t ldg,
+                                                      float* __restrict__ Dv, uint16_t* __restrict__ dqkv,
+                                                      int64_t lddq, float scale, float rroot)
 {
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT;
-    __shared__ __attribute__((aligned(16))) char kv[2][2][BLK * RS];
-    __shared__ __attribute__((aligned(16))) int32_t lab[2][BLK];
-    const int T = p.T, n_blk = (p.nt + NW - 1) / NW;
-    const Place at = place(p, n_blk);
+    __shared__ __attribute__((aligned(16))) char kv[4 * Sh::B * RS];
+    __shared__ __attribute__((aligned(16))) int32_t lab[2][Sh::B];
+    const int T = p.T;
+    const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
     if (!at.ok)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     const uint16_t* base = p.qkv + at.seq * T * ldq + at.h * HD;
-    const int32_t* reg = REG ? p.region + at.seq % p.n_region * T : nullptr;
-    const int qt = at.blk * NW + wave, q = qt * 32 + l32, qc = min(q, T - 1);
+    const int32_t* reg = REG ? labels(p, at.seq) : nullptr;
+    const int part = wave % Sh::KS, qt = at.blk * Sh::QW + wave / Sh::KS, q = qt * 32 + l32;
+    const int qc = min(q, T - 1);
     const bool busy = qt < p.nt;
-    int mine = 0;
-    if (REG) {
-        mine = reg[qc];
-        mine = mine < 0 ? NO_LABEL : mine;
-    }
+    const int mine = label_mine<REG>(reg, qc);
     const bool live = busy && mine != NO_LABEL;
-    F qf[KS], gf[KS], of[KS];
-    load_frags<F, HD>(qf, base + (int64_t)qc * ldq, half, live);
-    load_frags<F, HD>(gf, dout + (at.seq * T + qc) * ldg + at.h * HD, half, live);
-    load_frags<F, HD>(of, out + (at.seq * T + qc) * ldo + at.h * HD, half, live);
+    F qf[KS], gf[KS];
     float D = 0.0f;
+    {
+        F of[KS];
+        load_frags<F, HD>(gf, dout + (at.seq * T + qc) * ldg + at.h * HD, half, live);
+        load_frags<F, HD>(of, out + (at.seq * T + qc) * ldo + at.h * HD, half, live);
+        load_frags<F, HD>(qf, base + (int64_t)qc * ldq, half, live);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            D = fmaf((float)gf[ks][j], (float)of[ks][j], D);
-    D += __shfl_xor(D, 32, 64);
+            for (int j = 0; j < 8; ++j)
+                D = fmaf((float)gf[ks][j], (float)of[ks][j], D);
+        D = half_add(D);
+    }
     const int64_t stat = (at.seq * p.H + at.h) * T;
     float nl = -INFINITY;  // -lse in base 2; a row without pairs: every weight 2^-inf
     if (busy) {
         const float v = lse[stat + qc];
         nl = v == -INFINITY ? -INFINITY : -v * LOG2E;
-        if (half == 0 && q < T)
+        if (half == 0 && part == 0 && q < T)
             Dv[stat + q] = D;
     }
-    Stage<HD, 64 * NW, REG> st;
-    auto load_labels = [&](int b) {
-        int32_t v = -1;
-        const int r = b * BLK + threadIdx.x;
-        if (REG && threadIdx.x < BLK && r < T)
-            v = max(reg[r], -1);
-        return v;
-    };
-    st.load(base + hw, ldq, base + 2 * hw, ldq, 0, T, reg);
-    int32_t lv = load_labels(0);
-    const int n_kb = (T + BLK - 1) / BLK;
-    const float* bt = p.bias + (((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt) * 1024 + lane * 16;
-    f32x16 bn = load_bias(bt);
-    st.store(kv[0][0], kv[0][1]);
-    if (REG && threadIdx.x < BLK)
-        lab[0][threadIdx.x] = lv;
-    __syncthreads();
     f32x16 dq[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
         dq[d] = f32x16{};
-    for (int b = 0; b < n_kb; ++b) {
-        const int cur = b & 1;
-        if (b + 1 < n_kb) {
-            st.load(base + hw, ldq, base + 2 * hw, ldq, (b + 1) * BLK, T, reg);
-            lv = load_labels(b + 1);
-        }
-        if (busy) {
-            const uint32_t ka = lds32(kv[cur][0]) + l32 * RS + half * 16;
-            const uint32_t va = lds32(kv[cur][1]) + l32 * RS + half * 16;
-            const uint32_t kt_a = tr_base<HD>(kv[cur][0], lane);
-            for (int i = 0; i < 2; ++i) {
-                const int kt = 2 * b + i;
-                if (kt >= p.nt)
-                    break;
-                f32x16 s = bn, dp = {};
-                bn = load_bias(bt + (int64_t)min(kt + 1, p.nt - 1) * 1024);
+    int32_t lv = -1;
+    pass_blocks<HD, Sh, REG, 1>(
+        p, base + hw, ldq, base + 2 * hw, ldq, reg,
+        p.bias + ((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, kv,
+        [&](int blk) {
+            const int r = blk * Sh::B + threadIdx.x;
+            if (REG && threadIdx.x < Sh::B)
+                lv = r < T ? max(reg[r], -1) : -1;
+        },
+        [&](int b) {
+            if (REG && threadIdx.x < Sh::B)
+                lab[b][threadIdx.x] = lv;
+        },
+        [&](auto ni, int row0, const char* kb, const char* vb, int b, const f32x16* bias) {
+            constexpr int NI = decltype(ni)::value;
+            const uint32_t ka = lds32(kb) + (row0 + l32) * RS + half * 16;
+            const uint32_t va = lds32(vb) + (row0 + l32) * RS + half * 16;
+            const uint32_t kt = tr_base<HD>(kb, lane) + row0 * RS;
+            f32x16 s[NI], dp[NI];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    s = E::mma(as_frag<F>(att_read16(ka + i * 32 * RS + 32 * ks)), qf[ks], s);
+            for (int i = 0; i < NI; ++i) {
+                s[i] = bias[i];
+                dp[i] = f32x16{};
+            }
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    dp = E::mma(as_frag<F>(att_read16(va + i * 32 * RS + 32 * ks)), gf[ks], dp);
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    s[i] = E::mma(as_frag<F>(att_read16(ka + i * 32 * RS + 32 * ks)), qf[ks], s[i]);
+                    dp[i] = E::mma(as_frag<F>(att_read16(va + i * 32 * RS + 32 * ks)), gf[ks], dp[i]);
+                }
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
                 if (REG)
-                    mask_region(s, mine, lab[cur] + 32 * i, half);
+                    mask_region(s[i], mine, lab[b] + row0 + 32 * i, half);
                 uint32_t db[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * j], scale, nl));
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], scale, nl));
-                    db[j] = pack2<DT>(e0 * (dp[2 * j] - D), e1 * (dp[2 * j + 1] - D));
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j], scale, nl));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j + 1], scale, nl));
+                    db[j] = pack2<DT>(e0 * (dp[i][2 * j] - D), e1 * (dp[i][2 * j + 1] - D));
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const F df = as_frag<F>(uint4{db[4 * t], db[4 * t + 1], db[4 * t + 2], db[4 * t + 3]});
 #pragma unroll
                     for (int d = 0; d < ND; ++d)
-                        dq[d] = E::mma(tr_frag<F, HD>(kt_a, 32 * i + 16 * t, d), df, dq[d]);
+                        dq[d] = E::mma(tr_frag<F, HD>(kt, 32 * i + 16 * t, d), df, dq[d]);
                 }
             }
-        }
-        if (b + 1 < n_kb) {
-            st.store(kv[1 - cur][0], kv[1 - cur][1]);
-            if (REG && threadIdx.x < BLK)
-                lab[1 - cur][threadIdx.x] = lv;
-        }
-        __syncthreads();
+        });
+    if constexpr (Sh::KS == 2) {
+        static_assert(Sh::QW * ND * 4096 <= (int)sizeof(kv), "the joined rows fit");
+        if (!join_sums<ND>(kv, dq, wave))
+            return;
     }
     if (busy && q < T)
         store_rows<DT, HD>(dqkv + (at.seq * T + q) * lddq + at.h * HD, dq, rroot, half);
@@ -449,116 +596,103 @@ __global__ __launch_bounds__(64 * NW) void k_relpos_dq(Rp p, const uint16_t* __r
 // dK and dV: a wave holds a 32-key tile, the queries pass in blocks with their lse and D.
 // S = Q K^T and dP = dO V^T (lane = key) make P and dS the B operands of dV^T = dO^T P and
 // dK^T = Q^T dS as they stand.  The bias tiles are those of the transposed index.
-template <int DT, int HD, int NW, bool REG>
-__global__ __launch_bounds__(64 * NW) void k_relpos_dkv(Rp p, const float* __restrict__ lse,
-                                                        const float* __restrict__ Dv,
-                                                        const uint16_t* __restrict__ dout, int64_t ldg,
-                                                        uint16_t* __restrict__ dqkv, int64_t lddq,
-                                                        float scale, float rroot)
+template <int DT, int HD, typename Sh, bool REG>
+__global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __restrict__ lse,
+                                                       const float* __restrict__ Dv,
+                                                       const uint16_t* __restrict__ dout, int64_t ldg,
+                                                       uint16_t* __restrict__ dqkv, int64_t lddq,
+                                                       float scale, float rroot)
 {
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT;
-    __shared__ __attribute__((aligned(16))) char qg[2][2][BLK * RS];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][BLK];
-    __shared__ __attribute__((aligned(16))) int32_t lab[2][BLK];
-    const int T = p.T, n_blk = (p.nt + NW - 1) / NW;
-    const Place at = place(p, n_blk);
+    __shared__ __attribute__((aligned(16))) char qg[4 * Sh::B * RS];
+    __shared__ __attribute__((aligned(16))) float stats[2][2][Sh::B];
+    __shared__ __attribute__((aligned(16))) int32_t lab[2][Sh::B];
+    const int T = p.T;
+    const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
     if (!at.ok)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     const uint16_t* base = p.qkv + at.seq * T * ldq + at.h * HD;
-    const uint16_t* gbase = dout + at.seq * T * ldg + at.h * HD;
-    const int32_t* reg = REG ? p.region + at.seq % p.n_region * T : nullptr;
-    const int kt = at.blk * NW + wave, k = kt * 32 + l32, kc = min(k, T - 1);
+    const int32_t* reg = REG ? labels(p, at.seq) : nullptr;
+    const int part = wave % Sh::KS, kt = at.blk * Sh::QW + wave / Sh::KS, k = kt * 32 + l32;
+    const int kc = min(k, T - 1);
     const bool busy = kt < p.nt;
-    int mine = 0;
-    if (REG) {
-        mine = reg[kc];
-        mine = mine < 0 ? NO_LABEL : mine;
-    }
+    const int mine = label_mine<REG>(reg, kc);
     const bool live = busy && k < T && mine != NO_LABEL;
     F kf[KS], vf[KS];
     load_frags<F, HD>(kf, base + hw + (int64_t)kc * ldq, half, live);
     load_frags<F, HD>(vf, base + 2 * hw + (int64_t)kc * ldq, half, live);
     const int64_t stat = (at.seq * p.H + at.h) * T;
-    Stage<HD, 64 * NW, REG> st;
+    f32x16 acc[2 * ND];  // dK, dV
+#pragma unroll
+    for (int d = 0; d < 2 * ND; ++d)
+        acc[d] = f32x16{};
     float sl, sd;
     int32_t lv;
-    // -lse in base 2 (-inf past T and for rows without pairs: every weight 0), D and label
-    auto load_stats = [&](int b) {
-        sl = -INFINITY;
-        sd = 0.0f;
-        lv = -1;
-        const int r = b * BLK + threadIdx.x;
-        if (threadIdx.x < BLK && r < T) {
-            const float v = lse[stat + r];
-            sl = v == -INFINITY ? -INFINITY : -v * LOG2E;
-            sd = Dv[stat + r];
-            if (REG)
-                lv = max(reg[r], -1);
-        }
-    };
-    auto store_stats = [&](int buf) {
-        if (threadIdx.x < BLK) {
-            stats[buf][0][threadIdx.x] = sl;
-            stats[buf][1][threadIdx.x] = sd;
-            if (REG)
-                lab[buf][threadIdx.x] = lv;
-        }
-    };
-    st.load(base, ldq, gbase, ldg, 0, T, reg);
-    load_stats(0);
-    const int n_qb = (T + BLK - 1) / BLK;
-    const float* bt = p.bias + (((int64_t)at.h * p.nt + min(kt, p.nt - 1)) * p.nt) * 1024 + lane * 16;
-    f32x16 bn = load_bias(bt);
-    st.store(qg[0][0], qg[0][1]);
-    store_stats(0);
-    __syncthreads();
-    f32x16 dk[ND], dv[ND];
-#pragma unroll
-    for (int d = 0; d < ND; ++d) {
-        dk[d] = f32x16{};
-        dv[d] = f32x16{};
-    }
-    for (int b = 0; b < n_qb; ++b) {
-        const int cur = b & 1;
-        if (b + 1 < n_qb) {
-            st.load(base, ldq, gbase, ldg, (b + 1) * BLK, T, reg);
-            load_stats(b + 1);
-        }
-        if (busy) {
-            const uint32_t qa = lds32(qg[cur][0]) + l32 * RS + half * 16;
-            const uint32_t ga = lds32(qg[cur][1]) + l32 * RS + half * 16;
-            const uint32_t qtr = tr_base<HD>(qg[cur][0], lane), gtr = tr_base<HD>(qg[cur][1], lane);
-            for (int i = 0; i < 2; ++i) {
-                const int qt = 2 * b + i;
-                if (qt >= p.nt)
-                    break;
-                f32x16 s = bn, dp = {};
-                bn = load_bias(bt + (int64_t)min(qt + 1, p.nt - 1) * 1024);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    s = E::mma(as_frag<F>(att_read16(qa + i * 32 * RS + 32 * ks)), kf[ks], s);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks)
-                    dp = E::mma(as_frag<F>(att_read16(ga + i * 32 * RS + 32 * ks)), vf[ks], dp);
+    pass_blocks<HD, Sh, REG, 1>(
+        p, base, ldq, dout + at.seq * T * ldg + at.h * HD, ldg, reg,
+        p.bias + ((int64_t)at.h * p.nt + min(kt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, qg,
+        [&](int blk) {
+            // -lse in base 2 (-inf past T and for rows without pairs: every weight 0), D, label
+            sl = -INFINITY;
+            sd = 0.0f;
+            lv = -1;
+            const int r = blk * Sh::B + threadIdx.x;
+            if (threadIdx.x < Sh::B && r < T) {
+                const float v = lse[stat + r];
+                sl = v == -INFINITY ? -INFINITY : -v * LOG2E;
+                sd = Dv[stat + r];
                 if (REG)
-                    mask_region(s, mine, lab[cur] + 32 * i, half);
+                    lv = max(reg[r], -1);
+            }
+        },
+        [&](int b) {
+            if (threadIdx.x < Sh::B) {
+                stats[b][0][threadIdx.x] = sl;
+                stats[b][1][threadIdx.x] = sd;
+                if (REG)
+                    lab[b][threadIdx.x] = lv;
+            }
+        },
+        [&](auto ni, int row0, const char* qb, const char* gb, int b, const f32x16* bias) {
+            constexpr int NI = decltype(ni)::value;
+            const uint32_t qa = lds32(qb) + (row0 + l32) * RS + half * 16;
+            const uint32_t ga = lds32(gb) + (row0 + l32) * RS + half * 16;
+            const uint32_t qtr = tr_base<HD>(qb, lane) + row0 * RS;
+            const uint32_t gtr = tr_base<HD>(gb, lane) + row0 * RS;
+            f32x16 s[NI], dp[NI];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                s[i] = bias[i];
+                dp[i] = f32x16{};
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    s[i] = E::mma(as_frag<F>(att_read16(qa + i * 32 * RS + 32 * ks)), kf[ks], s[i]);
+                    dp[i] = E::mma(as_frag<F>(att_read16(ga + i * 32 * RS + 32 * ks)), vf[ks], dp[i]);
+                }
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                if (REG)
+                    mask_region(s[i], mine, lab[b] + row0 + 32 * i, half);
                 uint32_t pb[8], db[8];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const float4 nl = *(const float4*)(stats[cur][0] + 32 * i + 8 * g + 4 * half);
-                    const float4 D = *(const float4*)(stats[cur][1] + 32 * i + 8 * g + 4 * half);
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[4 * g], scale, nl.x));
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 1], scale, nl.y));
-                    const float e2 = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 2], scale, nl.z));
-                    const float e3 = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 3], scale, nl.w));
+                    const float4 nl = *(const float4*)(stats[b][0] + row0 + 32 * i + 8 * g + 4 * half);
+                    const float4 D = *(const float4*)(stats[b][1] + row0 + 32 * i + 8 * g + 4 * half);
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i][4 * g], scale, nl.x));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i][4 * g + 1], scale, nl.y));
+                    const float e2 = __builtin_amdgcn_exp2f(fmaf(s[i][4 * g + 2], scale, nl.z));
+                    const float e3 = __builtin_amdgcn_exp2f(fmaf(s[i][4 * g + 3], scale, nl.w));
                     pb[2 * g] = pack2<DT>(e0, e1);
                     pb[2 * g + 1] = pack2<DT>(e2, e3);
-                    db[2 * g] = pack2<DT>(e0 * (dp[4 * g] - D.x), e1 * (dp[4 * g + 1] - D.y));
-                    db[2 * g + 1] = pack2<DT>(e2 * (dp[4 * g + 2] - D.z), e3 * (dp[4 * g + 3] - D.w));
+                    db[2 * g] = pack2<DT>(e0 * (dp[i][4 * g] - D.x), e1 * (dp[i][4 * g + 1] - D.y));
+                    db[2 * g + 1] = pack2<DT>(e2 * (dp[i][4 * g + 2] - D.z), e3 * (dp[i][4 * g + 3] - D.w));
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -566,28 +700,27 @@ __global__ __launch_bounds__(64 * NW) void k_relpos_dkv(Rp p, const float* __res
                     const F df = as_frag<F>(uint4{db[4 * t], db[4 * t + 1], db[4 * t + 2], db[4 * t + 3]});
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
-                        dv[d] = E::mma(tr_frag<F, HD>(gtr, 32 * i + 16 * t, d), pf, dv[d]);
-                        dk[d] = E::mma(tr_frag<F, HD>(qtr, 32 * i + 16 * t, d), df, dk[d]);
+                        acc[d] = E::mma(tr_frag<F, HD>(qtr, 32 * i + 16 * t, d), df, acc[d]);
+                        acc[ND + d] = E::mma(tr_frag<F, HD>(gtr, 32 * i + 16 * t, d), pf, acc[ND + d]);
                     }
                 }
             }
-        }
-        if (b + 1 < n_qb) {
-            st.store(qg[1 - cur][0], qg[1 - cur][1]);
-            store_stats(1 - cur);
-        }
-        __syncthreads();
+        });
+    if constexpr (Sh::KS == 2) {
+        static_assert(Sh::QW * 2 * ND * 4096 <= (int)sizeof(qg), "the joined rows fit");
+        if (!join_sums<2 * ND>(qg, acc, wave))
+            return;
     }
     if (busy && k < T) {
         uint16_t* row = dqkv + (at.seq * T + k) * lddq + at.h * HD;
-        store_rows<DT, HD>(row + hw, dk, rroot, half);
-        store_rows<DT, HD>(row + 2 * hw, dv, 1.0f, half);
+        store_rows<DT, HD>(row + hw, acc, rroot, half);
+        store_rows<DT, HD>(row + 2 * hw, acc + ND, 1.0f, half);
     }
 }
 
 // Sum over a chunk of sequences of dS of one head's pairs, 64 x 64 pairs to a workgroup of
 // four waves (a 32 x 32 tile each, summed in its accumulators' places in float32), the four
-// matrices' rows staged in LDS a sequence ahead.  part: [head][chunk][tile][lane][16].
+// matrices' rows staged in LDS a sequence ahead.  part: [head][chunk][tile][r / 4][lane][r % 4].
 template <int DT, int HD, bool REG>
 __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restrict__ lse,
                                                       const float* __restrict__ Dv,
@@ -598,29 +731,29 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS;
-    __shared__ __attribute__((aligned(16))) char rows[4][BLK * RS];  // Q, dO, K, V
+    __shared__ __attribute__((aligned(16))) char rows[4][64 * RS];  // Q, dO, K, V
     const int T = p.T, n_blk = (p.nt + 1) / 2;
-    const int64_t id = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int64_t u = id / chunks;
-    const int chunk = (int)(id - u * chunks);
-    const int h = (int)(u / ((int64_t)n_blk * n_blk)), ab = (int)(u % ((int64_t)n_blk * n_blk));
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;  // (fewer than 2^18)
+    const uint32_t u = id / (uint32_t)chunks;
+    const int chunk = (int)(id - u * (uint32_t)chunks);
+    const int h = (int)(u / (uint32_t)(n_blk * n_blk)), ab = (int)(u - (uint32_t)h * (n_blk * n_blk));
     if (h >= p.H)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int qb = ab / n_blk, kb = ab - qb * n_blk;
     const int qt = 2 * qb + (wave >> 1), kt = 2 * kb + (wave & 1);
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     const bool busy = qt < p.nt && kt < p.nt;
     const int q = qt * 32 + l32, qc = min(q, T - 1);
     const f32x16 bias = load_bias(
-        p.bias + (((int64_t)h * p.nt + min(qt, p.nt - 1)) * p.nt + min(kt, p.nt - 1)) * 1024 + lane * 16);
+        p.bias + (((int64_t)h * p.nt + min(qt, p.nt - 1)) * p.nt + min(kt, p.nt - 1)) * 1024 + lane * 4);
     const int64_t s0 = p.n_seq * chunk / chunks, s1 = p.n_seq * (chunk + 1) / chunks;
-    Stage<HD, 256, REG> sq, sk;
+    Stage<HD, 256, 64, REG> sq, sk;
     auto load = [&](int64_t seq) {
         const uint16_t* base = p.qkv + seq * T * ldq + h * HD;
-        const int32_t* reg = REG ? p.region + seq % p.n_region * T : nullptr;
-        sq.load(base, ldq, dout + seq * T * ldg + h * HD, ldg, qb * BLK, T, reg);
-        sk.load(base + hw, ldq, base + 2 * hw, ldq, kb * BLK, T, reg);
+        const int32_t* reg = REG ? labels(p, seq) : nullptr;
+        sq.load(base, ldq, dout + seq * T * ldg + h * HD, ldg, qb * 64, T, reg);
+        sk.load(base + hw, ldq, base + 2 * hw, ldq, kb * 64, T, reg);
     };
     f32x16 sum = {};
     if (s0 < s1)
@@ -647,7 +780,7 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
                 dp = E::mma(as_frag<F>(att_read16(va + 32 * ks)), as_frag<F>(att_read16(ga + 32 * ks)), dp);
             }
             if (REG) {
-                const int32_t* reg = p.region + seq % p.n_region * T;
+                const int32_t* reg = labels(p, seq);
                 int mine = reg[qc];
                 mine = mine < 0 ? NO_LABEL : mine;
 #pragma unroll
@@ -664,33 +797,64 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
     }
     if (busy) {
         float* dst = part + (((int64_t)h * chunks + chunk) * p.nt * p.nt + (int64_t)qt * p.nt + kt) * 1024 +
-                     lane * 16;
+                     lane * 4;
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-            *(float4*)(dst + 4 * g) = float4{sum[4 * g], sum[4 * g + 1], sum[4 * g + 2], sum[4 * g + 3]};
+            *(float4*)(dst + 256 * g) = float4{sum[4 * g], sum[4 * g + 1], sum[4 * g + 2], sum[4 * g + 3]};
     }
 }
 
+// The chunks' sums of each pair: CL threads of a workgroup share a pair's chunks (each in
+// order, then the threads'), 4 pairs to a thread.
+template <int CL>
+__global__ __launch_bounds__(256) void k_relpos_fold(const float* __restrict__ part, int32_t chunks,
+                                                     int64_t n_pos, float* __restrict__ sum)
+{
+    __shared__ float4 red[256];
+    const int x = threadIdx.x % (256 / CL), c0 = threadIdx.x / (256 / CL), h = blockIdx.y;
+    const int64_t i = ((int64_t)blockIdx.x * (256 / CL) + x) * 4;  // (n_pos is a multiple of 1024)
+    const float* at = part + (int64_t)h * chunks * n_pos + i;
+    float4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = c0; c < chunks; c += CL) {
+        const float4 w = *(const float4*)(at + c * n_pos);
+        v.x += w.x;
+        v.y += w.y;
+        v.z += w.z;
+        v.w += w.w;
+    }
+    if (CL > 1) {
+        red[threadIdx.x] = v;
+        __syncthreads();
+        if (c0 > 0)
+            return;
+        for (int c = 1; c < CL; ++c) {
+            const float4 w = red[c * (256 / CL) + x];
+            v.x += w.x;
+            v.y += w.y;
+            v.z += w.z;
+            v.w += w.w;
+        }
+    }
+    *(float4*)(sum + h * n_pos + i) = v;
+}
+
 // The pairs of a bucket, in segments: order[seg_ptr[g] .. seg_ptr[g + 1]) are places in a
-// head's tiles.  A workgroup adds one segment over all chunks, each thread its pairs in
-// order, then a fixed tree; out: [segment][head] (16-bit: the table's gradient itself,
-// where every bucket is one segment).
+// head's tiles.  A workgroup adds one segment, each thread its pairs in order, then a fixed
+// tree; out: [segment][head], or the table's gradient where every bucket is one segment.
+// sum NULL: no sequences, all zero.
 template <int DT>
 __global__ __launch_bounds__(256) void k_relpos_segments(const int32_t* __restrict__ order,
                                                          const int32_t* __restrict__ seg_ptr,
-                                                         const float* __restrict__ part, int32_t chunks,
-                                                         int64_t n_pos, int32_t H, float* __restrict__ sums,
+                                                         const float* __restrict__ sum, int64_t n_pos,
+                                                         int32_t H, float* __restrict__ sums,
                                                          uint16_t* __restrict__ dtable)
 {
     __shared__ float red[4];
     const int g = blockIdx.x, h = blockIdx.y;
-    const float* base = part + (int64_t)h * chunks * n_pos;
     float v = 0.0f;
-    for (int i = seg_ptr[g] + threadIdx.x; i < seg_ptr[g + 1]; i += 256) {
-        const float* at = base + order[i];
-        for (int c = 0; c < chunks; ++c)
-            v += at[c * n_pos];
-    }
+    if (sum)
+        for (int i = seg_ptr[g] + threadIdx.x; i < seg_ptr[g + 1]; i += 256)
+            v += sum[h * n_pos + order[i]];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         v += __shfl_xor(v, o, 64);
@@ -722,20 +886,354 @@ __global__ __launch_bounds__(256) void k_relpos_buckets(const int32_t* __restric
     dtable[i] = Elem<DT>::from_f32(v);
 }
 
+// ---------------------------------------------------------------- up to 64 tokens
+
+// Windows of at most 64 tokens: everything of a window and head fits a wave's (forward) or a
+// small workgroup's (gradients) registers and LDS, so a workgroup stays with one head, whose
+// bias its registers hold as the accumulators' start, and takes one window after the other,
+// the next one's rows in flight.  Bound: HBM.
+
+// Forward: a wave to a window, four windows to a workgroup.  Q is read as the operand that it
+// is, K and V pass through the wave's LDS rows.
+template <int DT, int HD, int NT, bool REG>
+__global__ __launch_bounds__(256, HD == 32 ? 2 : 1) void k_relpos_window_fwd(
+    Rp p, const uint16_t* __restrict__ idx, const uint16_t* __restrict__ table, uint16_t* __restrict__ out,
+    int64_t ldo, float* __restrict__ lse, float scale, float root)
+{
+    using E = Elem<DT>;
+    using F = typename E::frag;
+    constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT, CH = HD / 8;
+    constexpr int RPC = 64 / CH, NC = 32 * NT / RPC;  // rows to a chunk of 64 lanes, chunks
+    __shared__ __attribute__((aligned(16))) char rows[4][2][32 * NT * RS];
+    __shared__ __attribute__((aligned(16))) int32_t labs[4][64];
+    __shared__ float4 tiles[NT * NT * 4 * 64];
+    const int T = p.T, lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
+    const int h = blockIdx.x % p.H;
+    const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD, step = (int64_t)(gridDim.x / p.H) * 4;
+    int64_t n = (int64_t)(blockIdx.x / p.H) * 4 + wave;
+    // the next window: Q fragments, K and V chunks (row lane / CH of each RPC), its label
+    F qn[NT][KS];
+    uint4 kn[NC], vn[NC];
+    int labn = 0;
+    auto load = [&](int64_t seq) {
+        const uint16_t* base = p.qkv + seq * T * ldq + h * HD;
+        if (REG)
+            labn = lane < T ? max(labels(p, seq)[lane], -1) : -1;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int r = i * RPC + lane / CH;
+            kn[i] = vn[i] = uint4{0u, 0u, 0u, 0u};
+            if (r < T) {
+                const uint16_t* at = base + (int64_t)r * ldq + 8 * (lane % CH);
+                kn[i] = *(const uint4*)(at + hw);
+                vn[i] = *(const uint4*)(at + 2 * hw);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            load_frags<F, HD>(qn[t], base + (int64_t)min(32 * t + l32, T - 1) * ldq, half, true);
+    };
+    if (n < p.n_seq)
+        load(n);
+    for (int i = wave; i < NT * NT * 4; i += 4)
+        tiles[i * 64 + lane] = gather_bias<DT>(idx, NT, i / 4 / NT, i / 4 % NT, i % 4, lane, table, p.H, h, root);
+    __syncthreads();
+    f32x16 bias[NT][NT];
+#pragma unroll
+    for (int a = 0; a < NT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+            bias[a][b] = load_bias((const float*)(tiles + (a * NT + b) * 256 + lane));
+    char* kb = rows[wave][0];
+    char* vb = rows[wave][1];
+    const uint32_t ka = lds32(kb) + l32 * RS + half * 16, va = tr_base<HD>(vb, lane);
+    for (; n < p.n_seq; n += step) {
+        F qf[NT][KS];
+        const int lab = labn;
+        bool cut = false;  // the window has more than one label, or padding
+        if (REG) {
+            labs[wave][lane] = lab;
+            cut = !__all(lane >= T || (lab == __builtin_amdgcn_readfirstlane(lab) && lab >= 0));
+        }
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int r = i * RPC + lane / CH;
+            if (REG && cut && __shfl(lab, r, 64) < 0)  // (padding may hold anything)
+                vn[i] = uint4{0u, 0u, 0u, 0u};
+            *(uint4*)(kb + r * RS + 16 * (lane % CH)) = kn[i];
+            *(uint4*)(vb + r * RS + 16 * (lane % CH)) = vn[i];
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                qf[t][ks] = qn[t][ks];
+        if (n + step < p.n_seq)
+            load(n + step);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a wave's LDS accesses run in order)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            f32x16 s[NT], o[ND];
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+                s[i] = bias[t][i];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+                    s[i] = E::mma(as_frag<F>(att_read16(ka + i * 32 * RS + 32 * ks)), qf[t][ks], s[i]);
+            if (REG && cut) {
+                const int mine = __shfl(lab, 32 * t + l32, 64);
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+                    mask_region(s[i], mine < 0 ? NO_LABEL : mine, labs[wave] + 32 * i, half);
+            }
+            float m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    m = fmaxf(m, fmaxf(fmaxf(s[i][j], s[i][j + 4]), fmaxf(s[i][j + 8], s[i][j + 12])));
+            m = half_max(m);
+            const float nms = m == -INFINITY ? 0.0f : -m * scale;
+            float ps[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                o[d] = f32x16{};
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                uint32_t pb[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j], scale, nms));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j + 1], scale, nms));
+                    ps[0] += e0;
+                    ps[1] += e1;
+                    pb[j] = pack2<DT>(e0, e1);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const F pf = as_frag<F>(uint4{pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]});
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+                        o[d] = E::mma(tr_frag<F, HD>(va, 32 * i + 16 * u, d), pf, o[d]);
+                }
+            }
+            const float l = half_add(ps[0] + ps[1]);
+            const int q = 32 * t + l32;
+            if (q < T) {
+                store_rows<DT, HD>(out + (n * T + q) * ldo + h * HD, o, l > 0.0f ? 1.0f / l : 0.0f, half);
+                if (lse && half == 0)
+                    lse[(n * p.H + h) * T + q] = l > 0.0f ? LN2 * (m * scale + __log2f(l)) : -INFINITY;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// Gradients: a workgroup of NT waves to a window, all four matrices' rows in LDS.  First a
+// wave holds a 32-query tile (lane = query): S^T, dP^T, D from the weights themselves, dS^T,
+// which its registers add up over the windows for the bias's gradient, and dQ^T = K^T dS^T.
+// P and dS, rounded once, cross to the other operand order through LDS; then a wave holds a
+// 32-key tile: dV^T = dO^T P, dK^T = Q^T dS.
+template <int DT, int HD, int NT, bool REG>
+__global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_grad(
+    Rp p, const uint16_t* __restrict__ idx, const uint16_t* __restrict__ table,
+    const float* __restrict__ lse, const uint16_t* __restrict__ dout, int64_t ldg,
+    uint16_t* __restrict__ dqkv, int64_t lddq, float* __restrict__ part, float scale, float root, float rroot)
+{
+    using E = Elem<DT>;
+    using F = typename E::frag;
+    constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT, CH = HD / 8;
+    constexpr int N = 32 * CH / 64;  // chunks of each matrix to a thread
+    constexpr int PS = 64 * NT + 16;  // bytes of a row of P and dS
+    __shared__ __attribute__((aligned(16))) char rows[4][32 * NT * RS];  // Q, K, V, dO
+    __shared__ __attribute__((aligned(16))) char cross[2][32 * NT * PS];
+    __shared__ __attribute__((aligned(16))) int32_t labs[32 * NT];
+    const int T = p.T, tid = threadIdx.x, lane = tid & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
+    const int h = blockIdx.x % p.H, chunk = blockIdx.x / p.H, chunks = gridDim.x / p.H;
+    const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
+    uint4 next[4][N];
+    float lsen = 0.0f;
+    int labn = 0;
+    const int q = 32 * wave + l32;
+    auto load = [&](int64_t seq) {
+        const uint16_t* base = p.qkv + seq * T * ldq + h * HD;
+        const uint16_t* g = dout + seq * T * ldg + h * HD;
+        const int32_t* reg = REG ? labels(p, seq) : nullptr;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = tid + i * 64 * NT, r = c / CH, k = 8 * (c % CH);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                next[j][i] = uint4{0u, 0u, 0u, 0u};
+            if (r < T && (!REG || reg[r] >= 0)) {  // (padding may hold anything)
+                const uint16_t* at = base + (int64_t)r * ldq + k;
+                next[0][i] = *(const uint4*)at;
+                next[1][i] = *(const uint4*)(at + hw);
+                next[2][i] = *(const uint4*)(at + 2 * hw);
+                next[3][i] = *(const uint4*)(g + (int64_t)r * ldg + k);
+            }
+        }
+        lsen = q < T ? lse[(seq * p.H + h) * T + q] : -INFINITY;
+        if (REG)
+            labn = q < T ? max(reg[q], -1) : -1;
+    };
+    int64_t n = chunk;
+    if (n < p.n_seq)
+        load(n);
+    f32x16 bias[NT], sum[NT];
+#pragma unroll
+    for (int b = 0; b < NT; ++b) {
+        sum[b] = f32x16{};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float4 v = gather_bias<DT>(idx, NT, wave, b, g, lane, table, p.H, h, root);
+            bias[b][4 * g] = v.x;
+            bias[b][4 * g + 1] = v.y;
+            bias[b][4 * g + 2] = v.z;
+            bias[b][4 * g + 3] = v.w;
+        }
+    }
+    const uint32_t qa = lds32(rows[0]) + q * RS + half * 16, ga = lds32(rows[3]) + q * RS + half * 16;
+    const uint32_t ka = lds32(rows[1]) + l32 * RS + half * 16, va = lds32(rows[2]) + l32 * RS + half * 16;
+    const uint32_t qtr = tr_base<HD>(rows[0], lane), ktr = tr_base<HD>(rows[1], lane),
+                   gtr = tr_base<HD>(rows[3], lane);
+    // this lane's transposing read of P and dS: rows are queries, columns this wave's keys
+    const int g16 = lane >> 4, j16 = lane & 15;
+    const uint32_t ptr = lds32(cross[0]) + ((j16 >> 2) + 4 * (g16 >> 1)) * PS +
+                         (32 * wave + 16 * (g16 & 1) + 4 * (j16 & 3)) * 2;
+    auto cross_frag = [&](uint32_t base, int row) {
+        const uint32_t at = base + row * PS;
+        const uint2 lo = att_tr_read(at), hi = att_tr_read(at + 8 * PS);
+        return as_frag<F>(uint4{lo.x, lo.y, hi.x, hi.y});
+    };
+    for (; n < p.n_seq; n += chunks) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = tid + i * 64 * NT;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *(uint4*)(rows[j] + c / CH * RS + 16 * (c % CH)) = next[j][i];
+        }
+        const float nl = lsen == -INFINITY ? -INFINITY : -lsen * LOG2E;
+        const int mine = labn < 0 ? NO_LABEL : labn;
+        if (REG && half == 0)
+            labs[q] = labn;
+        __syncthreads();
+        if (n + chunks < p.n_seq)
+            load(n + chunks);
+        F qf[KS], gf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qf[ks] = as_frag<F>(att_read16(qa + 32 * ks));
+            gf[ks] = as_frag<F>(att_read16(ga + 32 * ks));
+        }
+        f32x16 s[NT], dp[NT];
+        float D = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            s[b] = bias[b];
+            dp[b] = f32x16{};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                s[b] = E::mma(as_frag<F>(att_read16(ka + b * 32 * RS + 32 * ks)), qf[ks], s[b]);
+                dp[b] = E::mma(as_frag<F>(att_read16(va + b * 32 * RS + 32 * ks)), gf[ks], dp[b]);
+            }
+            if (REG)
+                mask_region(s[b], mine, labs + 32 * b, half);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], scale, nl));
+                D = fmaf(s[b][r], dp[b][r], D);
+            }
+        }
+        D = half_add(D);
+        f32x16 dq[ND];
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+            dq[d] = f32x16{};
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            uint32_t db[8];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float e[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    e[j] = s[b][4 * g + j] * (dp[b][4 * g + j] - D);
+                    sum[b][4 * g + j] += e[j];
+                }
+                db[2 * g] = pack2<DT>(e[0], e[1]);
+                db[2 * g + 1] = pack2<DT>(e[2], e[3]);
+                const int at = q * PS + (32 * b + 8 * g + 4 * half) * 2;
+                *(uint2*)(cross[0] + at) = uint2{pack2<DT>(s[b][4 * g], s[b][4 * g + 1]),
+                                                 pack2<DT>(s[b][4 * g + 2], s[b][4 * g + 3])};
+                *(uint2*)(cross[1] + at) = uint2{db[2 * g], db[2 * g + 1]};
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const F df = as_frag<F>(uint4{db[4 * u], db[4 * u + 1], db[4 * u + 2], db[4 * u + 3]});
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    dq[d] = E::mma(tr_frag<F, HD>(ktr, 32 * b + 16 * u, d), df, dq[d]);
+            }
+        }
+        uint16_t* row = dqkv + (n * T + q) * lddq + h * HD;
+        if (q < T)
+            store_rows<DT, HD>(row, dq, rroot, half);
+        __syncthreads();
+        f32x16 dk[ND], dv[ND];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            dk[d] = f32x16{};
+            dv[d] = f32x16{};
+        }
+#pragma unroll
+        for (int u = 0; u < 2 * NT; ++u) {
+            const F pf = cross_frag(ptr, 16 * u), df = cross_frag(ptr + 32 * NT * PS, 16 * u);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                dv[d] = E::mma(tr_frag<F, HD>(gtr, 16 * u, d), pf, dv[d]);
+                dk[d] = E::mma(tr_frag<F, HD>(qtr, 16 * u, d), df, dk[d]);
+            }
+        }
+        if (q < T) {
+            store_rows<DT, HD>(row + hw, dk, rroot, half);
+            store_rows<DT, HD>(row + 2 * hw, dv, 1.0f, half);
+        }
+        __syncthreads();
+    }
+    float* dst = part + (((int64_t)h * chunks + chunk) * NT + wave) * NT * 1024 + lane * 4;
+#pragma unroll
+    for (int b = 0; b < NT; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *(float4*)(dst + b * 1024 + 256 * g) =
+                float4{sum[b][4 * g], sum[b][4 * g + 1], sum[b][4 * g + 2], sum[b][4 * g + 3]};
+}
+
 int64_t tile_floats(const lpv_relpos* h) { return (int64_t)h->nt * h->nt * 1024; }
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
+constexpr int WINDOW_TILES = 2;  // tiles of 32 tokens that the window kernels take
+bool is_window(const lpv_relpos* h) { return h->nt <= WINDOW_TILES; }
+
 // Chunks of sequences of the bias gradient: 1024 workgroups, four to a compute unit.
 int bias_chunks(const lpv_relpos* h, int64_t n_seq, int32_t H)
 {
+    if (is_window(h)) {
+        const int64_t c = (1024 + H - 1) / H;
+        return (int)(c < n_seq ? c : n_seq);
+    }
     const int64_t n_blk = (h->nt + 1) / 2, wgs = (int64_t)H * n_blk * n_blk;
     const int64_t c = (1024 + wgs - 1) / wgs;
     return (int)(c < n_seq ? c : n_seq);
 }
 
 struct Ws {  // places in a gradient's workspace
-    float *bias, *bias_t, *D, *part, *sums;
+    float *bias, *bias_t, *D, *part, *sum, *sums;
     size_t bytes;
 };
 Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
@@ -747,10 +1245,12 @@ Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
         return p;
     };
     Ws w;
-    w.bias = take((size_t)(H * tile_floats(h)));
-    w.bias_t = take((size_t)(H * tile_floats(h)));
-    w.D = take((size_t)(n_seq * H * h->T));
+    const bool window = is_window(h);
+    w.bias = take(window ? 0 : (size_t)(H * tile_floats(h)));
+    w.bias_t = take(window ? 0 : (size_t)(H * tile_floats(h)));
+    w.D = take(window ? 0 : (size_t)(n_seq * H * h->T));
     w.part = take((size_t)(H * bias_chunks(h, n_seq, H) * tile_floats(h)));
+    w.sum = bias_chunks(h, n_seq, H) > 1 ? take((size_t)(H * tile_floats(h))) : w.part;
     w.sums = take((size_t)((int64_t)h->n_segs * H));
     w.bytes = at;
     return w;
@@ -767,19 +1267,67 @@ hipError_t expand_bias(const lpv_relpos* h, bool transposed, const void* table, 
     return hipGetLastError();
 }
 
-constexpr int NW = 4;
+// The general kernels' layout: a wave to a 32-row tile, four tiles to a workgroup; where
+// that leaves the chip with fewer than two waves to a SIMD, two waves to a tile.
+template <int DT, int HD, bool REG, typename Sh>
+hipError_t forward_tiles(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
+{
+    const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt,
+                  (const float*)c.ws};
+    const Grid2 g = grid_of(c.n_seq * c.H * ((h->nt + Sh::QW - 1) / Sh::QW));
+    hipLaunchKernelGGL((k_relpos_fwd<DT, HD, Sh, REG>), dim3(g.x, g.y), dim3(Sh::NT), 0, s, p,
+                       (uint16_t*)c.out, c.ldo, c.lse, LOG2E / sqrtf((float)HD));
+    return hipGetLastError();
+}
+
+bool few_tiles(const lpv_relpos* h, const RelposCall& c) { return c.n_seq * c.H * h->nt < 2048; }
+
+// Workgroups of four windows: at most two (32 dimensions) or one to a compute unit at once.
+template <int DT, int HD, bool REG, int NT>
+hipError_t forward_windows(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
+{
+    const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, nullptr};
+    const int64_t most = ((HD == 32 ? 512 : 256) + c.H - 1) / c.H, need = (c.n_seq + 3) / 4;
+    hipLaunchKernelGGL((k_relpos_window_fwd<DT, HD, NT, REG>), dim3((uint32_t)(need < most ? need : most) * c.H),
+                       dim3(256), 0, s, p, h->idx, (const uint16_t*)c.table, (uint16_t*)c.out, c.ldo, c.lse,
+                       LOG2E / sqrtf((float)HD), sqrtf((float)HD));
+    return hipGetLastError();
+}
+
+template <int DT, int HD, bool REG, int NT>
+hipError_t grad_windows(const lpv_relpos* h, const RelposCall& c, const Ws& w, int chunks, hipStream_t s)
+{
+    const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, nullptr};
+    hipLaunchKernelGGL((k_relpos_window_grad<DT, HD, NT, REG>), dim3((uint32_t)chunks * c.H), dim3(64 * NT), 0, s,
+                       p, h->idx, (const uint16_t*)c.table, c.lse, (const uint16_t*)c.dout, c.ldg,
+                       (uint16_t*)c.dqkv, c.lddq, w.part, LOG2E / sqrtf((float)HD), sqrtf((float)HD),
+                       1.0f / sqrtf((float)HD));
+    return hipGetLastError();
+}
 
 template <int DT, int HD, bool REG> hipError_t forward_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
 {
-    hipError_t e = expand_bias<DT>(h, false, c.table, c.H, HD, (float*)c.ws, s);
+    if (is_window(h))
+        return h->nt == 1 ? forward_windows<DT, HD, REG, 1>(h, c, s) : forward_windows<DT, HD, REG, 2>(h, c, s);
+    const hipError_t e = expand_bias<DT>(h, false, c.table, c.H, HD, (float*)c.ws, s);
     if (e != hipSuccess)
         return e;
-    const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt,
-                  (const float*)c.ws};
-    const int64_t wgs = c.n_seq * c.H * ((h->nt + NW - 1) / NW);
-    const Grid2 g = grid_of(wgs);
-    hipLaunchKernelGGL((k_relpos_fwd<DT, HD, NW, REG>), dim3(g.x, g.y), dim3(64 * NW), 0, s, p,
-                       (uint16_t*)c.out, c.ldo, c.lse, LOG2E / sqrtf((float)HD));
+    return few_tiles(h, c) ? forward_tiles<DT, HD, REG, Shape<2, 2>>(h, c, s)
+                           : forward_tiles<DT, HD, REG, Shape<4, 1>>(h, c, s);
+}
+
+template <int DT, int HD, bool REG, typename Sh>
+hipError_t grad_tiles(const lpv_relpos* h, const RelposCall& c, const Ws& w, hipStream_t s)
+{
+    const float scale = LOG2E / sqrtf((float)HD), rroot = 1.0f / sqrtf((float)HD);
+    Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
+    const Grid2 g = grid_of(c.n_seq * c.H * ((h->nt + Sh::QW - 1) / Sh::QW));
+    hipLaunchKernelGGL((k_relpos_dq<DT, HD, Sh, REG>), dim3(g.x, g.y), dim3(Sh::NT), 0, s, p,
+                       (const uint16_t*)c.out, c.ldo, c.lse, (const uint16_t*)c.dout, c.ldg, w.D,
+                       (uint16_t*)c.dqkv, c.lddq, scale, rroot);
+    p.bias = w.bias_t;
+    hipLaunchKernelGGL((k_relpos_dkv<DT, HD, Sh, REG>), dim3(g.x, g.y), dim3(Sh::NT), 0, s, p, c.lse, w.D,
+                       (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, scale, rroot);
     return hipGetLastError();
 }
 
@@ -788,30 +1336,35 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
 {
     const Ws w = grad_ws(h, c.n_seq, c.H, c.ws);
     const int chunks = bias_chunks(h, c.n_seq, c.H);
-    if (chunks > 0) {  // (n_seq > 0)
-        const float scale = LOG2E / sqrtf((float)HD), rroot = 1.0f / sqrtf((float)HD);
-        hipError_t e = expand_bias<DT>(h, false, c.table, c.H, HD, w.bias, s);
+    const int64_t n_pos = tile_floats(h);
+    hipError_t e = hipSuccess;
+    if (chunks > 0 && is_window(h)) {
+        e = h->nt == 1 ? grad_windows<DT, HD, REG, 1>(h, c, w, chunks, s)
+                       : grad_windows<DT, HD, REG, 2>(h, c, w, chunks, s);
+    } else if (chunks > 0) {  // (n_seq > 0)
+        e = expand_bias<DT>(h, false, c.table, c.H, HD, w.bias, s);
         if (e == hipSuccess)
             e = expand_bias<DT>(h, true, c.table, c.H, HD, w.bias_t, s);
-        if (e != hipSuccess)
-            return e;
-        Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
-        const Grid2 g = grid_of(c.n_seq * c.H * ((h->nt + NW - 1) / NW));
-        hipLaunchKernelGGL((k_relpos_dq<DT, HD, NW, REG>), dim3(g.x, g.y), dim3(64 * NW), 0, s, p,
-                           (const uint16_t*)c.out, c.ldo, c.lse, (const uint16_t*)c.dout, c.ldg, w.D,
-                           (uint16_t*)c.dqkv, c.lddq, scale, rroot);
-        p.bias = w.bias_t;
-        hipLaunchKernelGGL((k_relpos_dkv<DT, HD, NW, REG>), dim3(g.x, g.y), dim3(64 * NW), 0, s, p, c.lse, w.D,
-                           (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, scale, rroot);
-        p.bias = w.bias;
+        if (e == hipSuccess)
+            e = few_tiles(h, c) ? grad_tiles<DT, HD, REG, Shape<2, 2>>(h, c, w, s)
+                                : grad_tiles<DT, HD, REG, Shape<4, 1>>(h, c, w, s);
+        const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
         const int64_t n_blk = (h->nt + 1) / 2;
         const Grid2 gb = grid_of((int64_t)c.H * n_blk * n_blk * chunks);
         hipLaunchKernelGGL((k_relpos_dbias<DT, HD, REG>), dim3(gb.x, gb.y), dim3(256), 0, s, p, c.lse, w.D,
-                           (const uint16_t*)c.dout, c.ldg, w.part, chunks, scale);
+                           (const uint16_t*)c.dout, c.ldg, w.part, chunks, LOG2E / sqrtf((float)HD));
     }
+    if (e != hipSuccess)
+        return e;
+    if (chunks >= 16)
+        hipLaunchKernelGGL((k_relpos_fold<16>), dim3((uint32_t)(n_pos / 64), c.H), dim3(256), 0, s, w.part,
+                           chunks, n_pos, w.sum);
+    else if (chunks > 1)
+        hipLaunchKernelGGL((k_relpos_fold<1>), dim3((uint32_t)(n_pos / 1024), c.H), dim3(256), 0, s,
+                           w.part, chunks, n_pos, w.sum);
     const bool whole = h->n_segs == h->n_buckets;
     hipLaunchKernelGGL((k_relpos_segments<DT>), dim3(h->n_segs, c.H), dim3(256), 0, s, h->order, h->seg_ptr,
-                       w.part, chunks, tile_floats(h), c.H, w.sums, whole ? (uint16_t*)c.dtable : nullptr);
+                       chunks > 0 ? w.sum : nullptr, n_pos, c.H, w.sums, whole ? (uint16_t*)c.dtable : nullptr);
     if (!whole)
         hipLaunchKernelGGL((k_relpos_buckets<DT>),
                            dim3((uint32_t)(((int64_t)h->n_buckets * c.H + 255) / 256)), dim3(256), 0, s,
@@ -825,7 +1378,7 @@ size_t relpos_workspace_bytes(const lpv_relpos* h, int64_t n_seq, int32_t H, boo
 {
     if (grad)
         return grad_ws(h, n_seq, H, nullptr).bytes;
-    return up256((size_t)(H * tile_floats(h)) * sizeof(float));
+    return is_window(h) ? 0 : up256((size_t)(H * tile_floats(h)) * sizeof(float));
 }
 
 RelposSizes relpos_sizes(const int32_t* index, int32_t T, int32_t n_buckets, int32_t* count)
@@ -874,8 +1427,8 @@ void relpos_tables(const int32_t* index, int32_t T, int32_t n_buckets, int32_t n
             idx[i * Tp + j] = (uint16_t)b;
             idx_t[j * Tp + i] = (uint16_t)b;
             // the pair's place in a head's tiles: row i % 32 in the lanes
-            const int32_t c = j % 32, lane = i % 32 + 32 * (c / 4 % 2), r = 4 * (c / 8) + c % 4;
-            order[count[b]++] = ((i / 32) * nt + j / 32) * 1024 + lane * 16 + r;
+            const int32_t c = j % 32, lane = i % 32 + 32 * (c / 4 % 2);
+            order[count[b]++] = ((i / 32) * nt + j / 32) * 1024 + c / 8 * 256 + lane * 4 + c % 4;
         }
 }
 
