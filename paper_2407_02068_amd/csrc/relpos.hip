@@ -893,6 +893,34 @@ __global__ __launch_bounds__(256) void k_relpos_buckets(const int32_t* __restric
 // bias its registers hold as the accumulators' start, and takes one window after the other,
 // the next one's rows in flight.  Bound: HBM.
 
+// Workgroup -> head and run of windows.  Workgroups L and L + 8 share an XCD: the heads of a
+// run of windows are 8 apart, so that the lines that rows of two heads share are fetched and
+// written back once.
+struct WindowPlace {
+    int h, chunk, of;
+};
+__device__ inline WindowPlace window_place(int H)
+{
+    const uint32_t j = blockIdx.x / 8, of = gridDim.x / (uint32_t)H, c = j / (uint32_t)H;
+    if (of < 8)
+        return {(int)(blockIdx.x % (uint32_t)H), (int)(blockIdx.x / (uint32_t)H), (int)of};
+    return {(int)(j - c * (uint32_t)H), (int)(8 * c + blockIdx.x % 8), (int)of};
+}
+
+// Runs of windows (a multiple of 8, or fewer) for a launch of at most `most` workgroups of `each`
+// windows at a time: no more passes than needed, and in them as few as do.
+int window_runs(int64_t n_seq, int32_t H, int64_t most, int each)
+{
+    const int64_t need = (n_seq + each - 1) / each;
+    if (need < 8)
+        return (int)need;
+    int64_t runs = most / H / 8 * 8;
+    if (runs < 8)
+        runs = 8;
+    const int64_t its = (n_seq + runs * each - 1) / (runs * each);
+    return (int)((n_seq + its * each * 8 - 1) / (its * each * 8) * 8);
+}
+
 // Forward: a wave to a window, four windows to a workgroup.  Q is read as the operand that it
 // is, K and V pass through the wave's LDS rows.
 template <int DT, int HD, int NT, bool REG>
@@ -908,9 +936,10 @@ __global__ __launch_bounds__(256, HD == 32 ? 2 : 1) void k_relpos_window_fwd(
     __shared__ __attribute__((aligned(16))) int32_t labs[4][64];
     __shared__ float4 tiles[NT * NT * 4 * 64];
     const int T = p.T, lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
-    const int h = blockIdx.x % p.H;
-    const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD, step = (int64_t)(gridDim.x / p.H) * 4;
-    int64_t n = (int64_t)(blockIdx.x / p.H) * 4 + wave;
+    const WindowPlace at = window_place(p.H);
+    const int h = at.h;
+    const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD, step = (int64_t)at.of * 4;
+    int64_t n = (int64_t)at.chunk * 4 + wave;
     // the next window: Q fragments, K and V chunks (row lane / CH of each RPC), its label
     F qn[NT][KS];
     uint4 kn[NC], vn[NC];
@@ -1051,7 +1080,8 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
     __shared__ __attribute__((aligned(16))) char cross[2][32 * NT * PS];
     __shared__ __attribute__((aligned(16))) int32_t labs[32 * NT];
     const int T = p.T, tid = threadIdx.x, lane = tid & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
-    const int h = blockIdx.x % p.H, chunk = blockIdx.x / p.H, chunks = gridDim.x / p.H;
+    const WindowPlace at = window_place(p.H);
+    const int h = at.h, chunk = at.chunk, chunks = at.of;
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     uint4 next[4][N];
     float lsen = 0.0f;
@@ -1224,8 +1254,8 @@ bool is_window(const lpv_relpos* h) { return h->nt <= WINDOW_TILES; }
 int bias_chunks(const lpv_relpos* h, int64_t n_seq, int32_t H)
 {
     if (is_window(h)) {
-        const int64_t c = (1024 + H - 1) / H;
-        return (int)(c < n_seq ? c : n_seq);
+        // 4 workgroups to a compute unit, or more where there are more heads
+        return window_runs(n_seq, H, 1024, 1);
     }
     const int64_t n_blk = (h->nt + 1) / 2, wgs = (int64_t)H * n_blk * n_blk;
     const int64_t c = (1024 + wgs - 1) / wgs;
@@ -1287,8 +1317,8 @@ template <int DT, int HD, bool REG, int NT>
 hipError_t forward_windows(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
 {
     const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, nullptr};
-    const int64_t most = ((HD == 32 ? 512 : 256) + c.H - 1) / c.H, need = (c.n_seq + 3) / 4;
-    hipLaunchKernelGGL((k_relpos_window_fwd<DT, HD, NT, REG>), dim3((uint32_t)(need < most ? need : most) * c.H),
+    const int runs = window_runs(c.n_seq, c.H, HD == 32 ? 512 : 256, 4);
+    hipLaunchKernelGGL((k_relpos_window_fwd<DT, HD, NT, REG>), dim3((uint32_t)runs * c.H),
                        dim3(256), 0, s, p, h->idx, (const uint16_t*)c.table, (uint16_t*)c.out, c.ldo, c.lse,
                        LOG2E / sqrtf((float)HD), sqrtf((float)HD));
     return hipGetLastError();

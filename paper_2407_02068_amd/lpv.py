@@ -125,7 +125,7 @@ def _check(status, where):
 
 def _stream(stream):
     if stream is None:
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
     return ctypes.c_void_p(int(stream))
@@ -461,22 +461,22 @@ def _on_current(*tensors):
     """Every tensor's device is the current one (the library works on that)."""
     dev = torch.cuda.current_device()
     for name, t in tensors:
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise ValueError("%s must be a tensor on the GPU" % name)
-        if t.device.index != dev:
-            raise ValueError("%s lives on device %d, current device is %d" % (name, t.device.index, dev))
+        if t is not None and t.get_device() != dev:
+            if not t.is_cuda:
+                raise ValueError("%s must live on the GPU" % name)
+            raise ValueError("%s lives on device %d, current device is %d" % (name, t.get_device(), dev))
 
 
 def _rows(t, name, M, cols, dtype):
-    """(pointer, row stride) of an M x cols matrix of ``dtype``."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or tuple(t.shape) != (M, cols) \
-            or t.dtype != dtype:
+    """(address, row stride) of an M x cols matrix of ``dtype``."""
+    if not isinstance(t, torch.Tensor) or t.shape != (M, cols) or t.dtype != dtype:
         raise ValueError("%s must be a %d x %d tensor of %s" % (name, M, cols, dtype))
     if M == 0:  # (an empty tensor's strides say nothing)
         return None, cols
-    return _mat(t, name)
+    ld, unit = t.stride()
+    if cols > 1 and unit != 1:
+        raise ValueError("%s must have unit stride along its columns" % name)
+    return t.data_ptr(), ld if M > 1 else max(ld, cols)
 
 
 class RelPos:
@@ -485,6 +485,7 @@ class RelPos:
     def __init__(self, handle, T, n_buckets, device):
         self._h = ctypes.c_void_p(handle)
         self.T, self.n_buckets, self.device = T, n_buckets, device
+        self._sizes = {}  # workspace bytes by (sequences, heads, gradient)
 
     @property
     def handle(self):
@@ -524,8 +525,18 @@ def relpos_workspace_size(rp, n_seq, H, grad=False):
     return nbytes.value
 
 
+def _relpos_workspace(rp, n_seq, H, grad, workspace, device, stream):
+    key = (n_seq, H, grad)
+    nbytes = rp._sizes.get(key)
+    if nbytes is None:
+        if len(rp._sizes) >= 64:
+            rp._sizes.clear()
+        nbytes = rp._sizes[key] = relpos_workspace_size(rp, n_seq, H, grad)
+    return _workspace(workspace, nbytes, device, stream)
+
+
 def _workspace(workspace, nbytes, device, stream):
-    """(pointer, bytes, tensor) of the caller's workspace, or of one from torch's
+    """(address, bytes, tensor) of the caller's workspace, or of one from torch's
     allocator (on the current stream only: that is what its reuse is ordered by)."""
     if workspace is None:
         if nbytes == 0:
@@ -536,32 +547,29 @@ def _workspace(workspace, nbytes, device, stream):
     elif not isinstance(workspace, torch.Tensor) or not workspace.is_cuda \
             or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor")
-    return (ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size(),
-            workspace)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def _relpos_args(rp, table, qkv, n_seq, H, hd, region):
     """The leading arguments that both position-biased attention calls share."""
     if not isinstance(table, torch.Tensor) or table.dtype not in DTYPES \
-            or tuple(table.shape) != (rp.n_buckets, H) or not table.is_contiguous():
+            or table.shape != (rp.n_buckets, H) or not table.is_contiguous():
         raise ValueError("table must be a contiguous %d x %d tensor" % (rp.n_buckets, H))
     qp, ldq = _rows(qkv, "qkv", n_seq * rp.T, 3 * H * hd, table.dtype)
-    n_region = 0
-    if region is not None:
-        if not isinstance(region, torch.Tensor) or region.dim() != 2 or region.shape[1] != rp.T \
-                or region.dtype != torch.int32 or not region.is_contiguous():
-            raise ValueError("region must be a contiguous n x %d int32 tensor" % rp.T)
-        n_region = region.shape[0]
-    return (rp.handle, ctypes.c_void_p(table.data_ptr()), qp, ldq, n_seq, H, hd,
-            DTYPES[table.dtype], ctypes.c_void_p(region.data_ptr() if region is not None else 0),
-            n_region)
+    if region is None:
+        return (rp.handle, table.data_ptr(), qp, ldq, n_seq, H, hd, DTYPES[table.dtype], None, 0)
+    if not isinstance(region, torch.Tensor) or region.dim() != 2 or region.shape[1] != rp.T \
+            or region.dtype != torch.int32 or not region.is_contiguous():
+        raise ValueError("region must be a contiguous n x %d int32 tensor" % rp.T)
+    return (rp.handle, table.data_ptr(), qp, ldq, n_seq, H, hd, DTYPES[table.dtype],
+            region.data_ptr(), region.shape[0])
 
 
 def _lse(lse, n_seq, H, T):
     if not isinstance(lse, torch.Tensor) or lse.dtype != torch.float32 \
             or lse.numel() != n_seq * H * T or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 tensor of n_seq x H x T elements")
-    return ctypes.c_void_p(lse.data_ptr())
+    return lse.data_ptr()
 
 
 def relpos_attention(rp, table, qkv, n_seq, H, region=None, out=None, lse=None, workspace=None,
@@ -577,7 +585,7 @@ def relpos_attention(rp, table, qkv, n_seq, H, region=None, out=None, lse=None, 
     lp = _lse(lse, n_seq, H, rp.T) if lse is not None else None
     _on_current(("table", table), ("qkv", qkv), ("region", region), ("out", out), ("lse", lse),
                 ("workspace", workspace))
-    wp, nbytes, keep = _workspace(workspace, relpos_workspace_size(rp, n_seq, H), qkv.device, stream)
+    wp, nbytes, keep = _relpos_workspace(rp, n_seq, H, False, workspace, qkv.device, stream)
     _check(lib().lpv_relpos_attention(*args, op, ldo, lp, wp, nbytes, _stream(stream)),
            "lpv_relpos_attention")
     return out
@@ -593,8 +601,7 @@ def relpos_attention_grad(rp, table, qkv, out, lse, dout, n_seq, H, region=None,
         dqkv = torch.empty((M, 3 * H * hd), dtype=qkv.dtype, device=qkv.device)
     if dtable is None:
         dtable = torch.empty_like(table)
-    if tuple(dtable.shape) != tuple(table.shape) or dtable.dtype != table.dtype \
-            or not dtable.is_contiguous():
+    elif dtable.shape != table.shape or dtable.dtype != table.dtype or not dtable.is_contiguous():
         raise ValueError("dtable must be a contiguous tensor shaped and typed like table")
     op, ldo = _rows(out, "out", M, H * hd, qkv.dtype)
     gp, ldg = _rows(dout, "dout", M, H * hd, qkv.dtype)
@@ -602,11 +609,9 @@ def relpos_attention_grad(rp, table, qkv, out, lse, dout, n_seq, H, region=None,
     lp = _lse(lse, n_seq, H, rp.T)
     _on_current(("table", table), ("qkv", qkv), ("region", region), ("out", out), ("lse", lse),
                 ("dout", dout), ("dqkv", dqkv), ("dtable", dtable), ("workspace", workspace))
-    wp, nbytes, keep = _workspace(workspace, relpos_workspace_size(rp, n_seq, H, True), qkv.device,
-                                  stream)
-    _check(lib().lpv_relpos_attention_grad(*args, op, ldo, lp, gp, ldg, dp, ldd,
-                                           ctypes.c_void_p(dtable.data_ptr()), wp, nbytes,
-                                           _stream(stream)), "lpv_relpos_attention_grad")
+    wp, nbytes, keep = _relpos_workspace(rp, n_seq, H, True, workspace, qkv.device, stream)
+    _check(lib().lpv_relpos_attention_grad(*args, op, ldo, lp, gp, ldg, dp, ldd, dtable.data_ptr(), wp,
+                                           nbytes, _stream(stream)), "lpv_relpos_attention_grad")
     return dqkv, dtable
 
 
@@ -634,24 +639,20 @@ def _distill(logits, ids, teacher, temperature, dloss, loss, dlogits, Vd, worksp
     if loss is None:
         loss = torch.empty(M, dtype=torch.float32, device=logits.device)
     for t, name in ((loss, "loss"), (dloss, "dloss")):
-        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (M,) or not t.is_contiguous()):
+        if t is not None and (t.dtype != torch.float32 or t.shape != (M,) or not t.is_contiguous()):
             raise ValueError("%s must be a contiguous float32 tensor of M elements" % name)
     _on_current(("logits", logits), ("ids", ids), ("teacher", teacher), ("dloss", dloss),
                 ("loss", loss), ("dlogits", dlogits), ("workspace", workspace))
-    pad = 16 // logits.element_size()
-
-    def rows(t, name, cols):
-        p, ld = _rows(t, name, M, V, logits.dtype)
-        # (one row's stride says nothing: any that covers it)
-        return p, ld if M > 1 else (cols + pad - 1) // pad * pad
-    zp, ldz = rows(logits, "logits", V)
-    dp, ldd = rows(dlogits, "dlogits", Vd) if dlogits is not None else (None, 0)
+    zp, ldz = _rows(logits, "logits", M, V, logits.dtype)
+    dp, ldd = _rows(dlogits, "dlogits", M, V, logits.dtype) if dlogits is not None else (None, 0)
+    if M == 1:  # (one row's stride says nothing: any that covers it)
+        pad = 16 // logits.element_size()
+        ldz, ldd = (V + pad - 1) // pad * pad, (max(V, Vd) + pad - 1) // pad * pad
     wp, nbytes, keep = _workspace(workspace, distill_workspace_size(M, V, k, logits.dtype), logits.device,
                                   stream)
-    vec = lambda t: ctypes.c_void_p(t.data_ptr() if t is not None else 0)
-    _check(lib().lpv_distill(zp, ldz, M, V, DTYPES[logits.dtype], vec(ids), vec(teacher), ldt, k,
-                             float(temperature), vec(dloss), vec(loss), dp, ldd, Vd, wp, nbytes,
-                             _stream(stream)), "lpv_distill")
+    _check(lib().lpv_distill(zp, ldz, M, V, DTYPES[logits.dtype], ids.data_ptr(), teacher.data_ptr(), ldt, k,
+                             float(temperature), dloss.data_ptr() if dloss is not None else None,
+                             loss.data_ptr(), dp, ldd, Vd, wp, nbytes, _stream(stream)), "lpv_distill")
     return loss
 
 
