@@ -30,4 +30,11 @@ __device__ inline uint4 att_read16(uint32_t addr)
     return __builtin_bit_cast(uint4, *(const __attribute__((address_space(3))) att_u4*)(uintptr_t)addr);
 }
 
+// The same as an operand (read as the vector that it is: taken apart and put together, the
+// load may become four).
+template <typename F> __device__ inline F att_frag(uint32_t addr)
+{
+    return *(const __attribute__((address_space(3))) F*)(uintptr_t)addr;
+}
+
 }  // namespace lpv

@@ -60,6 +60,13 @@ __device__ inline uint32_t lds32(const void* p)
 // column 8 (r / 4) + 4 (l / 32) + r % 4; in memory [r / 4][lane][r % 4], so that a wave's
 // loads and stores are whole lines.
 
+// A bias as the accumulator's start.  (A finite one stays finite: the product's overflow
+// would mask the pair.)
+__device__ inline float ready_bias(uint16_t t, uint16_t lowest, uint16_t neg_inf, float f)
+{
+    return t == lowest || t == neg_inf ? -INFINITY : fminf(fmaxf(f, -3e38f), 3e38f);
+}
+
 // Elements 4 g .. 4 g + 3 of this lane.
 template <int DT>
 __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, int g, int lane,
@@ -73,28 +80,57 @@ __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint16_t t = e[j] == 0xffff ? NEG_INF : table[(int64_t)e[j] * H + h];
-        // (a finite bias stays finite: the product's overflow would mask the pair)
-        const float f = fminf(fmaxf(Elem<DT>::to_f32(t) * root, -3e38f), 3e38f);
-        of[j] = t == LOWEST || t == NEG_INF ? -INFINITY : f;
+        of[j] = ready_bias(t, LOWEST, NEG_INF, Elem<DT>::to_f32(t) * root);
     }
     return o;
 }
 
+// The bias tiles of every head: blockIdx.z 0 those of idx, 1 those of its transpose.  A
+// workgroup takes a head and BIAS_TILES tiles; a head's column of the table is made ready in
+// LDS once, where its gathers cost no more than reads of consecutive values do (the lanes of
+// a tile's row differ by a constant in most indexes); larger tables are gathered in memory.
+constexpr int BIAS_TILES = 4, BIAS_LDS = 12288;  // buckets
+
 template <int DT>
-__global__ __launch_bounds__(256) void k_relpos_bias(const uint16_t* __restrict__ idx, int32_t nt,
-                                                     const uint16_t* __restrict__ table, int32_t H,
-                                                     float root, float* __restrict__ bias)
+__global__ __launch_bounds__(256) void k_relpos_bias(const uint16_t* __restrict__ idx,
+                                                     const uint16_t* __restrict__ idx_t, int32_t nt,
+                                                     const uint16_t* __restrict__ table, int32_t n_buckets,
+                                                     int32_t H, float root, float* __restrict__ bias,
+                                                     float* __restrict__ bias_t)
 {
-    const int64_t n_tiles = (int64_t)nt * nt;
-    const int64_t tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int h = blockIdx.y, lane = threadIdx.x & 63;
-    if (tile >= n_tiles)
-        return;
-    const int a = (int)(tile / nt), b = (int)(tile - (int64_t)a * nt);
-    float* dst = bias + ((int64_t)h * n_tiles + tile) * 1024 + lane * 4;
+    extern __shared__ float column[];  // n_buckets, or none
+    const int n_tiles = nt * nt, h = blockIdx.y, lane = threadIdx.x & 63;
+    const bool in_lds = n_buckets <= BIAS_LDS;
+    if (in_lds) {
+        constexpr uint16_t LOWEST = DT == LPV_BF16 ? 0xff7f : 0xfbff, NEG_INF = DT == LPV_BF16 ? 0xff80 : 0xfc00;
+        for (int i = threadIdx.x; i < n_buckets; i += 256) {
+            const uint16_t t = table[(int64_t)i * H + h];
+            column[i] = ready_bias(t, LOWEST, NEG_INF, Elem<DT>::to_f32(t) * root);
+        }
+        __syncthreads();
+    }
+    const uint16_t* from = blockIdx.z ? idx_t : idx;
+    float* to = (blockIdx.z ? bias_t : bias) + (int64_t)h * n_tiles * 1024 + lane * 4;
+    const int end = min(((int)blockIdx.x + 1) * BIAS_TILES, n_tiles);
+    for (int tile = blockIdx.x * BIAS_TILES + wave_id(); tile < end; tile += 4) {
+        const int a = tile / nt, b = tile - a * nt;
+        const uint16_t* src = from + ((int64_t)a * 32 + (lane & 31)) * (nt * 32) + b * 32 + 4 * (lane >> 5);
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-        *(float4*)(dst + 256 * g) = gather_bias<DT>(idx, nt, a, b, g, lane, table, H, h, root);
+        for (int g = 0; g < 4; ++g) {
+            float4 o;
+            if (in_lds) {
+                const uint2 v = *(const uint2*)(src + 8 * g);
+                const uint32_t e[4] = {v.x & 0xffffu, v.x >> 16, v.y & 0xffffu, v.y >> 16};
+                float* of = (float*)&o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    of[j] = e[j] == 0xffffu ? -INFINITY : column[e[j]];
+            } else {
+                o = gather_bias<DT>(from, nt, a, b, g, lane, table, H, h, root);
+            }
+            *(float4*)(to + (int64_t)tile * 1024 + 256 * g) = o;
+        }
+    }
 }
 
 __device__ inline f32x16 load_bias(const float* p)
@@ -226,14 +262,25 @@ __device__ inline void store_rows(uint16_t* row, const f32x16* o, float f, int h
 }
 
 // How a workgroup of the general kernels is laid out: QW 32-row tiles of one sequence and
-// head, KS waves to each; the other side's rows pass in blocks of B, of which a wave takes
+// head, KS waves to each; the other side's rows pass in blocks of 64, of which a wave takes
 // NI 32-row tiles.
 template <int QW_, int KS_> struct Shape {
-    static constexpr int QW = QW_, KS = KS_, NW = QW_ * KS_, NT = 64 * NW;
-    static constexpr int NI = KS_ == 1 ? 2 : 1, B = 32 * NI * KS_;
+    static constexpr int QW = QW_, KS = KS_, NW = QW_ * KS_, NT = 64 * NW, B = 64, NI = 2 / KS_;
 };
 
-// Workgroup -> (sequence, head, block of row tiles).
+// Workgroups of a launch in an order in which each XCD (workgroup L runs on XCD L % 8) takes
+// one run of neighbours, which find each other's rows and bias in its L2.
+__device__ inline uint32_t xcd_order(uint32_t n)
+{
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;  // (below 2^31 + 2^20)
+    const uint32_t per = n / 8, rest = n % 8, x = id % 8;
+    return id < n ? x * per + min(x, rest) + id / 8 : n;
+}
+
+// Workgroup -> (sequence, head, block of row tiles).  A head's blocks of a sequence follow
+// each other while its bias is small (they share K and V); else the sequences of a block do
+// (they share its bias: 4 KB a pair of tiles).
+constexpr int BIAS_SMALL = 256;  // tiles of a head's bias: 1 MB
 struct Place {
     int64_t seq;
     int h, blk;
@@ -241,10 +288,13 @@ struct Place {
 };
 __device__ inline Place place(const Rp& p, int n_blk)
 {
-    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;  // (below 2^31 + 2^20)
-    const uint32_t u = id / (uint32_t)p.n_seq;  // the sequences of one head's block follow each other
-    const uint32_t h = u / (uint32_t)n_blk;
-    return {(int64_t)(id - u * (uint32_t)p.n_seq), (int)h, (int)(u - h * (uint32_t)n_blk), h < (uint32_t)p.H};
+    const uint32_t seqs = (uint32_t)p.n_seq, n = seqs * (uint32_t)(p.H * n_blk), id = xcd_order(n);
+    const uint32_t inner = p.nt * p.nt <= BIAS_SMALL ? (uint32_t)n_blk : seqs;
+    const uint32_t u = id / inner, in = id - u * inner;
+    const uint32_t outer = p.nt * p.nt <= BIAS_SMALL ? seqs : (uint32_t)n_blk;
+    const uint32_t h = u / outer, out = u - h * outer;
+    return p.nt * p.nt <= BIAS_SMALL ? Place{(int64_t)out, (int)h, (int)in, id < n}
+                                     : Place{(int64_t)in, (int)h, (int)out, id < n};
 }
 
 // The label of a token that attends (mine) or is attended (theirs); 0 without labels.
@@ -253,28 +303,25 @@ template <bool REG> __device__ inline int label_mine(const int32_t* reg, int i)
     return !REG ? 0 : reg[i] < 0 ? NO_LABEL : reg[i];
 }
 
-// The pipeline of a general kernel: the next block's rows in flight while a block is worked
-// on, and the bias tiles of the next step.  step(nj, first row of the step in the block, the
-// block's rows in LDS, block % 2, the tiles' bias) takes J tiles at once (fewer at the end).
-// A step's bias is asked for before the rows that are asked for in the same block, so that
-// its wait is not for them too.
-template <int HD, typename Sh, bool REG, int J, typename LoadMore, typename StoreMore, typename Step>
+// The pipeline of a general kernel: the next block's rows are in flight while a block is
+// worked on, and the bias of the next tile.  step(first row of the tile in the block, the
+// block's rows in LDS, block % 2, the tile's bias) takes a tile; load_more(block) and
+// store_more(buffer) go along with the rows.  (In a block the bias is asked for before the
+// rows, so that its wait is not for those.  Two blocks ahead, and the bias two tiles, cost a
+// third of the waves: 64 x 197 tokens x 12 heads of 64 35.4 us against 29.0.)
+template <int HD, typename Sh, bool REG, typename LoadMore, typename StoreMore, typename Step>
 __device__ inline void pass_blocks(const Rp& p, const uint16_t* a, int64_t lda, const uint16_t* b,
                                    int64_t ldb, const int32_t* reg, const float* bias, bool busy, int part,
                                    char* buf, LoadMore&& load_more, StoreMore&& store_more, Step&& step)
 {
     constexpr int HALF = Sh::B * Row<HD>::RS;  // buf: [2][2][HALF]
     constexpr int NI = Sh::NI;
-    static_assert(J == 1 || J == NI, "a step is a tile or the wave's part of a block");
     const int n_b = (p.T + Sh::B - 1) / Sh::B;
     Stage<HD, Sh::NT, Sh::B, REG> st;
-    auto load_tiles = [&](f32x16* t, int blk, int i) {
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-            t[j] = load_bias(bias + (int64_t)min(blk * NI * Sh::KS + part + i + j, p.nt - 1) * 1024);
+    auto load_tile = [&](int blk, int i) {
+        return load_bias(bias + (int64_t)min(blk * NI * Sh::KS + part + i, p.nt - 1) * 1024);
     };
-    f32x16 next[J];
-    load_tiles(next, 0, 0);
+    f32x16 next = load_tile(0, 0);
     st.load(a, lda, b, ldb, 0, p.T, reg);
     load_more(0);
     st.store(buf, buf + HALF);
@@ -285,27 +332,16 @@ __device__ inline void pass_blocks(const Rp& p, const uint16_t* a, int64_t lda, 
         char* to = buf + (~blk & 1) * 2 * HALF;
         const bool more = blk + 1 < n_b;
 #pragma unroll
-        for (int i = 0; i < NI; i += J) {
-            f32x16 cur[J];
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-                cur[j] = next[j];
-            if (i + J < NI)
-                load_tiles(next, blk, i + J);
-            else
-                load_tiles(next, blk + 1, 0);
+        for (int i = 0; i < NI; ++i) {
+            const f32x16 cur = next;
+            next = i + 1 < NI ? load_tile(blk, i + 1) : load_tile(blk + 1, 0);
             if (i == 0 && more) {
                 st.load(a, lda, b, ldb, (blk + 1) * Sh::B, p.T, reg);
                 load_more(blk + 1);
             }
             __builtin_amdgcn_sched_barrier(0);
-            const int t = blk * NI * Sh::KS + part + i;
-            if (busy && t < p.nt) {
-                if (J == 1 || t + 1 < p.nt)
-                    step(std::integral_constant<int, J>(), 32 * (part + i), at, at + HALF, blk & 1, cur);
-                else
-                    step(std::integral_constant<int, 1>(), 32 * (part + i), at, at + HALF, blk & 1, cur);
-            }
+            if (busy && blk * NI * Sh::KS + part + i < p.nt)
+                step(32 * (part + i), at, at + HALF, blk & 1, cur);
         }
         if (more) {
             st.store(to, to + HALF);
@@ -351,7 +387,7 @@ __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, u
         o[d] = f32x16{};
     float m = -INFINITY, l = 0.0f;
     int32_t lv = -1;
-    pass_blocks<HD, Sh, REG, 1>(
+    pass_blocks<HD, Sh, REG>(
         p, base + hw, ldq, base + 2 * hw, ldq, reg,
         p.bias + ((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, kv,
         [&](int blk) {
@@ -363,30 +399,20 @@ __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, u
             if (REG && threadIdx.x < Sh::B)
                 lab[b][threadIdx.x] = lv;
         },
-        [&](auto ni, int row0, const char* kb, const char* vb, int b, const f32x16* bias) {
-            constexpr int NI = decltype(ni)::value;
+        [&](int row0, const char* kb, const char* vb, int b, const f32x16& bias) {
             const uint32_t ka = lds32(kb) + (row0 + l32) * RS + half * 16;
             const uint32_t va = tr_base<HD>(vb, lane) + row0 * RS;
-            f32x16 s[NI];
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-                s[i] = bias[i];
+            f32x16 s = bias;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
+                s = E::mma(att_frag<F>(ka + 32 * ks), qf[ks], s);
+            if (REG)
+                mask_region(s, mine, lab[b] + row0, half);
+            float t[4];
 #pragma unroll
-                for (int i = 0; i < NI; ++i)
-                    s[i] = E::mma(as_frag<F>(att_read16(ka + i * 32 * RS + 32 * ks)), qf[ks], s[i]);
-            float mt = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                if (REG)
-                    mask_region(s[i], mine, lab[b] + row0 + 32 * i, half);
-                float t[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    t[j] = fmaxf(fmaxf(s[i][j], s[i][j + 4]), fmaxf(s[i][j + 8], s[i][j + 12]));
-                mt = fmaxf(mt, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
-            }
+            for (int j = 0; j < 4; ++j)
+                t[j] = fmaxf(fmaxf(s[j], s[j + 4]), fmaxf(s[j + 8], s[j + 12]));
+            float mt = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
             mt = half_max(mt);
             // the weights' reference m follows a row's maximum when that is over 2^8 weights
             // above it: most tiles then need no rescaling (each row by its own scores)
@@ -401,24 +427,21 @@ __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, u
             }
             const float nms = m == -INFINITY ? 0.0f : -m * scale;  // (nothing yet: all weights 0)
             float ps[2] = {0.0f, 0.0f};
+            uint32_t pb[8];
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                uint32_t pb[8];
+            for (int j = 0; j < 8; ++j) {
+                const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * j], scale, nms));
+                const float e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], scale, nms));
+                ps[0] += e0;
+                ps[1] += e1;
+                pb[j] = pack2<DT>(e0, e1);
+            }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j], scale, nms));
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j + 1], scale, nms));
-                    ps[0] += e0;
-                    ps[1] += e1;
-                    pb[j] = pack2<DT>(e0, e1);
-                }
+            for (int u = 0; u < 2; ++u) {
+                const F pf = as_frag<F>(uint4{pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]});
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const F pf = as_frag<F>(uint4{pb[4 * t], pb[4 * t + 1], pb[4 * t + 2], pb[4 * t + 3]});
-#pragma unroll
-                    for (int d = 0; d < ND; ++d)
-                        o[d] = E::mma(tr_frag<F, HD>(va, 32 * i + 16 * t, d), pf, o[d]);
-                }
+                for (int d = 0; d < ND; ++d)
+                    o[d] = E::mma(tr_frag<F, HD>(va, 16 * u, d), pf, o[d]);
             }
             l += ps[0] + ps[1];
         });
@@ -534,7 +557,7 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __re
     for (int d = 0; d < ND; ++d)
         dq[d] = f32x16{};
     int32_t lv = -1;
-    pass_blocks<HD, Sh, REG, 1>(
+    pass_blocks<HD, Sh, REG>(
         p, base + hw, ldq, base + 2 * hw, ldq, reg,
         p.bias + ((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, kv,
         [&](int blk) {
@@ -546,42 +569,29 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __re
             if (REG && threadIdx.x < Sh::B)
                 lab[b][threadIdx.x] = lv;
         },
-        [&](auto ni, int row0, const char* kb, const char* vb, int b, const f32x16* bias) {
-            constexpr int NI = decltype(ni)::value;
+        [&](int row0, const char* kb, const char* vb, int b, const f32x16& bias) {
             const uint32_t ka = lds32(kb) + (row0 + l32) * RS + half * 16;
             const uint32_t va = lds32(vb) + (row0 + l32) * RS + half * 16;
             const uint32_t kt = tr_base<HD>(kb, lane) + row0 * RS;
-            f32x16 s[NI], dp[NI];
+            f32x16 s = bias, dp = {};
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                s[i] = bias[i];
-                dp[i] = f32x16{};
+            for (int ks = 0; ks < KS; ++ks) {
+                s = E::mma(att_frag<F>(ka + 32 * ks), qf[ks], s);
+                dp = E::mma(att_frag<F>(va + 32 * ks), gf[ks], dp);
             }
+            if (REG)
+                mask_region(s, mine, lab[b] + row0, half);
+            uint32_t db[8];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+            for (int j = 0; j < 8; ++j)
+                db[j] = pack2<DT>(__builtin_amdgcn_exp2f(fmaf(s[2 * j], scale, nl)) * (dp[2 * j] - D),
+                                  __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], scale, nl)) * (dp[2 * j + 1] - D));
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    s[i] = E::mma(as_frag<F>(att_read16(ka + i * 32 * RS + 32 * ks)), qf[ks], s[i]);
-                    dp[i] = E::mma(as_frag<F>(att_read16(va + i * 32 * RS + 32 * ks)), gf[ks], dp[i]);
-                }
+            for (int u = 0; u < 2; ++u) {
+                const F df = as_frag<F>(uint4{db[4 * u], db[4 * u + 1], db[4 * u + 2], db[4 * u + 3]});
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                if (REG)
-                    mask_region(s[i], mine, lab[b] + row0 + 32 * i, half);
-                uint32_t db[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j], scale, nl));
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i][2 * j + 1], scale, nl));
-                    db[j] = pack2<DT>(e0 * (dp[i][2 * j] - D), e1 * (dp[i][2 * j + 1] - D));
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const F df = as_frag<F>(uint4{db[4 * t], db[4 * t + 1], db[4 * t + 2], db[4 * t + 3]});
-#pragma unroll
-                    for (int d = 0; d < ND; ++d)
-                        dq[d] = E::mma(tr_frag<F, HD>(kt, 32 * i + 16 * t, d), df, dq[d]);
-                }
+                for (int d = 0; d < ND; ++d)
+                    dq[d] = E::mma(tr_frag<F, HD>(kt, 16 * u, d), df, dq[d]);
             }
         });
     if constexpr (Sh::KS == 2) {
@@ -632,7 +642,7 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
         acc[d] = f32x16{};
     float sl, sd;
     int32_t lv;
-    pass_blocks<HD, Sh, REG, 1>(
+    pass_blocks<HD, Sh, REG>(
         p, base, ldq, dout + at.seq * T * ldg + at.h * HD, ldg, reg,
         p.bias + ((int64_t)at.h * p.nt + min(kt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, qg,
         [&](int blk) {
@@ -657,52 +667,41 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
                     lab[b][threadIdx.x] = lv;
             }
         },
-        [&](auto ni, int row0, const char* qb, const char* gb, int b, const f32x16* bias) {
-            constexpr int NI = decltype(ni)::value;
+        [&](int row0, const char* qb, const char* gb, int b, const f32x16& bias) {
             const uint32_t qa = lds32(qb) + (row0 + l32) * RS + half * 16;
             const uint32_t ga = lds32(gb) + (row0 + l32) * RS + half * 16;
             const uint32_t qtr = tr_base<HD>(qb, lane) + row0 * RS;
             const uint32_t gtr = tr_base<HD>(gb, lane) + row0 * RS;
-            f32x16 s[NI], dp[NI];
+            f32x16 s = bias, dp = {};
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                s[i] = bias[i];
-                dp[i] = f32x16{};
+            for (int ks = 0; ks < KS; ++ks) {
+                s = E::mma(att_frag<F>(qa + 32 * ks), kf[ks], s);
+                dp = E::mma(att_frag<F>(ga + 32 * ks), vf[ks], dp);
+            }
+            if (REG)
+                mask_region(s, mine, lab[b] + row0, half);
+            uint32_t pb[8], db[8];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 nl = *(const float4*)(stats[b][0] + row0 + 8 * g + 4 * half);
+                const float4 D = *(const float4*)(stats[b][1] + row0 + 8 * g + 4 * half);
+                const float e0 = __builtin_amdgcn_exp2f(fmaf(s[4 * g], scale, nl.x));
+                const float e1 = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 1], scale, nl.y));
+                const float e2 = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 2], scale, nl.z));
+                const float e3 = __builtin_amdgcn_exp2f(fmaf(s[4 * g + 3], scale, nl.w));
+                pb[2 * g] = pack2<DT>(e0, e1);
+                pb[2 * g + 1] = pack2<DT>(e2, e3);
+                db[2 * g] = pack2<DT>(e0 * (dp[4 * g] - D.x), e1 * (dp[4 * g + 1] - D.y));
+                db[2 * g + 1] = pack2<DT>(e2 * (dp[4 * g + 2] - D.z), e3 * (dp[4 * g + 3] - D.w));
             }
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+            for (int u = 0; u < 2; ++u) {
+                const F pf = as_frag<F>(uint4{pb[4 * u], pb[4 * u + 1], pb[4 * u + 2], pb[4 * u + 3]});
+                const F df = as_frag<F>(uint4{db[4 * u], db[4 * u + 1], db[4 * u + 2], db[4 * u + 3]});
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    s[i] = E::mma(as_frag<F>(att_read16(qa + i * 32 * RS + 32 * ks)), kf[ks], s[i]);
-                    dp[i] = E::mma(as_frag<F>(att_read16(ga + i * 32 * RS + 32 * ks)), vf[ks], dp[i]);
-                }
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                if (REG)
-                    mask_region(s[i], mine, lab[b] + row0 + 32 * i, half);
-                uint32_t pb[8], db[8];
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float4 nl = *(const float4*)(stats[b][0] + row0 + 32 * i + 8 * g + 4 * half);
-                    const float4 D = *(const float4*)(stats[b][1] + row0 + 32 * i + 8 * g + 4 * half);
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[i][4 * g], scale, nl.x));
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[i][4 * g + 1], scale, nl.y));
-                    const float e2 = __builtin_amdgcn_exp2f(fmaf(s[i][4 * g + 2], scale, nl.z));
-                    const float e3 = __builtin_amdgcn_exp2f(fmaf(s[i][4 * g + 3], scale, nl.w));
-                    pb[2 * g] = pack2<DT>(e0, e1);
-                    pb[2 * g + 1] = pack2<DT>(e2, e3);
-                    db[2 * g] = pack2<DT>(e0 * (dp[i][4 * g] - D.x), e1 * (dp[i][4 * g + 1] - D.y));
-                    db[2 * g + 1] = pack2<DT>(e2 * (dp[i][4 * g + 2] - D.z), e3 * (dp[i][4 * g + 3] - D.w));
-                }
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const F pf = as_frag<F>(uint4{pb[4 * t], pb[4 * t + 1], pb[4 * t + 2], pb[4 * t + 3]});
-                    const F df = as_frag<F>(uint4{db[4 * t], db[4 * t + 1], db[4 * t + 2], db[4 * t + 3]});
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        acc[d] = E::mma(tr_frag<F, HD>(qtr, 32 * i + 16 * t, d), df, acc[d]);
-                        acc[ND + d] = E::mma(tr_frag<F, HD>(gtr, 32 * i + 16 * t, d), pf, acc[ND + d]);
-                    }
+                for (int d = 0; d < ND; ++d) {
+                    acc[d] = E::mma(tr_frag<F, HD>(qtr, 16 * u, d), df, acc[d]);
+                    acc[ND + d] = E::mma(tr_frag<F, HD>(gtr, 16 * u, d), pf, acc[ND + d]);
                 }
             }
         });
@@ -733,11 +732,11 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS;
     __shared__ __attribute__((aligned(16))) char rows[4][64 * RS];  // Q, dO, K, V
     const int T = p.T, n_blk = (p.nt + 1) / 2;
-    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;  // (fewer than 2^18)
-    const uint32_t u = id / (uint32_t)chunks;
-    const int chunk = (int)(id - u * (uint32_t)chunks);
-    const int h = (int)(u / (uint32_t)(n_blk * n_blk)), ab = (int)(u - (uint32_t)h * (n_blk * n_blk));
-    if (h >= p.H)
+    // (the blocks of pairs of one head and chunk follow each other: they share the rows)
+    const uint32_t n2 = (uint32_t)(n_blk * n_blk), n = n2 * (uint32_t)(chunks * p.H), id = xcd_order(n);
+    const uint32_t u = id / n2;
+    const int ab = (int)(id - u * n2), h = (int)(u / (uint32_t)chunks), chunk = (int)(u - (uint32_t)(h * chunks));
+    if (id >= n)
         return;
     const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int qb = ab / n_blk, kb = ab - qb * n_blk;
@@ -776,8 +775,8 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
             f32x16 s = bias, dp = {};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                s = E::mma(as_frag<F>(att_read16(ka + 32 * ks)), as_frag<F>(att_read16(qa + 32 * ks)), s);
-                dp = E::mma(as_frag<F>(att_read16(va + 32 * ks)), as_frag<F>(att_read16(ga + 32 * ks)), dp);
+                s = E::mma(att_frag<F>(ka + 32 * ks), att_frag<F>(qa + 32 * ks), s);
+                dp = E::mma(att_frag<F>(va + 32 * ks), att_frag<F>(ga + 32 * ks), dp);
             }
             if (REG) {
                 const int32_t* reg = labels(p, seq);
@@ -870,20 +869,23 @@ __global__ __launch_bounds__(256) void k_relpos_segments(const int32_t* __restri
     }
 }
 
-// The segments of each bucket, in order.
+// The segments of a bucket: a wave adds them, each lane its own in order, then a fixed tree.
 template <int DT>
 __global__ __launch_bounds__(256) void k_relpos_buckets(const int32_t* __restrict__ bucket_seg,
                                                         const float* __restrict__ sums, int32_t n_buckets,
                                                         int32_t H, uint16_t* __restrict__ dtable)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (int64_t)n_buckets * H)
+    const int b = blockIdx.x * 4 + wave_id(), h = blockIdx.y, lane = threadIdx.x & 63;
+    if (b >= n_buckets)
         return;
-    const int b = (int)(i / H), h = (int)(i - (int64_t)b * H);
     float v = 0.0f;
-    for (int g = bucket_seg[b]; g < bucket_seg[b + 1]; ++g)
+    for (int g = bucket_seg[b] + lane; g < bucket_seg[b + 1]; g += 64)
         v += sums[(int64_t)g * H + h];
-    dtable[i] = Elem<DT>::from_f32(v);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+        v += __shfl_xor(v, o, 64);
+    if (lane == 0)
+        dtable[(int64_t)b * H + h] = Elem<DT>::from_f32(v);
 }
 
 // ---------------------------------------------------------------- up to 64 tokens
@@ -1010,7 +1012,7 @@ __global__ __launch_bounds__(256, HD == 32 ? 2 : 1) void k_relpos_window_fwd(
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
                 for (int i = 0; i < NT; ++i)
-                    s[i] = E::mma(as_frag<F>(att_read16(ka + i * 32 * RS + 32 * ks)), qf[t][ks], s[i]);
+                    s[i] = E::mma(att_frag<F>(ka + i * 32 * RS + 32 * ks), qf[t][ks], s[i]);
             if (REG && cut) {
                 const int mine = __shfl(lab, 32 * t + l32, 64);
 #pragma unroll
@@ -1156,8 +1158,8 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
         F qf[KS], gf[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            qf[ks] = as_frag<F>(att_read16(qa + 32 * ks));
-            gf[ks] = as_frag<F>(att_read16(ga + 32 * ks));
+            qf[ks] = att_frag<F>(qa + 32 * ks);
+            gf[ks] = att_frag<F>(ga + 32 * ks);
         }
         f32x16 s[NT], dp[NT];
         float D = 0.0f;
@@ -1167,8 +1169,8 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
             dp[b] = f32x16{};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                s[b] = E::mma(as_frag<F>(att_read16(ka + b * 32 * RS + 32 * ks)), qf[ks], s[b]);
-                dp[b] = E::mma(as_frag<F>(att_read16(va + b * 32 * RS + 32 * ks)), gf[ks], dp[b]);
+                s[b] = E::mma(att_frag<F>(ka + b * 32 * RS + 32 * ks), qf[ks], s[b]);
+                dp[b] = E::mma(att_frag<F>(va + b * 32 * RS + 32 * ks), gf[ks], dp[b]);
             }
             if (REG)
                 mask_region(s[b], mine, labs + 32 * b, half);
@@ -1287,13 +1289,14 @@ Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
 }
 
 template <int DT>
-hipError_t expand_bias(const lpv_relpos* h, bool transposed, const void* table, int32_t H, int32_t hd,
-                       float* bias, hipStream_t s)
+hipError_t expand_bias(const lpv_relpos* h, const void* table, int32_t H, int32_t hd, float* bias,
+                       float* bias_t, hipStream_t s)
 {
-    const int64_t tiles = (int64_t)h->nt * h->nt;
-    hipLaunchKernelGGL((k_relpos_bias<DT>), dim3((uint32_t)((tiles + 3) / 4), H), dim3(256), 0, s,
-                       transposed ? h->idx_t : h->idx, h->nt, (const uint16_t*)table, H,
-                       sqrtf((float)hd), bias);
+    const int tiles = h->nt * h->nt;
+    const dim3 grid((tiles + BIAS_TILES - 1) / BIAS_TILES, H, bias_t ? 2 : 1);
+    hipLaunchKernelGGL((k_relpos_bias<DT>), grid, dim3(256), h->n_buckets <= BIAS_LDS ? h->n_buckets * 4 : 0, s,
+                       h->idx, h->idx_t, h->nt, (const uint16_t*)table, h->n_buckets, H, sqrtf((float)hd), bias,
+                       bias_t);
     return hipGetLastError();
 }
 
@@ -1339,7 +1342,7 @@ template <int DT, int HD, bool REG> hipError_t forward_as(const lpv_relpos* h, c
 {
     if (is_window(h))
         return h->nt == 1 ? forward_windows<DT, HD, REG, 1>(h, c, s) : forward_windows<DT, HD, REG, 2>(h, c, s);
-    const hipError_t e = expand_bias<DT>(h, false, c.table, c.H, HD, (float*)c.ws, s);
+    const hipError_t e = expand_bias<DT>(h, c.table, c.H, HD, (float*)c.ws, nullptr, s);
     if (e != hipSuccess)
         return e;
     return few_tiles(h, c) ? forward_tiles<DT, HD, REG, Shape<2, 2>>(h, c, s)
@@ -1372,9 +1375,7 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
         e = h->nt == 1 ? grad_windows<DT, HD, REG, 1>(h, c, w, chunks, s)
                        : grad_windows<DT, HD, REG, 2>(h, c, w, chunks, s);
     } else if (chunks > 0) {  // (n_seq > 0)
-        e = expand_bias<DT>(h, false, c.table, c.H, HD, w.bias, s);
-        if (e == hipSuccess)
-            e = expand_bias<DT>(h, true, c.table, c.H, HD, w.bias_t, s);
+        e = expand_bias<DT>(h, c.table, c.H, HD, w.bias, w.bias_t, s);
         if (e == hipSuccess)
             e = few_tiles(h, c) ? grad_tiles<DT, HD, REG, Shape<2, 2>>(h, c, w, s)
                                 : grad_tiles<DT, HD, REG, Shape<4, 1>>(h, c, w, s);
@@ -1397,8 +1398,8 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
                        chunks > 0 ? w.sum : nullptr, n_pos, c.H, w.sums, whole ? (uint16_t*)c.dtable : nullptr);
     if (!whole)
         hipLaunchKernelGGL((k_relpos_buckets<DT>),
-                           dim3((uint32_t)(((int64_t)h->n_buckets * c.H + 255) / 256)), dim3(256), 0, s,
-                           h->bucket_seg, w.sums, h->n_buckets, c.H, (uint16_t*)c.dtable);
+                           dim3((h->n_buckets + 3) / 4, c.H), dim3(256), 0, s, h->bucket_seg,
+                           w.sums, h->n_buckets, c.H, (uint16_t*)c.dtable);
     return hipGetLastError();
 }
 
