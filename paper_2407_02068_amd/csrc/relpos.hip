@@ -804,15 +804,18 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
 }
 
 // The chunks' sums of each pair: CL threads of a workgroup share a pair's chunks (each in
-// order, then the threads'), 4 pairs to a thread.
+// order, then the threads'), 4 pairs to a thread.  per > 0: of a head's slots, those that
+// k_relpos_mid_grad's workgroups have filled, which take `per` of all heads' sequences each.
 template <int CL>
-__global__ __launch_bounds__(256) void k_relpos_fold(const float* __restrict__ part, int32_t chunks,
-                                                     int64_t n_pos, float* __restrict__ sum)
+__global__ __launch_bounds__(256) void k_relpos_fold(const float* __restrict__ part, int32_t slots,
+                                                     uint32_t n_seq, uint32_t per, int64_t n_pos,
+                                                     float* __restrict__ sum)
 {
     __shared__ float4 red[256];
     const int x = threadIdx.x % (256 / CL), c0 = threadIdx.x / (256 / CL), h = blockIdx.y;
     const int64_t i = ((int64_t)blockIdx.x * (256 / CL) + x) * 4;  // (n_pos is a multiple of 1024)
-    const float* at = part + (int64_t)h * chunks * n_pos + i;
+    const float* at = part + (int64_t)h * slots * n_pos + i;
+    const int chunks = per ? (int)(((h + 1) * n_seq - 1) / per - h * n_seq / per) + 1 : slots;
     float4 v = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int c = c0; c < chunks; c += CL) {
         const float4 w = *(const float4*)(at + c * n_pos);
@@ -1249,8 +1252,281 @@ int64_t tile_floats(const lpv_relpos* h) { return (int64_t)h->nt * h->nt * 1024;
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
+// ---------------------------------------------------------------- gradients, 65 to 224 tokens
+
+// Gradients of sequences whose tiles of dS a workgroup's registers can add up: a wave to a
+// 32-query tile, all of a sequence's in one workgroup, and one wave more.  A workgroup takes
+// the `per` next sequences, head after head.  The key tiles pass one at a time: every query
+// wave forms S^T, P, dS of its queries (lane = query), adds dS to its sums and dS K to its dQ,
+// and leaves P and dS, rounded once, in one of two LDS buffers; meanwhile the last wave turns
+// the tile before into dV^T = dO^T P and dK^T = Q^T dS over all queries.  So every score is
+// formed once, with five products, where the general kernels form it three times with nine.
+// LDS holds all rows of Q and dO, two key tiles and the two buffers.  Bound: LDS reads and
+// the chain of a tile at two waves to a SIMD (the sums leave registers for no more).
+template <int DT, int HD, int NT, bool REG>
+__global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
+    Rp p, const uint16_t* __restrict__ out, int64_t ldo, const float* __restrict__ lse,
+    const uint16_t* __restrict__ dout, int64_t ldg, uint16_t* __restrict__ dqkv, int64_t lddq,
+    float* __restrict__ part, int32_t per, int32_t slots, float scale, float rroot)
+{
+    using E = Elem<DT>;
+    using F = typename E::frag;
+    constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT, CH = HD / 8;
+    constexpr int XS = 80;                  // bytes of a row of P or dS: 32 keys
+    constexpr int KV = 32 * RS;             // a key tile of K or V
+    constexpr int NR = 32 * CH / 64;        // a tile's chunks to a lane
+    constexpr int NK = (64 * CH + 191) / 192;  // a key tile's chunks of K and V to a thread (3 query waves or more)
+    constexpr bool KEEP = HD == 32;  // the operands of Q and dO stay in registers; else LDS has them
+    extern __shared__ uint4 mid_lds[];
+    const int T = p.T, nt = p.nt, tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+    const int l32 = lane & 31, half = lane >> 5, threads = 64 * nt;
+    char* Qr = (char*)mid_lds;
+    char* Gr = Qr + 32 * nt * RS;
+    char* kv = Gr + 32 * nt * RS;  // [2][K, V][KV]
+    char* X = kv + 4 * KV;         // [2][P, dS][32 nt][XS]
+    int32_t* labs = (int32_t*)(X + 4 * 32 * nt * XS);
+    const uint32_t units = (uint32_t)p.n_seq * (uint32_t)p.H, wgs = (units + per - 1) / per, wg = xcd_order(wgs);
+    if (wg >= wgs)
+        return;
+    const uint32_t u0 = wg * per, u1 = min(u0 + per, units), seqs = (uint32_t)p.n_seq;
+    const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
+    const uint32_t qtr = tr_base<HD>(Qr, lane), gtr = tr_base<HD>(Gr, lane);
+    if (wave == nt) {  // dK and dV
+        // this lane's transposing read of P and dS (rows are queries, columns the tile's keys)
+        const int g16 = lane >> 4, j16 = lane & 15;
+        const uint32_t xtr = lds32(X) + ((j16 >> 2) + 4 * (g16 >> 1)) * XS + (16 * (g16 & 1) + 4 * (j16 & 3)) * 2;
+        for (uint32_t u = u0; u < u1; ++u) {
+            const uint32_t h = u / seqs;
+            const int64_t seq = u - h * seqs;
+            auto outputs = [&](int kt) {
+                f32x16 dk[ND], dv[ND];
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    dk[d] = f32x16{};
+                    dv[d] = f32x16{};
+                }
+                const uint32_t x = xtr + (kt & 1) * 2 * 32 * nt * XS;
+                auto x_frag = [&](uint32_t at) {
+                    const uint2 lo = att_tr_read(at), hi = att_tr_read(at + 8 * XS);
+                    return as_frag<F>(uint4{lo.x, lo.y, hi.x, hi.y});
+                };
+                // a step's operands are read while the step before is multiplied
+                struct Step {
+                    F p, ds, g[ND], q[ND];
+                } step[2];
+                auto read = [&](Step& t, int row) {
+                    t.p = x_frag(x + row * XS);
+                    t.ds = x_frag(x + (32 * nt + row) * XS);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        t.g[d] = tr_frag<F, HD>(gtr, row, d);
+                        t.q[d] = tr_frag<F, HD>(qtr, row, d);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                auto multiply = [&](const Step& t) {
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        dv[d] = E::mma(t.g[d], t.p, dv[d]);
+                        dk[d] = E::mma(t.q[d], t.ds, dk[d]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                read(step[0], 0);
+                for (int row = 0; row < 32 * nt; row += 32) {
+                    read(step[1], row + 16);
+                    multiply(step[0]);
+                    read(step[0], row + 32 < 32 * nt ? row + 32 : 0);  // (the last one's is not used)
+                    multiply(step[1]);
+                }
+                const int k = 32 * kt + l32;
+                if (k < T) {
+                    uint16_t* row = dqkv + (seq * T + k) * lddq + h * HD;
+                    store_rows<DT, HD>(row + hw, dk, rroot, half);
+                    store_rows<DT, HD>(row + 2 * hw, dv, 1.0f, half);
+                }
+            };
+            __syncthreads();
+            __syncthreads();
+            for (int kt = 0; kt < nt; ++kt) {
+                if (kt > 0)
+                    outputs(kt - 1);
+                __syncthreads();
+            }
+            outputs(nt - 1);
+        }
+        return;
+    }
+    const int q = 32 * wave + l32;
+    const uint32_t qa = lds32(Qr) + q * RS + half * 16, ga = lds32(Gr) + q * RS + half * 16;
+    for (uint32_t unit = u0; unit < u1;) {  // a head
+        const uint32_t h = unit / seqs, end = min(u1, (h + 1) * seqs);
+        f32x16 sum[NT];
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+            sum[b] = f32x16{};
+        for (; unit < end; ++unit) {
+            const int64_t seq = unit - h * seqs;
+            const uint16_t* base = p.qkv + seq * T * ldq + h * HD;
+            const uint16_t* g = dout + seq * T * ldg + h * HD;
+            const int32_t* reg = REG ? labels(p, seq) : nullptr;
+            const float* bias = p.bias + ((int64_t)h * nt + wave) * nt * 1024 + lane * 4;
+            uint4 kvr[NK];
+            // (the thread's number as no constant: its chunks' places would be kept in registers)
+            auto load_kv = [&](int kt) {
+                int t = tid;
+                asm volatile("" : "+v"(t));
+#pragma unroll
+                for (int i = 0; i < NK; ++i) {
+                    const int c = t + i * threads, m = c / (32 * CH), r = 32 * kt + c / CH % 32;
+                    kvr[i] = uint4{0u, 0u, 0u, 0u};
+                    if (c < 64 * CH && r < T && (!REG || reg[r] >= 0))
+                        kvr[i] = *(const uint4*)(base + (1 + m) * hw + (int64_t)r * ldq + 8 * (c % CH));
+                }
+            };
+            auto store_kv = [&](int buf) {
+                int t = tid;
+                asm volatile("" : "+v"(t));
+#pragma unroll
+                for (int i = 0; i < NK; ++i) {
+                    const int c = t + i * threads;
+                    if (c < 64 * CH)
+                        *(uint4*)(kv + (2 * buf + c / (32 * CH)) * KV + c / CH % 32 * RS + 16 * (c % CH)) = kvr[i];
+                }
+            };
+            load_kv(0);
+            uint4 qr[NR], gr[NR];
+            int lo = lane;
+            asm volatile("" : "+v"(lo));
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const int c = lo + 64 * i, r = 32 * wave + c / CH, k = 8 * (c % CH);
+                qr[i] = gr[i] = uint4{0u, 0u, 0u, 0u};
+                if (r < T && (!REG || reg[r] >= 0)) {
+                    qr[i] = *(const uint4*)(base + (int64_t)r * ldq + k);
+                    gr[i] = *(const uint4*)(g + (int64_t)r * ldg + k);
+                }
+            }
+            const int lab = REG && q < T ? max(reg[q], -1) : -1;
+            const int mine = !REG ? 0 : lab < 0 ? NO_LABEL : lab;
+            float D = 0.0f, nl = -INFINITY;
+            F qf[KS], gf[KS];
+            {
+                F of[KS];
+                load_frags<F, HD>(of, out + (seq * T + min(q, T - 1)) * ldo + h * HD, half,
+                                  q < T && (!REG || lab >= 0));
+                if (q < T) {
+                    const float v = lse[(seq * p.H + h) * T + q];
+                    nl = v == -INFINITY ? -INFINITY : -v * LOG2E;
+                }
+                __syncthreads();  // (the last sequence's rows have been read)
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    const int c = lo + 64 * i, at = (32 * wave + c / CH) * RS + 16 * (c % CH);
+                    *(uint4*)(Qr + at) = qr[i];
+                    *(uint4*)(Gr + at) = gr[i];
+                }
+                if (REG && half == 0)
+                    labs[q] = lab;
+                store_kv(0);
+                if (nt > 1)
+                    load_kv(1);
+                __syncthreads();
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    qf[ks] = att_frag<F>(qa + 32 * ks);
+                    gf[ks] = att_frag<F>(ga + 32 * ks);
+                }
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        D = fmaf((float)gf[ks][j], (float)of[ks][j], D);
+                D = half_add(D);
+            }
+            f32x16 dq[ND];
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                dq[d] = f32x16{};
+            f32x16 s = load_bias(bias);
+#pragma unroll
+            for (int sk = 0; sk < NT; ++sk) {
+                if (sk >= nt)
+                    break;
+                int kt = sk;  // (as no constant, for the same reason)
+                asm volatile("" : "+s"(kt));
+                const uint32_t kb = lds32(kv) + (kt & 1) * 2 * KV;
+                const uint32_t ka = kb + l32 * RS + half * 16, va = ka + KV;
+                const uint32_t ktr = tr_base<HD>(kv, lane) + (kt & 1) * 2 * KV;
+                char* x = X + (kt & 1) * 2 * 32 * nt * XS;
+                f32x16 dp = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    s = E::mma(att_frag<F>(ka + 32 * ks), KEEP ? qf[ks] : att_frag<F>(qa + 32 * ks), s);
+                    dp = E::mma(att_frag<F>(va + 32 * ks), KEEP ? gf[ks] : att_frag<F>(ga + 32 * ks), dp);
+                }
+                if (REG)
+                    mask_region(s, mine, labs + 32 * kt, half);
+                uint32_t db[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float e[4], f[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        e[j] = __builtin_amdgcn_exp2f(fmaf(s[4 * i + j], scale, nl));
+                        f[j] = e[j] * (dp[4 * i + j] - D);
+                        sum[sk][4 * i + j] += f[j];
+                    }
+                    db[2 * i] = pack2<DT>(f[0], f[1]);
+                    db[2 * i + 1] = pack2<DT>(f[2], f[3]);
+                    const int at = q * XS + (8 * i + 4 * half) * 2;
+                    *(uint2*)(x + at) = uint2{pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3])};
+                    *(uint2*)(x + 32 * nt * XS + at) = uint2{db[2 * i], db[2 * i + 1]};
+                }
+                if (kt + 1 < nt) {
+                    s = load_bias(bias + (kt + 1) * 1024);
+                    store_kv(1 - (kt & 1));
+                    if (kt + 2 < nt)
+                        load_kv(kt + 2);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const F df = as_frag<F>(uint4{db[4 * u], db[4 * u + 1], db[4 * u + 2], db[4 * u + 3]});
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+                        dq[d] = E::mma(tr_frag<F, HD>(ktr, 16 * u, d), df, dq[d]);
+                }
+                __syncthreads();
+            }
+            if (q < T)
+                store_rows<DT, HD>(dqkv + (seq * T + q) * lddq + h * HD, dq, rroot, half);
+        }
+        // the sums, to this workgroup's slot of the head
+        float* dst = part + (((int64_t)h * slots + (wg - h * seqs / per)) * nt + wave) * nt * 1024 + lane * 4;
+#pragma unroll
+        for (int b = 0; b < NT; ++b)
+            if (b < nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *(float4*)(dst + b * 1024 + 256 * i) =
+                        float4{sum[b][4 * i], sum[b][4 * i + 1], sum[b][4 * i + 2], sum[b][4 * i + 3]};
+    }
+}
+
 constexpr int WINDOW_TILES = 2;  // tiles of 32 tokens that the window kernels take
 bool is_window(const lpv_relpos* h) { return h->nt <= WINDOW_TILES; }
+
+// The longest sequences of k_relpos_mid_grad, in tiles: with the wave more, two waves to a
+// SIMD, which their sums' registers allow.
+constexpr int MID_TILES = 7;
+bool is_mid(const lpv_relpos* h) { return !is_window(h) && h->nt <= MID_TILES; }
+size_t mid_lds_bytes(int nt, int hd)
+{
+    const size_t rs = (size_t)hd * 2 + 16;
+    return 2 * 32 * nt * rs + 4 * 32 * rs + 4 * 32 * (size_t)nt * 80 + 32 * nt * 4;
+}
+// Sequences of a head to a workgroup, one to a compute unit.
+int32_t mid_per(int64_t n_seq, int32_t H) { return (int32_t)((n_seq * H + 255) / 256); }
 
 // Chunks of sequences of the bias gradient: 1024 workgroups, four to a compute unit.
 int bias_chunks(const lpv_relpos* h, int64_t n_seq, int32_t H)
@@ -1258,6 +1534,10 @@ int bias_chunks(const lpv_relpos* h, int64_t n_seq, int32_t H)
     if (is_window(h)) {
         // 4 workgroups to a compute unit, or more where there are more heads
         return window_runs(n_seq, H, 1024, 1);
+    }
+    if (is_mid(h)) {  // (a head's sequences may begin and end inside a workgroup's)
+        const int32_t per = mid_per(n_seq, H);
+        return per ? (int)((n_seq + per - 1) / per + 1) : 0;
     }
     const int64_t n_blk = (h->nt + 1) / 2, wgs = (int64_t)H * n_blk * n_blk;
     const int64_t c = (1024 + wgs - 1) / wgs;
@@ -1277,12 +1557,13 @@ Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
         return p;
     };
     Ws w;
-    const bool window = is_window(h);
+    const bool window = is_window(h), mid = is_mid(h);
+    const int chunks = bias_chunks(h, n_seq, H);
     w.bias = take(window ? 0 : (size_t)(H * tile_floats(h)));
-    w.bias_t = take(window ? 0 : (size_t)(H * tile_floats(h)));
-    w.D = take(window ? 0 : (size_t)(n_seq * H * h->T));
-    w.part = take((size_t)(H * bias_chunks(h, n_seq, H) * tile_floats(h)));
-    w.sum = bias_chunks(h, n_seq, H) > 1 ? take((size_t)(H * tile_floats(h))) : w.part;
+    w.bias_t = take(window || mid ? 0 : (size_t)(H * tile_floats(h)));
+    w.D = take(window || mid ? 0 : (size_t)(n_seq * H * h->T));
+    w.part = take((size_t)(H * chunks * tile_floats(h)));
+    w.sum = chunks > 1 ? take((size_t)(H * tile_floats(h))) : w.part;
     w.sums = take((size_t)((int64_t)h->n_segs * H));
     w.bytes = at;
     return w;
@@ -1364,6 +1645,27 @@ hipError_t grad_tiles(const lpv_relpos* h, const RelposCall& c, const Ws& w, hip
     return hipGetLastError();
 }
 
+template <int DT, int HD, bool REG, int NT>
+hipError_t grad_mid(const lpv_relpos* h, const RelposCall& c, const Ws& w, int chunks, hipStream_t s)
+{
+    static bool allowed = false;  // (idempotent: a race between threads is harmless)
+    if (!allowed) {
+        const hipError_t e = hipFuncSetAttribute((const void*)k_relpos_mid_grad<DT, HD, NT, REG>,
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)mid_lds_bytes(NT, HD));
+        if (e != hipSuccess)
+            return e;
+        allowed = true;
+    }
+    const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
+    const int32_t per = mid_per(c.n_seq, c.H);
+    hipLaunchKernelGGL((k_relpos_mid_grad<DT, HD, NT, REG>), dim3((uint32_t)((c.n_seq * c.H + per - 1) / per)),
+                       dim3(64 * (h->nt + 1)), mid_lds_bytes(h->nt, HD), s, p, (const uint16_t*)c.out, c.ldo, c.lse,
+                       (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, w.part, per, chunks,
+                       LOG2E / sqrtf((float)HD), 1.0f / sqrtf((float)HD));
+    return hipGetLastError();
+}
+
 template <int DT, int HD, bool REG>
 hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
 {
@@ -1374,6 +1676,11 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
     if (chunks > 0 && is_window(h)) {
         e = h->nt == 1 ? grad_windows<DT, HD, REG, 1>(h, c, w, chunks, s)
                        : grad_windows<DT, HD, REG, 2>(h, c, w, chunks, s);
+    } else if (chunks > 0 && is_mid(h)) {
+        e = expand_bias<DT>(h, c.table, c.H, HD, w.bias, nullptr, s);
+        if (e == hipSuccess)
+            e = h->nt <= 5 ? grad_mid<DT, HD, REG, 5>(h, c, w, chunks, s)
+                           : grad_mid<DT, HD, REG, MID_TILES>(h, c, w, chunks, s);
     } else if (chunks > 0) {  // (n_seq > 0)
         e = expand_bias<DT>(h, c.table, c.H, HD, w.bias, w.bias_t, s);
         if (e == hipSuccess)
@@ -1387,12 +1694,13 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
     }
     if (e != hipSuccess)
         return e;
+    const uint32_t per = is_mid(h) ? (uint32_t)mid_per(c.n_seq, c.H) : 0;
     if (chunks >= 16)
         hipLaunchKernelGGL((k_relpos_fold<16>), dim3((uint32_t)(n_pos / 64), c.H), dim3(256), 0, s, w.part,
-                           chunks, n_pos, w.sum);
+                           chunks, (uint32_t)c.n_seq, per, n_pos, w.sum);
     else if (chunks > 1)
         hipLaunchKernelGGL((k_relpos_fold<1>), dim3((uint32_t)(n_pos / 1024), c.H), dim3(256), 0, s,
-                           w.part, chunks, n_pos, w.sum);
+                           w.part, chunks, (uint32_t)c.n_seq, per, n_pos, w.sum);
     const bool whole = h->n_segs == h->n_buckets;
     hipLaunchKernelGGL((k_relpos_segments<DT>), dim3(h->n_segs, c.H), dim3(256), 0, s, h->order, h->seg_ptr,
                        chunks > 0 ? w.sum : nullptr, n_pos, c.H, w.sums, whole ? (uint16_t*)c.dtable : nullptr);
