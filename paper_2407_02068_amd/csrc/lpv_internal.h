@@ -188,7 +188,7 @@ hipError_t launch_add_layernorm(const void* x, const void* y, int64_t M, int32_t
 hipError_t launch_attention(const void* qkv, int64_t n_seq, int32_t T, int32_t H, int dtype,
                             void* out, hipStream_t s);
 // relpos.hip
-constexpr int32_t RELPOS_MAX_T = 2048, RELPOS_MAX_BUCKETS = 65535, RELPOS_SEG = 2048;
+constexpr int32_t RELPOS_MAX_T = 2048, RELPOS_MAX_BUCKETS = 65535, RELPOS_SEG = 512;
 struct RelposCall {
     const void* table;  // n_buckets x H
     const void* qkv;

@@ -841,35 +841,42 @@ __global__ __launch_bounds__(256) void k_relpos_fold(const float* __restrict__ p
 }
 
 // The pairs of a bucket, in segments: order[seg_ptr[g] .. seg_ptr[g + 1]) are places in a
-// head's tiles.  A workgroup adds one segment, each thread its pairs in order, then a fixed
-// tree; out: [segment][head], or the table's gradient where every bucket is one segment.
-// sum NULL: no sequences, all zero.
+// head's tiles.  A wave adds one segment, each lane its pairs in order, then a fixed tree; out:
+// [segment][head], or the table's gradient where every bucket is one segment.  sum NULL: no
+// sequences, all zero.
 template <int DT>
 __global__ __launch_bounds__(256) void k_relpos_segments(const int32_t* __restrict__ order,
-                                                         const int32_t* __restrict__ seg_ptr,
+                                                         const int32_t* __restrict__ seg_ptr, int32_t n_segs,
                                                          const float* __restrict__ sum, int64_t n_pos,
                                                          int32_t H, float* __restrict__ sums,
                                                          uint16_t* __restrict__ dtable)
 {
-    __shared__ float red[4];
-    const int g = blockIdx.x, h = blockIdx.y;
+    const int g = blockIdx.x * 4 + wave_id(), h = blockIdx.y, lane = threadIdx.x & 63;
+    if (g >= n_segs)
+        return;
     float v = 0.0f;
-    if (sum)
-        for (int i = seg_ptr[g] + threadIdx.x; i < seg_ptr[g + 1]; i += 256)
-            v += sum[h * n_pos + order[i]];
+    if (sum) {
+        const float* at = sum + h * n_pos;
+        const int end = seg_ptr[g + 1];
+        for (int i = seg_ptr[g] + lane; i < end; i += 256) {
+            float w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[j] = i + 64 * j < end ? at[order[i + 64 * j]] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                v += w[j];
+        }
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
         v += __shfl_xor(v, o, 64);
-    if ((threadIdx.x & 63) == 0)
-        red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        v = (red[0] + red[1]) + (red[2] + red[3]);
-        if (dtable)
-            dtable[(int64_t)g * H + h] = Elem<DT>::from_f32(v);
-        else
-            sums[(int64_t)g * H + h] = v;
-    }
+    if (lane)
+        return;
+    if (dtable)
+        dtable[(int64_t)g * H + h] = Elem<DT>::from_f32(v);
+    else
+        sums[(int64_t)g * H + h] = v;
 }
 
 // The segments of a bucket: a wave adds them, each lane its own in order, then a fixed tree.
@@ -1263,6 +1270,7 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // formed once, with five products, where the general kernels form it three times with nine.
 // LDS holds all rows of Q and dO, two key tiles and the two buffers.  Bound: LDS reads and
 // the chain of a tile at two waves to a SIMD (the sums leave registers for no more).
+constexpr int MID_XS = 72;  // bytes of a row of P or dS, 32 keys: the writes of 32 rows' 8 bytes meet all banks
 template <int DT, int HD, int NT, bool REG>
 __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
     Rp p, const uint16_t* __restrict__ out, int64_t ldo, const float* __restrict__ lse,
@@ -1272,7 +1280,7 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT, CH = HD / 8;
-    constexpr int XS = 80;                  // bytes of a row of P or dS: 32 keys
+    constexpr int XS = MID_XS;
     constexpr int KV = 32 * RS;             // a key tile of K or V
     constexpr int NR = 32 * CH / 64;        // a tile's chunks to a lane
     constexpr int NK = (64 * CH + 191) / 192;  // a key tile's chunks of K and V to a thread (3 query waves or more)
@@ -1361,6 +1369,7 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
     const uint32_t qa = lds32(Qr) + q * RS + half * 16, ga = lds32(Gr) + q * RS + half * 16;
     for (uint32_t unit = u0; unit < u1;) {  // a head
         const uint32_t h = unit / seqs, end = min(u1, (h + 1) * seqs);
+        float* slot = part + (((int64_t)h * slots + (wg - h * seqs / per)) * nt + wave) * nt * 1024 + lane * 4;
         f32x16 sum[NT];
 #pragma unroll
         for (int b = 0; b < NT; ++b)
@@ -1496,20 +1505,18 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
                     for (int d = 0; d < ND; ++d)
                         dq[d] = E::mma(tr_frag<F, HD>(ktr, 16 * u, d), df, dq[d]);
                 }
+                if (unit + 1 == end) {  // the tile's sum is whole: to this workgroup's slot of the head
+                    float* dst = slot + kt * 1024;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *(float4*)(dst + 256 * i) = float4{sum[sk][4 * i], sum[sk][4 * i + 1], sum[sk][4 * i + 2],
+                                                           sum[sk][4 * i + 3]};
+                }
                 __syncthreads();
             }
             if (q < T)
                 store_rows<DT, HD>(dqkv + (seq * T + q) * lddq + h * HD, dq, rroot, half);
         }
-        // the sums, to this workgroup's slot of the head
-        float* dst = part + (((int64_t)h * slots + (wg - h * seqs / per)) * nt + wave) * nt * 1024 + lane * 4;
-#pragma unroll
-        for (int b = 0; b < NT; ++b)
-            if (b < nt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *(float4*)(dst + b * 1024 + 256 * i) =
-                        float4{sum[b][4 * i], sum[b][4 * i + 1], sum[b][4 * i + 2], sum[b][4 * i + 3]};
     }
 }
 
@@ -1523,7 +1530,7 @@ bool is_mid(const lpv_relpos* h) { return !is_window(h) && h->nt <= MID_TILES; }
 size_t mid_lds_bytes(int nt, int hd)
 {
     const size_t rs = (size_t)hd * 2 + 16;
-    return 2 * 32 * nt * rs + 4 * 32 * rs + 4 * 32 * (size_t)nt * 80 + 32 * nt * 4;
+    return 2 * 32 * nt * rs + 4 * 32 * rs + 4 * 32 * (size_t)nt * MID_XS + 32 * nt * 4;
 }
 // Sequences of a head to a workgroup, one to a compute unit.
 int32_t mid_per(int64_t n_seq, int32_t H) { return (int32_t)((n_seq * H + 255) / 256); }
@@ -1702,8 +1709,8 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
         hipLaunchKernelGGL((k_relpos_fold<1>), dim3((uint32_t)(n_pos / 1024), c.H), dim3(256), 0, s,
                            w.part, chunks, (uint32_t)c.n_seq, per, n_pos, w.sum);
     const bool whole = h->n_segs == h->n_buckets;
-    hipLaunchKernelGGL((k_relpos_segments<DT>), dim3(h->n_segs, c.H), dim3(256), 0, s, h->order, h->seg_ptr,
-                       chunks > 0 ? w.sum : nullptr, n_pos, c.H, w.sums, whole ? (uint16_t*)c.dtable : nullptr);
+    hipLaunchKernelGGL((k_relpos_segments<DT>), dim3((h->n_segs + 3) / 4, c.H), dim3(256), 0, s, h->order,
+                       h->seg_ptr, h->n_segs, chunks > 0 ? w.sum : nullptr, n_pos, c.H, w.sums, whole ? (uint16_t*)c.dtable : nullptr);
     if (!whole)
         hipLaunchKernelGGL((k_relpos_buckets<DT>),
                            dim3((h->n_buckets + 3) / 4, c.H), dim3(256), 0, s, h->bucket_seg,
@@ -1759,16 +1766,22 @@ void relpos_tables(const int32_t* index, int32_t T, int32_t n_buckets, int32_t n
     bucket_seg[n_buckets] = seg;
     seg_ptr[seg] = at;
     for (int32_t i = 0; i < T; ++i)
-        for (int32_t j = 0; j < T; ++j) {
-            const int32_t b = index[(int64_t)i * T + j];
-            if (b < 0)
-                continue;
-            idx[i * Tp + j] = (uint16_t)b;
-            idx_t[j * Tp + i] = (uint16_t)b;
-            // the pair's place in a head's tiles: row i % 32 in the lanes
-            const int32_t c = j % 32, lane = i % 32 + 32 * (c / 4 % 2);
-            order[count[b]++] = ((i / 32) * nt + j / 32) * 1024 + c / 8 * 256 + lane * 4 + c % 4;
-        }
+        for (int32_t j = 0; j < T; ++j)
+            if (index[(int64_t)i * T + j] >= 0) {
+                idx[i * Tp + j] = (uint16_t)index[(int64_t)i * T + j];
+                idx_t[j * Tp + i] = (uint16_t)index[(int64_t)i * T + j];
+            }
+    // a bucket's pairs in the order of their places (so that neighbours are read together):
+    // tile after tile, in one [c / 8][lane][c % 4] with row i % 32 in the lanes
+    for (int32_t a = 0; a < nt; ++a)
+        for (int32_t c = 0; c < nt; ++c)
+            for (int32_t at = 0; at < 1024; ++at) {
+                const int32_t lane = at / 4 % 64, i = 32 * a + lane % 32;
+                const int32_t j = 32 * c + at / 256 * 8 + lane / 32 * 4 + at % 4;
+                const uint16_t b = idx[i * Tp + j];
+                if (b != 0xffff)
+                    order[count[b]++] = (a * nt + c) * 1024 + at;
+            }
 }
 
 #define LPV_RP(FN_)                                                                          \
