@@ -147,12 +147,21 @@ __device__ inline f32x16 load_bias(const float* p)
     return s;
 }
 
+// A chunk of a row, or zero for a padding token's.
+template <bool REG> __device__ inline uint4 unless_padding(uint4 v, int lab)
+{
+    if (REG && lab < 0)
+        v = uint4{0u, 0u, 0u, 0u};
+    return v;
+}
+
 // ROWS rows of a head's slices of two matrices, from global memory through registers into
 // LDS, zero past T and for padding tokens (whose values, NaN too, then reach nothing).
 template <int HD, int NT, int ROWS, bool REG> struct Stage {
     static constexpr int CH = HD / 8;                    // 16-byte chunks per row
     static constexpr int N = (ROWS * CH + NT - 1) / NT;   // chunks per thread and matrix
     uint4 a[N], b[N];
+    int lab[N];  // the rows' labels: asked for beside them, so that neither waits for the other
     __device__ inline void load(const uint16_t* pa, int64_t lda, const uint16_t* pb, int64_t ldb,
                                 int row0, int T, const int32_t* reg)
     {
@@ -161,12 +170,12 @@ template <int HD, int NT, int ROWS, bool REG> struct Stage {
             const int c = threadIdx.x + i * NT, r = row0 + c / CH, k = c % CH;
             a[i] = uint4{0u, 0u, 0u, 0u};
             b[i] = uint4{0u, 0u, 0u, 0u};
-            bool ok = r < T && c < ROWS * CH;
-            if (REG && ok)
-                ok = reg[r] >= 0;
-            if (ok) {
+            lab[i] = 0;
+            if (r < T && c < ROWS * CH) {
                 a[i] = *(const uint4*)(pa + (int64_t)r * lda + 8 * k);
                 b[i] = *(const uint4*)(pb + (int64_t)r * ldb + 8 * k);
+                if (REG)
+                    lab[i] = reg[r];
             }
         }
     }
@@ -175,21 +184,23 @@ template <int HD, int NT, int ROWS, bool REG> struct Stage {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = threadIdx.x + i * NT;
+            const uint4 va = unless_padding<REG>(a[i], lab[i]), vb = unless_padding<REG>(b[i], lab[i]);
             if (ROWS * CH % NT == 0 || c < ROWS * CH) {
-                *(uint4*)(la + c / CH * Row<HD>::RS + 16 * (c % CH)) = a[i];
-                *(uint4*)(lb + c / CH * Row<HD>::RS + 16 * (c % CH)) = b[i];
+                *(uint4*)(la + c / CH * Row<HD>::RS + 16 * (c % CH)) = va;
+                *(uint4*)(lb + c / CH * Row<HD>::RS + 16 * (c % CH)) = vb;
             }
         }
     }
 };
 
-// A fragment of 8 head dimensions (8 half + 16 ks ..) of one row per lane, zero unless ok.
+// A fragment of 8 head dimensions (8 half + 16 ks ..) of one row per lane, zero unless ok
+// (the row, which exists, is read either way: it does not wait for its label).
 template <typename F, int HD>
 __device__ inline void load_frags(F* f, const uint16_t* row, int half, bool ok)
 {
 #pragma unroll
     for (int ks = 0; ks < HD / 16; ++ks)
-        f[ks] = as_frag<F>(ok ? *(const uint4*)(row + 8 * half + 16 * ks) : uint4{0u, 0u, 0u, 0u});
+        f[ks] = as_frag<F>(unless_padding<true>(*(const uint4*)(row + 8 * half + 16 * ks), ok ? 0 : -1));
 }
 
 // This lane's address for transposing reads of row-major staged rows: 16-lane group g
@@ -1097,7 +1108,7 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     uint4 next[4][N];
     float lsen = 0.0f;
-    int labn = 0;
+    int labn = 0, rlab[N] = {};
     const int q = 32 * wave + l32;
     auto load = [&](int64_t seq) {
         const uint16_t* base = p.qkv + seq * T * ldq + h * HD;
@@ -1109,7 +1120,9 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 next[j][i] = uint4{0u, 0u, 0u, 0u};
-            if (r < T && (!REG || reg[r] >= 0)) {  // (padding may hold anything)
+            if (r < T) {
+                if (REG)
+                    rlab[i] = reg[r];
                 const uint16_t* at = base + (int64_t)r * ldq + k;
                 next[0][i] = *(const uint4*)at;
                 next[1][i] = *(const uint4*)(at + hw);
@@ -1156,7 +1169,7 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
             const int c = tid + i * 64 * NT;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                *(uint4*)(rows[j] + c / CH * RS + 16 * (c % CH)) = next[j][i];
+                *(uint4*)(rows[j] + c / CH * RS + 16 * (c % CH)) = unless_padding<REG>(next[j][i], rlab[i]);
         }
         const float nl = lsen == -INFINITY ? -INFINITY : -lsen * LOG2E;
         const int mine = labn < 0 ? NO_LABEL : labn;
@@ -1381,6 +1394,7 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
             const int32_t* reg = REG ? labels(p, seq) : nullptr;
             const float* bias = p.bias + ((int64_t)h * nt + wave) * nt * 1024 + lane * 4;
             uint4 kvr[NK];
+            int kvl[NK];  // (the rows' labels, asked for beside them)
             // (the thread's number as no constant: its chunks' places would be kept in registers)
             auto load_kv = [&](int kt) {
                 int t = tid;
@@ -1389,8 +1403,12 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
                 for (int i = 0; i < NK; ++i) {
                     const int c = t + i * threads, m = c / (32 * CH), r = 32 * kt + c / CH % 32;
                     kvr[i] = uint4{0u, 0u, 0u, 0u};
-                    if (c < 64 * CH && r < T && (!REG || reg[r] >= 0))
+                    kvl[i] = 0;
+                    if (c < 64 * CH && r < T) {
                         kvr[i] = *(const uint4*)(base + (1 + m) * hw + (int64_t)r * ldq + 8 * (c % CH));
+                        if (REG)
+                            kvl[i] = reg[r];
+                    }
                 }
             };
             auto store_kv = [&](int buf) {
@@ -1400,20 +1418,26 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
                 for (int i = 0; i < NK; ++i) {
                     const int c = t + i * threads;
                     if (c < 64 * CH)
-                        *(uint4*)(kv + (2 * buf + c / (32 * CH)) * KV + c / CH % 32 * RS + 16 * (c % CH)) = kvr[i];
+                        *(uint4*)(kv + (2 * buf + c / (32 * CH)) * KV + c / CH % 32 * RS + 16 * (c % CH)) =
+                            unless_padding<REG>(kvr[i], kvl[i]);
                 }
             };
+            f32x16 s = load_bias(bias);
             load_kv(0);
             uint4 qr[NR], gr[NR];
+            int ql[NR];
             int lo = lane;
             asm volatile("" : "+v"(lo));
 #pragma unroll
             for (int i = 0; i < NR; ++i) {
                 const int c = lo + 64 * i, r = 32 * wave + c / CH, k = 8 * (c % CH);
                 qr[i] = gr[i] = uint4{0u, 0u, 0u, 0u};
-                if (r < T && (!REG || reg[r] >= 0)) {
+                ql[i] = 0;
+                if (r < T) {
                     qr[i] = *(const uint4*)(base + (int64_t)r * ldq + k);
                     gr[i] = *(const uint4*)(g + (int64_t)r * ldg + k);
+                    if (REG)
+                        ql[i] = reg[r];
                 }
             }
             const int lab = REG && q < T ? max(reg[q], -1) : -1;
@@ -1432,8 +1456,8 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
 #pragma unroll
                 for (int i = 0; i < NR; ++i) {
                     const int c = lo + 64 * i, at = (32 * wave + c / CH) * RS + 16 * (c % CH);
-                    *(uint4*)(Qr + at) = qr[i];
-                    *(uint4*)(Gr + at) = gr[i];
+                    *(uint4*)(Qr + at) = unless_padding<REG>(qr[i], ql[i]);
+                    *(uint4*)(Gr + at) = unless_padding<REG>(gr[i], ql[i]);
                 }
                 if (REG && half == 0)
                     labs[q] = lab;
@@ -1457,7 +1481,6 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
 #pragma unroll
             for (int d = 0; d < ND; ++d)
                 dq[d] = f32x16{};
-            f32x16 s = load_bias(bias);
 #pragma unroll
             for (int sk = 0; sk < NT; ++sk) {
                 if (sk >= nt)
