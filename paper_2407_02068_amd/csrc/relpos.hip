@@ -11,6 +11,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "lpv_attention.h"
@@ -86,17 +87,17 @@ __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, 
 }
 
 // The bias tiles of every head: blockIdx.z 0 those of idx, 1 those of its transpose.  A
-// workgroup takes a head and BIAS_TILES tiles; a head's column of the table is made ready in
+// workgroup takes a head and `per` tiles; a head's column of the table is made ready in
 // LDS once, where its gathers cost no more than reads of consecutive values do (the lanes of
 // a tile's row differ by a constant in most indexes); larger tables are gathered in memory.
-constexpr int BIAS_TILES = 4, BIAS_LDS = 12288;  // buckets
+constexpr int BIAS_LDS = 12288;  // buckets
 
 template <int DT>
 __global__ __launch_bounds__(256) void k_relpos_bias(const uint16_t* __restrict__ idx,
                                                      const uint16_t* __restrict__ idx_t, int32_t nt,
                                                      const uint16_t* __restrict__ table, int32_t n_buckets,
-                                                     int32_t H, float root, float* __restrict__ bias,
-                                                     float* __restrict__ bias_t)
+                                                     int32_t H, float root, int32_t per,
+                                                     float* __restrict__ bias, float* __restrict__ bias_t)
 {
     extern __shared__ float column[];  // n_buckets, or none
     const int n_tiles = nt * nt, h = blockIdx.y, lane = threadIdx.x & 63;
@@ -111,8 +112,8 @@ __global__ __launch_bounds__(256) void k_relpos_bias(const uint16_t* __restrict_
     }
     const uint16_t* from = blockIdx.z ? idx_t : idx;
     float* to = (blockIdx.z ? bias_t : bias) + (int64_t)h * n_tiles * 1024 + lane * 4;
-    const int end = min(((int)blockIdx.x + 1) * BIAS_TILES, n_tiles);
-    for (int tile = blockIdx.x * BIAS_TILES + wave_id(); tile < end; tile += 4) {
+    const int end = min(((int)blockIdx.x + 1) * per, n_tiles);
+    for (int tile = blockIdx.x * per + wave_id(); tile < end; tile += 4) {
         const int a = tile / nt, b = tile - a * nt;
         const uint16_t* src = from + ((int64_t)a * 32 + (lane & 31)) * (nt * 32) + b * 32 + 4 * (lane >> 5);
 #pragma unroll
@@ -244,6 +245,15 @@ __device__ inline void mask_region(f32x16& s, int mine, const int32_t* lab, int 
         s[4 * g + 2] = o.z == mine ? s[4 * g + 2] : -INFINITY;
         s[4 * g + 3] = o.w == mine ? s[4 * g + 3] : -INFINITY;
     }
+}
+
+// What the labels of 32 rows have in common: their value, DEAD (all padding) or MIXED.  lab:
+// this lane's row's (negative: -1); lanes 0-31 and 32-63 are a tile each.
+constexpr int32_t DEAD = -1, MIXED = -2;
+__device__ inline int32_t tile_state(int32_t lab, int half)
+{
+    const int32_t first = __shfl(lab, 32 * half, 64);
+    return (uint32_t)(__ballot(lab == first) >> (32 * half)) == 0xffffffffu ? first : MIXED;
 }
 
 // The label of a padding token as the one that attends; as the one attended it is -1, so
@@ -379,6 +389,8 @@ __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, u
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT;
     __shared__ __attribute__((aligned(16))) char kv[4 * Sh::B * RS];
     __shared__ __attribute__((aligned(16))) int32_t lab[2][Sh::B];
+    __shared__ int32_t states[2][2];
+    static_assert(Sh::B == 64, "a wave stages a block's labels");
     const int T = p.T;
     const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
     if (!at.ok)
@@ -390,6 +402,7 @@ __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, u
     const int part = wave % Sh::KS, qt = at.blk * Sh::QW + wave / Sh::KS, q = qt * 32 + l32;
     const bool busy = qt < p.nt;
     const int mine = label_mine<REG>(reg, min(q, T - 1));
+    const bool steps = busy && (!REG || !__all(mine == NO_LABEL));
     F qf[KS];
     load_frags<F, HD>(qf, base + (int64_t)min(q, T - 1) * ldq, half, busy && mine != NO_LABEL);
     f32x16 o[ND];
@@ -400,24 +413,29 @@ __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, u
     int32_t lv = -1;
     pass_blocks<HD, Sh, REG>(
         p, base + hw, ldq, base + 2 * hw, ldq, reg,
-        p.bias + ((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, kv,
+        p.bias + ((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt * 1024 + lane * 4, steps, part, kv,
         [&](int blk) {
             const int r = blk * Sh::B + threadIdx.x;
             if (REG && threadIdx.x < Sh::B)
                 lv = r < T ? max(reg[r], -1) : -1;
         },
         [&](int b) {
-            if (REG && threadIdx.x < Sh::B)
-                lab[b][threadIdx.x] = lv;
+            if (REG && wave == 0) {
+                lab[b][lane] = lv;
+                states[b][half] = tile_state(lv, half);
+            }
         },
         [&](int row0, const char* kb, const char* vb, int b, const f32x16& bias) {
             const uint32_t ka = lds32(kb) + (row0 + l32) * RS + half * 16;
             const uint32_t va = tr_base<HD>(vb, lane) + row0 * RS;
+            const int state = REG ? states[b][row0 / 32] : 0;
+            if (REG && state == DEAD)
+                return;
             f32x16 s = bias;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
                 s = E::mma(att_frag<F>(ka + 32 * ks), qf[ks], s);
-            if (REG)
+            if (REG && !__all(mine == state))
                 mask_region(s, mine, lab[b] + row0, half);
             float t[4];
 #pragma unroll
@@ -528,6 +546,8 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __re
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT;
     __shared__ __attribute__((aligned(16))) char kv[4 * Sh::B * RS];
     __shared__ __attribute__((aligned(16))) int32_t lab[2][Sh::B];
+    __shared__ int32_t states[2][2];
+    static_assert(Sh::B == 64, "a wave stages a block's labels");
     const int T = p.T;
     const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
     if (!at.ok)
@@ -540,7 +560,7 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __re
     const int qc = min(q, T - 1);
     const bool busy = qt < p.nt;
     const int mine = label_mine<REG>(reg, qc);
-    const bool live = busy && mine != NO_LABEL;
+    const bool live = busy && mine != NO_LABEL, steps = busy && (!REG || !__all(mine == NO_LABEL));
     F qf[KS], gf[KS];
     float D = 0.0f;
     {
@@ -570,27 +590,32 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __re
     int32_t lv = -1;
     pass_blocks<HD, Sh, REG>(
         p, base + hw, ldq, base + 2 * hw, ldq, reg,
-        p.bias + ((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, kv,
+        p.bias + ((int64_t)at.h * p.nt + min(qt, p.nt - 1)) * p.nt * 1024 + lane * 4, steps, part, kv,
         [&](int blk) {
             const int r = blk * Sh::B + threadIdx.x;
             if (REG && threadIdx.x < Sh::B)
                 lv = r < T ? max(reg[r], -1) : -1;
         },
         [&](int b) {
-            if (REG && threadIdx.x < Sh::B)
-                lab[b][threadIdx.x] = lv;
+            if (REG && wave == 0) {
+                lab[b][lane] = lv;
+                states[b][half] = tile_state(lv, half);
+            }
         },
         [&](int row0, const char* kb, const char* vb, int b, const f32x16& bias) {
             const uint32_t ka = lds32(kb) + (row0 + l32) * RS + half * 16;
             const uint32_t va = lds32(vb) + (row0 + l32) * RS + half * 16;
             const uint32_t kt = tr_base<HD>(kb, lane) + row0 * RS;
+            const int state = REG ? states[b][row0 / 32] : 0;
+            if (REG && state == DEAD)
+                return;
             f32x16 s = bias, dp = {};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 s = E::mma(att_frag<F>(ka + 32 * ks), qf[ks], s);
                 dp = E::mma(att_frag<F>(va + 32 * ks), gf[ks], dp);
             }
-            if (REG)
+            if (REG && !__all(mine == state))
                 mask_region(s, mine, lab[b] + row0, half);
             uint32_t db[8];
 #pragma unroll
@@ -630,6 +655,8 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
     __shared__ __attribute__((aligned(16))) char qg[4 * Sh::B * RS];
     __shared__ __attribute__((aligned(16))) float stats[2][2][Sh::B];
     __shared__ __attribute__((aligned(16))) int32_t lab[2][Sh::B];
+    __shared__ int32_t states[2][2];
+    static_assert(Sh::B == 64, "a wave stages a block's labels");
     const int T = p.T;
     const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
     if (!at.ok)
@@ -643,6 +670,7 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
     const bool busy = kt < p.nt;
     const int mine = label_mine<REG>(reg, kc);
     const bool live = busy && k < T && mine != NO_LABEL;
+    const bool steps = busy && (!REG || !__all(mine == NO_LABEL));
     F kf[KS], vf[KS];
     load_frags<F, HD>(kf, base + hw + (int64_t)kc * ldq, half, live);
     load_frags<F, HD>(vf, base + 2 * hw + (int64_t)kc * ldq, half, live);
@@ -655,7 +683,7 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
     int32_t lv;
     pass_blocks<HD, Sh, REG>(
         p, base, ldq, dout + at.seq * T * ldg + at.h * HD, ldg, reg,
-        p.bias + ((int64_t)at.h * p.nt + min(kt, p.nt - 1)) * p.nt * 1024 + lane * 4, busy, part, qg,
+        p.bias + ((int64_t)at.h * p.nt + min(kt, p.nt - 1)) * p.nt * 1024 + lane * 4, steps, part, qg,
         [&](int blk) {
             // -lse in base 2 (-inf past T and for rows without pairs: every weight 0), D, label
             sl = -INFINITY;
@@ -671,11 +699,13 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
             }
         },
         [&](int b) {
-            if (threadIdx.x < Sh::B) {
-                stats[b][0][threadIdx.x] = sl;
-                stats[b][1][threadIdx.x] = sd;
-                if (REG)
-                    lab[b][threadIdx.x] = lv;
+            if (wave == 0) {
+                stats[b][0][lane] = sl;
+                stats[b][1][lane] = sd;
+                if (REG) {
+                    lab[b][lane] = lv;
+                    states[b][half] = tile_state(lv, half);
+                }
             }
         },
         [&](int row0, const char* qb, const char* gb, int b, const f32x16& bias) {
@@ -683,13 +713,16 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
             const uint32_t ga = lds32(gb) + (row0 + l32) * RS + half * 16;
             const uint32_t qtr = tr_base<HD>(qb, lane) + row0 * RS;
             const uint32_t gtr = tr_base<HD>(gb, lane) + row0 * RS;
+            const int state = REG ? states[b][row0 / 32] : 0;
+            if (REG && state == DEAD)
+                return;
             f32x16 s = bias, dp = {};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 s = E::mma(att_frag<F>(qa + 32 * ks), kf[ks], s);
                 dp = E::mma(att_frag<F>(ga + 32 * ks), vf[ks], dp);
             }
-            if (REG)
+            if (REG && !__all(mine == state))
                 mask_region(s, mine, lab[b] + row0, half);
             uint32_t pb[8], db[8];
 #pragma unroll
@@ -1102,6 +1135,7 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
     __shared__ __attribute__((aligned(16))) char rows[4][32 * NT * RS];  // Q, K, V, dO
     __shared__ __attribute__((aligned(16))) char cross[2][32 * NT * PS];
     __shared__ __attribute__((aligned(16))) int32_t labs[32 * NT];
+    __shared__ int32_t states[NT];
     const int T = p.T, tid = threadIdx.x, lane = tid & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const WindowPlace at = window_place(p.H);
     const int h = at.h, chunk = at.chunk, chunks = at.of;
@@ -1173,8 +1207,13 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
         }
         const float nl = lsen == -INFINITY ? -INFINITY : -lsen * LOG2E;
         const int mine = labn < 0 ? NO_LABEL : labn;
-        if (REG && half == 0)
-            labs[q] = labn;
+        if (REG) {
+            const int32_t state = tile_state(labn, half);  // (both halves hold the same rows)
+            if (half == 0)
+                labs[q] = labn;
+            if (lane == 0)
+                states[wave] = state;
+        }
         __syncthreads();
         if (n + chunks < p.n_seq)
             load(n + chunks);
@@ -1195,7 +1234,7 @@ __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_gra
                 s[b] = E::mma(att_frag<F>(ka + b * 32 * RS + 32 * ks), qf[ks], s[b]);
                 dp[b] = E::mma(att_frag<F>(va + b * 32 * RS + 32 * ks), gf[ks], dp[b]);
             }
-            if (REG)
+            if (REG && !__all(q >= T || mine == states[b]))
                 mask_region(s[b], mine, labs + 32 * b, half);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -1306,6 +1345,7 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
     char* kv = Gr + 32 * nt * RS;  // [2][K, V][KV]
     char* X = kv + 4 * KV;         // [2][P, dS][32 nt][XS]
     int32_t* labs = (int32_t*)(X + 4 * 32 * nt * XS);
+    int32_t* states = labs + 32 * nt;
     const uint32_t units = (uint32_t)p.n_seq * (uint32_t)p.H, wgs = (units + per - 1) / per, wg = xcd_order(wgs);
     if (wg >= wgs)
         return;
@@ -1459,8 +1499,13 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
                     *(uint4*)(Qr + at) = unless_padding<REG>(qr[i], ql[i]);
                     *(uint4*)(Gr + at) = unless_padding<REG>(gr[i], ql[i]);
                 }
-                if (REG && half == 0)
-                    labs[q] = lab;
+                if (REG) {
+                    const int32_t state = tile_state(lab, half);  // (both halves hold the same rows)
+                    if (half == 0)
+                        labs[q] = lab;
+                    if (lane == 0)
+                        states[wave] = state;
+                }
                 store_kv(0);
                 if (nt > 1)
                     load_kv(1);
@@ -1497,7 +1542,7 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
                     s = E::mma(att_frag<F>(ka + 32 * ks), KEEP ? qf[ks] : att_frag<F>(qa + 32 * ks), s);
                     dp = E::mma(att_frag<F>(va + 32 * ks), KEEP ? gf[ks] : att_frag<F>(ga + 32 * ks), dp);
                 }
-                if (REG)
+                if (REG && !__all(mine == states[kt]))
                     mask_region(s, mine, labs + 32 * kt, half);
                 uint32_t db[8];
 #pragma unroll
@@ -1553,7 +1598,7 @@ bool is_mid(const lpv_relpos* h) { return !is_window(h) && h->nt <= MID_TILES; }
 size_t mid_lds_bytes(int nt, int hd)
 {
     const size_t rs = (size_t)hd * 2 + 16;
-    return 2 * 32 * nt * rs + 4 * 32 * rs + 4 * 32 * (size_t)nt * MID_XS + 32 * nt * 4;
+    return 2 * 32 * nt * rs + 4 * 32 * rs + 4 * 32 * (size_t)nt * MID_XS + 33 * nt * 4;
 }
 // Sequences of a head to a workgroup, one to a compute unit.
 int32_t mid_per(int64_t n_seq, int32_t H) { return (int32_t)((n_seq * H + 255) / 256); }
@@ -1603,11 +1648,13 @@ template <int DT>
 hipError_t expand_bias(const lpv_relpos* h, const void* table, int32_t H, int32_t hd, float* bias,
                        float* bias_t, hipStream_t s)
 {
-    const int tiles = h->nt * h->nt;
-    const dim3 grid((tiles + BIAS_TILES - 1) / BIAS_TILES, H, bias_t ? 2 : 1);
+    // (a tile to a wave, or more of them where that makes over 1024 workgroups, each of which
+    // makes the column ready for itself)
+    const int tiles = h->nt * h->nt, per = std::max(4, (tiles * H + 1023) / 1024);
+    const dim3 grid((tiles + per - 1) / per, H, bias_t ? 2 : 1);
     hipLaunchKernelGGL((k_relpos_bias<DT>), grid, dim3(256), h->n_buckets <= BIAS_LDS ? h->n_buckets * 4 : 0, s,
-                       h->idx, h->idx_t, h->nt, (const uint16_t*)table, h->n_buckets, H, sqrtf((float)hd), bias,
-                       bias_t);
+                       h->idx, h->idx_t, h->nt, (const uint16_t*)table, h->n_buckets, H, sqrtf((float)hd), per,
+                       bias, bias_t);
     return hipGetLastError();
 }
 
