@@ -291,9 +291,8 @@ template <int QW_, int KS_> struct Shape {
 
 // Workgroups of a launch in an order in which each XCD (workgroup L runs on XCD L % 8) takes
 // one run of neighbours, which find each other's rows and bias in its L2.
-__device__ inline uint32_t xcd_order(uint32_t n)
+__device__ inline uint32_t xcd_order(uint32_t n, uint32_t id)
 {
-    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x;  // (below 2^31 + 2^20)
     const uint32_t per = n / 8, rest = n % 8, x = id % 8;
     return id < n ? x * per + min(x, rest) + id / 8 : n;
 }
@@ -305,17 +304,16 @@ constexpr int BIAS_SMALL = 256;  // tiles of a head's bias: 1 MB
 struct Place {
     int64_t seq;
     int h, blk;
-    bool ok;
 };
-__device__ inline Place place(const Rp& p, int n_blk)
+__device__ inline Place place(const Rp& p, int n_blk, uint32_t id)
 {
-    const uint32_t seqs = (uint32_t)p.n_seq, n = seqs * (uint32_t)(p.H * n_blk), id = xcd_order(n);
+    const uint32_t seqs = (uint32_t)p.n_seq;
     const uint32_t inner = p.nt * p.nt <= BIAS_SMALL ? (uint32_t)n_blk : seqs;
     const uint32_t u = id / inner, in = id - u * inner;
     const uint32_t outer = p.nt * p.nt <= BIAS_SMALL ? seqs : (uint32_t)n_blk;
     const uint32_t h = u / outer, out = u - h * outer;
-    return p.nt * p.nt <= BIAS_SMALL ? Place{(int64_t)out, (int)h, (int)in, id < n}
-                                     : Place{(int64_t)in, (int)h, (int)out, id < n};
+    return p.nt * p.nt <= BIAS_SMALL ? Place{(int64_t)out, (int)h, (int)in}
+                                     : Place{(int64_t)in, (int)h, (int)out};
 }
 
 // The label of a token that attends (mine) or is attended (theirs); 0 without labels.
@@ -392,9 +390,12 @@ __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, u
     __shared__ int32_t states[2][2];
     static_assert(Sh::B == 64, "a wave stages a block's labels");
     const int T = p.T;
-    const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
-    if (!at.ok)
+    const int n_blk = (p.nt + Sh::QW - 1) / Sh::QW;
+    const uint32_t n = (uint32_t)p.n_seq * (uint32_t)(p.H * n_blk);
+    const uint32_t id = xcd_order(n, blockIdx.y * gridDim.x + blockIdx.x);  // (below 2^31 + 2^20)
+    if (id >= n)
         return;
+    const Place at = place(p, n_blk, id);
     const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     const uint16_t* base = p.qkv + at.seq * T * ldq + at.h * HD;
@@ -531,27 +532,69 @@ template <int N> __device__ inline bool join_sums(char* buf, f32x16* o, int wave
     return true;
 }
 
+// What the gradient kernels take beside Rp.
+struct Gp {
+    const float* lse;
+    const float* Dv;  // dO . O of each row, in lse's layout (anything for a row without pairs)
+    const uint16_t* dout;
+    int64_t ldg;
+    uint16_t* dqkv;
+    int64_t lddq;
+    const float* bias_t;  // the bias of the transposed index
+    float* part;
+    int32_t chunks;
+    float scale, rroot;
+};
+
+// LDS of a workgroup of the general gradients, whichever part it does.
+template <int HD> struct GradLds {
+    __attribute__((aligned(16))) char rows[4 * 64 * Row<HD>::RS];
+    __attribute__((aligned(16))) float stats[2][2][64];
+    __attribute__((aligned(16))) int32_t lab[2][64];
+    int32_t states[2][2];
+};
+
+// D = dO . O of every row and head, hd / 8 lanes to a row.
+template <int DT, int HD>
+__global__ __launch_bounds__(256) void k_relpos_rows(const uint16_t* __restrict__ out, int64_t ldo,
+                                                     const uint16_t* __restrict__ dout, int64_t ldg, int64_t M,
+                                                     int32_t T, int32_t H, float* __restrict__ Dv)
+{
+    using F = typename Elem<DT>::frag;
+    constexpr int CH = HD / 8;
+    // (the lanes of a row leave together)
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i / CH < M * H; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / CH, row = r / H, seq = row / T;
+        const int h = (int)(r - row * H), k = (int)(i % CH) * 8;
+        const F g = *(const F*)(dout + row * ldg + h * HD + k), o = *(const F*)(out + row * ldo + h * HD + k);
+        float v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v = fmaf((float)g[j], (float)o[j], v);
+#pragma unroll
+        for (int d = 1; d < CH; d <<= 1)
+            v += __shfl_xor(v, d, 64);
+        if (k == 0)
+            Dv[(seq * H + h) * T + (row - seq * T)] = v;
+    }
+}
+
 // dQ, tiled as the forward: the weights come back from lse, dP^T = V dO^T, and dS^T,
-// rounded once, is the B operand of dQ^T = K^T dS^T.  D = dO . O is formed first and kept
-// for the next kernel.
+// rounded once, is the B operand of dQ^T = K^T dS^T.
 template <int DT, int HD, typename Sh, bool REG>
-__global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __restrict__ out, int64_t ldo,
-                                                      const float* __restrict__ lse,
-                                                      const uint16_t* __restrict__ dout, int64_t ldg,
-                                                      float* __restrict__ Dv, uint16_t* __restrict__ dqkv,
-                                                      int64_t lddq, float scale, float rroot)
+__device__ inline void grad_q(const Rp& p, const Gp& c, uint32_t id, GradLds<HD>& sh)
 {
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT;
-    __shared__ __attribute__((aligned(16))) char kv[4 * Sh::B * RS];
-    __shared__ __attribute__((aligned(16))) int32_t lab[2][Sh::B];
-    __shared__ int32_t states[2][2];
     static_assert(Sh::B == 64, "a wave stages a block's labels");
+    char* kv = sh.rows;
+    auto& lab = sh.lab;
+    auto& states = sh.states;
+    const int64_t ldg = c.ldg, lddq = c.lddq;
+    const float scale = c.scale, rroot = c.rroot;
     const int T = p.T;
-    const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
-    if (!at.ok)
-        return;
+    const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW, id);
     const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     const uint16_t* base = p.qkv + at.seq * T * ldq + at.h * HD;
@@ -562,27 +605,12 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __re
     const int mine = label_mine<REG>(reg, qc);
     const bool live = busy && mine != NO_LABEL, steps = busy && (!REG || !__all(mine == NO_LABEL));
     F qf[KS], gf[KS];
-    float D = 0.0f;
-    {
-        F of[KS];
-        load_frags<F, HD>(gf, dout + (at.seq * T + qc) * ldg + at.h * HD, half, live);
-        load_frags<F, HD>(of, out + (at.seq * T + qc) * ldo + at.h * HD, half, live);
-        load_frags<F, HD>(qf, base + (int64_t)qc * ldq, half, live);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                D = fmaf((float)gf[ks][j], (float)of[ks][j], D);
-        D = half_add(D);
-    }
+    load_frags<F, HD>(qf, base + (int64_t)qc * ldq, half, live);
+    load_frags<F, HD>(gf, c.dout + (at.seq * T + qc) * ldg + at.h * HD, half, live);
     const int64_t stat = (at.seq * p.H + at.h) * T;
-    float nl = -INFINITY;  // -lse in base 2; a row without pairs: every weight 2^-inf
-    if (busy) {
-        const float v = lse[stat + qc];
-        nl = v == -INFINITY ? -INFINITY : -v * LOG2E;
-        if (half == 0 && part == 0 && q < T)
-            Dv[stat + q] = D;
-    }
+    // (a row without pairs, padding for one, whose D may be anything: every weight 2^-inf)
+    const float v = c.lse[stat + qc], D = v == -INFINITY ? 0.0f : c.Dv[stat + qc];
+    const float nl = v == -INFINITY ? -INFINITY : -v * LOG2E;
     f32x16 dq[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -631,36 +659,31 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dq(Rp p, const uint16_t* __re
             }
         });
     if constexpr (Sh::KS == 2) {
-        static_assert(Sh::QW * ND * 4096 <= (int)sizeof(kv), "the joined rows fit");
+        static_assert(Sh::QW * ND * 4096 <= (int)sizeof(sh.rows), "the joined rows fit");
         if (!join_sums<ND>(kv, dq, wave))
             return;
     }
     if (busy && q < T)
-        store_rows<DT, HD>(dqkv + (at.seq * T + q) * lddq + at.h * HD, dq, rroot, half);
+        store_rows<DT, HD>(c.dqkv + (at.seq * T + q) * lddq + at.h * HD, dq, rroot, half);
 }
 
 // dK and dV: a wave holds a 32-key tile, the queries pass in blocks with their lse and D.
 // S = Q K^T and dP = dO V^T (lane = key) make P and dS the B operands of dV^T = dO^T P and
 // dK^T = Q^T dS as they stand.  The bias tiles are those of the transposed index.
 template <int DT, int HD, typename Sh, bool REG>
-__global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __restrict__ lse,
-                                                       const float* __restrict__ Dv,
-                                                       const uint16_t* __restrict__ dout, int64_t ldg,
-                                                       uint16_t* __restrict__ dqkv, int64_t lddq,
-                                                       float scale, float rroot)
+__device__ inline void grad_kv(const Rp& p, const Gp& c, uint32_t id, GradLds<HD>& sh)
 {
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS, ND = Row<HD>::DT;
-    __shared__ __attribute__((aligned(16))) char qg[4 * Sh::B * RS];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][Sh::B];
-    __shared__ __attribute__((aligned(16))) int32_t lab[2][Sh::B];
-    __shared__ int32_t states[2][2];
-    static_assert(Sh::B == 64, "a wave stages a block's labels");
+    char* qg = sh.rows;
+    auto& stats = sh.stats;
+    auto& lab = sh.lab;
+    auto& states = sh.states;
+    const int64_t ldg = c.ldg, lddq = c.lddq;
+    const float scale = c.scale, rroot = c.rroot;
     const int T = p.T;
-    const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW);
-    if (!at.ok)
-        return;
+    const Place at = place(p, (p.nt + Sh::QW - 1) / Sh::QW, id);
     const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int64_t ldq = p.ldq, hw = (int64_t)p.H * HD;
     const uint16_t* base = p.qkv + at.seq * T * ldq + at.h * HD;
@@ -682,8 +705,8 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
     float sl, sd;
     int32_t lv;
     pass_blocks<HD, Sh, REG>(
-        p, base, ldq, dout + at.seq * T * ldg + at.h * HD, ldg, reg,
-        p.bias + ((int64_t)at.h * p.nt + min(kt, p.nt - 1)) * p.nt * 1024 + lane * 4, steps, part, qg,
+        p, base, ldq, c.dout + at.seq * T * ldg + at.h * HD, ldg, reg,
+        c.bias_t + ((int64_t)at.h * p.nt + min(kt, p.nt - 1)) * p.nt * 1024 + lane * 4, steps, part, qg,
         [&](int blk) {
             // -lse in base 2 (-inf past T and for rows without pairs: every weight 0), D, label
             sl = -INFINITY;
@@ -691,9 +714,9 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
             lv = -1;
             const int r = blk * Sh::B + threadIdx.x;
             if (threadIdx.x < Sh::B && r < T) {
-                const float v = lse[stat + r];
+                const float v = c.lse[stat + r];
                 sl = v == -INFINITY ? -INFINITY : -v * LOG2E;
-                sd = Dv[stat + r];
+                sd = v == -INFINITY ? 0.0f : c.Dv[stat + r];
                 if (REG)
                     lv = max(reg[r], -1);
             }
@@ -750,12 +773,12 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
             }
         });
     if constexpr (Sh::KS == 2) {
-        static_assert(Sh::QW * 2 * ND * 4096 <= (int)sizeof(qg), "the joined rows fit");
+        static_assert(Sh::QW * 2 * ND * 4096 <= (int)sizeof(sh.rows), "the joined rows fit");
         if (!join_sums<2 * ND>(qg, acc, wave))
             return;
     }
     if (busy && k < T) {
-        uint16_t* row = dqkv + (at.seq * T + k) * lddq + at.h * HD;
+        uint16_t* row = c.dqkv + (at.seq * T + k) * lddq + at.h * HD;
         store_rows<DT, HD>(row + hw, acc, rroot, half);
         store_rows<DT, HD>(row + 2 * hw, acc + ND, 1.0f, half);
     }
@@ -765,23 +788,20 @@ __global__ __launch_bounds__(Sh::NT) void k_relpos_dkv(Rp p, const float* __rest
 // four waves (a 32 x 32 tile each, summed in its accumulators' places in float32), the four
 // matrices' rows staged in LDS a sequence ahead.  part: [head][chunk][tile][r / 4][lane][r % 4].
 template <int DT, int HD, bool REG>
-__global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restrict__ lse,
-                                                      const float* __restrict__ Dv,
-                                                      const uint16_t* __restrict__ dout, int64_t ldg,
-                                                      float* __restrict__ part, int32_t chunks,
-                                                      float scale)
+__device__ inline void grad_bias(const Rp& p, const Gp& c, uint32_t id, GradLds<HD>& sh)
 {
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS;
-    __shared__ __attribute__((aligned(16))) char rows[4][64 * RS];  // Q, dO, K, V
+    char(&rows)[4][64 * RS] = *(char(*)[4][64 * RS])sh.rows;  // Q, dO, K, V
+    const int64_t ldg = c.ldg;
+    const int32_t chunks = c.chunks;
+    const float scale = c.scale;
     const int T = p.T, n_blk = (p.nt + 1) / 2;
     // (the blocks of pairs of one head and chunk follow each other: they share the rows)
-    const uint32_t n2 = (uint32_t)(n_blk * n_blk), n = n2 * (uint32_t)(chunks * p.H), id = xcd_order(n);
+    const uint32_t n2 = (uint32_t)(n_blk * n_blk);
     const uint32_t u = id / n2;
     const int ab = (int)(id - u * n2), h = (int)(u / (uint32_t)chunks), chunk = (int)(u - (uint32_t)(h * chunks));
-    if (id >= n)
-        return;
     const int lane = threadIdx.x & 63, wave = wave_id(), l32 = lane & 31, half = lane >> 5;
     const int qb = ab / n_blk, kb = ab - qb * n_blk;
     const int qt = 2 * qb + (wave >> 1), kt = 2 * kb + (wave & 1);
@@ -795,7 +815,7 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
     auto load = [&](int64_t seq) {
         const uint16_t* base = p.qkv + seq * T * ldq + h * HD;
         const int32_t* reg = REG ? labels(p, seq) : nullptr;
-        sq.load(base, ldq, dout + seq * T * ldg + h * HD, ldg, qb * 64, T, reg);
+        sq.load(base, ldq, c.dout + seq * T * ldg + h * HD, ldg, qb * 64, T, reg);
         sk.load(base + hw, ldq, base + 2 * hw, ldq, kb * 64, T, reg);
     };
     f32x16 sum = {};
@@ -809,7 +829,7 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
         sq.store(rows[0], rows[1]);
         sk.store(rows[2], rows[3]);
         const int64_t stat = (seq * p.H + h) * T;
-        const float v = lse[stat + qc], D = Dv[stat + qc];
+        const float v = c.lse[stat + qc], D = v == -INFINITY ? 0.0f : c.Dv[stat + qc];
         // (a query past T: every weight 2^-inf)
         const float nl = v == -INFINITY || q >= T ? -INFINITY : -v * LOG2E;
         __syncthreads();
@@ -839,11 +859,35 @@ __global__ __launch_bounds__(256) void k_relpos_dbias(Rp p, const float* __restr
         __syncthreads();
     }
     if (busy) {
-        float* dst = part + (((int64_t)h * chunks + chunk) * p.nt * p.nt + (int64_t)qt * p.nt + kt) * 1024 +
+        float* dst = c.part + (((int64_t)h * chunks + chunk) * p.nt * p.nt + (int64_t)qt * p.nt + kt) * 1024 +
                      lane * 4;
 #pragma unroll
         for (int g = 0; g < 4; ++g)
             *(float4*)(dst + 256 * g) = float4{sum[4 * g], sum[4 * g + 1], sum[4 * g + 2], sum[4 * g + 3]};
+    }
+}
+
+// All gradients of longer sequences in one launch, so that its parts fill the chip together:
+// workgroups of dQ, then of dK and dV, then of the bias's.
+template <int DT, int HD, typename Sh, bool REG>
+__global__ __launch_bounds__(256, 2) void k_relpos_grad(Rp p, Gp c, uint32_t n_tiles, uint32_t n_pairs)
+{
+    static_assert(Sh::NT == 256, "every part has 256 threads");
+    __shared__ GradLds<HD> sh;
+    // (each part's workgroups in runs per XCD: the counts but the last are multiples of 8)
+    const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x, span = (n_tiles + 7) / 8 * 8;
+    if (id < 2 * span) {
+        const uint32_t i = xcd_order(n_tiles, id % span);
+        if (i >= n_tiles)
+            return;
+        if (id < span)
+            grad_q<DT, HD, Sh, REG>(p, c, i, sh);
+        else
+            grad_kv<DT, HD, Sh, REG>(p, c, i, sh);
+    } else {
+        const uint32_t i = xcd_order(n_pairs, id - 2 * span);
+        if (i < n_pairs)
+            grad_bias<DT, HD, REG>(p, c, i, sh);
     }
 }
 
@@ -1346,7 +1390,7 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
     char* X = kv + 4 * KV;         // [2][P, dS][32 nt][XS]
     int32_t* labs = (int32_t*)(X + 4 * 32 * nt * XS);
     int32_t* states = labs + 32 * nt;
-    const uint32_t units = (uint32_t)p.n_seq * (uint32_t)p.H, wgs = (units + per - 1) / per, wg = xcd_order(wgs);
+    const uint32_t units = (uint32_t)p.n_seq * (uint32_t)p.H, wgs = (units + per - 1) / per, wg = xcd_order(wgs, blockIdx.x);
     if (wg >= wgs)
         return;
     const uint32_t u0 = wg * per, u1 = min(u0 + per, units), seqs = (uint32_t)p.n_seq;
@@ -1707,18 +1751,26 @@ template <int DT, int HD, bool REG> hipError_t forward_as(const lpv_relpos* h, c
                            : forward_tiles<DT, HD, REG, Shape<4, 1>>(h, c, s);
 }
 
-template <int DT, int HD, bool REG, typename Sh>
-hipError_t grad_tiles(const lpv_relpos* h, const RelposCall& c, const Ws& w, hipStream_t s)
+template <int DT, int HD>
+hipError_t launch_row_products(const lpv_relpos* h, const RelposCall& c, float* D, hipStream_t s)
 {
-    const float scale = LOG2E / sqrtf((float)HD), rroot = 1.0f / sqrtf((float)HD);
-    Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
-    const Grid2 g = grid_of(c.n_seq * c.H * ((h->nt + Sh::QW - 1) / Sh::QW));
-    hipLaunchKernelGGL((k_relpos_dq<DT, HD, Sh, REG>), dim3(g.x, g.y), dim3(Sh::NT), 0, s, p,
-                       (const uint16_t*)c.out, c.ldo, c.lse, (const uint16_t*)c.dout, c.ldg, w.D,
-                       (uint16_t*)c.dqkv, c.lddq, scale, rroot);
-    p.bias = w.bias_t;
-    hipLaunchKernelGGL((k_relpos_dkv<DT, HD, Sh, REG>), dim3(g.x, g.y), dim3(Sh::NT), 0, s, p, c.lse, w.D,
-                       (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, scale, rroot);
+    const int64_t n = c.n_seq * h->T * c.H * (HD / 8), wgs = (n + 255) / 256;
+    hipLaunchKernelGGL((k_relpos_rows<DT, HD>), dim3((uint32_t)(wgs < 4096 ? wgs : 4096)), dim3(256), 0, s,
+                       (const uint16_t*)c.out, c.ldo, (const uint16_t*)c.dout, c.ldg, c.n_seq * h->T, h->T, c.H, D);
+    return hipGetLastError();
+}
+
+template <int DT, int HD, bool REG, typename Sh>
+hipError_t grad_tiles(const lpv_relpos* h, const RelposCall& c, const Ws& w, int chunks, hipStream_t s)
+{
+    const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
+    const Gp g = {c.lse, w.D, (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, w.bias_t, w.part, chunks,
+                  LOG2E / sqrtf((float)HD), 1.0f / sqrtf((float)HD)};
+    const int64_t n_tiles = c.n_seq * c.H * ((h->nt + Sh::QW - 1) / Sh::QW), n_blk = (h->nt + 1) / 2;
+    const int64_t n_pairs = (int64_t)c.H * n_blk * n_blk * chunks;
+    const Grid2 grid = grid_of(2 * ((n_tiles + 7) / 8 * 8) + n_pairs);
+    hipLaunchKernelGGL((k_relpos_grad<DT, HD, Sh, REG>), dim3(grid.x, grid.y), dim3(256), 0, s, p, g,
+                       (uint32_t)n_tiles, (uint32_t)n_pairs);
     return hipGetLastError();
 }
 
@@ -1761,13 +1813,10 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
     } else if (chunks > 0) {  // (n_seq > 0)
         e = expand_bias<DT>(h, c.table, c.H, HD, w.bias, w.bias_t, s);
         if (e == hipSuccess)
-            e = few_tiles(h, c) ? grad_tiles<DT, HD, REG, Shape<2, 2>>(h, c, w, s)
-                                : grad_tiles<DT, HD, REG, Shape<4, 1>>(h, c, w, s);
-        const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
-        const int64_t n_blk = (h->nt + 1) / 2;
-        const Grid2 gb = grid_of((int64_t)c.H * n_blk * n_blk * chunks);
-        hipLaunchKernelGGL((k_relpos_dbias<DT, HD, REG>), dim3(gb.x, gb.y), dim3(256), 0, s, p, c.lse, w.D,
-                           (const uint16_t*)c.dout, c.ldg, w.part, chunks, LOG2E / sqrtf((float)HD));
+            e = launch_row_products<DT, HD>(h, c, w.D, s);
+        if (e == hipSuccess)
+            e = few_tiles(h, c) ? grad_tiles<DT, HD, REG, Shape<2, 2>>(h, c, w, chunks, s)
+                                : grad_tiles<DT, HD, REG, Shape<4, 1>>(h, c, w, chunks, s);
     }
     if (e != hipSuccess)
         return e;

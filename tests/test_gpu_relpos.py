@@ -143,7 +143,8 @@ class Case:
 @pytest.mark.parametrize("T,n_seq,H,hd", [
     (1, 1, 1, 32), (1, 70, 3, 64), (2, 5, 2, 32), (31, 3, 2, 64), (32, 3, 1, 32), (33, 2, 3, 32),
     (63, 3, 2, 64), (64, 2, 2, 32), (65, 2, 1, 64), (96, 2, 2, 32), (127, 1, 2, 64),
-    (128, 2, 1, 32), (129, 2, 1, 64), (161, 1, 2, 32), (257, 1, 2, 64)])
+    (128, 2, 1, 32), (129, 2, 1, 64), (161, 1, 2, 32), (223, 2, 1, 64), (224, 1, 2, 32),
+    (225, 1, 2, 32), (257, 1, 2, 64), (290, 2, 1, 32)])
 def test_lengths(T, n_seq, H, hd, dtype):
     say("relpos", dtype, "T=%d n_seq=%d H=%d hd=%d" % (T, n_seq, H, hd))
     Case(*line_index(T, 9), n_seq, H, hd, dtype, seed=120 + T).run()
@@ -157,7 +158,7 @@ def test_windows(side, extra, n_seq, H, hd, dtype):
     Case(*window_index(side, extra), n_seq, H, hd, dtype, seed=130).run()
 
 
-@pytest.mark.parametrize("T,hd", [(49, 32), (49, 64), (20, 32), (100, 64), (197, 32)])
+@pytest.mark.parametrize("T,hd", [(49, 32), (49, 64), (20, 32), (100, 64), (197, 32), (230, 64), (261, 32)])
 def test_labels_and_padding(T, hd):
     """Parts of a window, labels of every sign, sequences padded wholly and in part; padding
     tokens hold NaN and infinities."""
@@ -208,6 +209,43 @@ def test_every_pair_masked():
     c = Case(np.full((40, 40), -1, np.int32), 5, 3, 2, 64, "bf16", seed=151)
     out, lse, dqkv, dtable = c.run()
     assert not out.any() and not dqkv.any() and not dtable.any()
+
+
+@pytest.mark.parametrize("T,n_seq,H", [(100, 5, 3), (197, 90, 3), (70, 1, 1), (145, 257, 2), (240, 7, 2),
+                                       (230, 40, 8)])
+def test_many_sequences_and_heads(T, n_seq, H):
+    """More and fewer sequences than workgroups: whole heads, parts of them, several heads to
+    a workgroup; few and many tiles."""
+    say("relpos sums", T, n_seq, H)
+    idx, n = line_index(T, 7)
+    c = Case(idx, n, 1, H, 32, "bf16", seed=156)
+    # the same sequence n_seq times: dtable is n_seq times one's, dqkv repeats
+    one_out, one_lse = c.forward()
+    dq1, dt1 = c.grad(one_out, one_lse)
+    rep = lambda t: t.repeat(n_seq, 1)
+    qkv, dout = rep(c.qkv), rep(c.dout)
+    lse = torch.empty((n_seq, H, T), device="cuda")
+    out = lpv.relpos_attention(c.rp, c.table, qkv, n_seq, H, lse=lse, hd=32)
+    dq, dt = lpv.relpos_attention_grad(c.rp, c.table, qkv, out, lse, dout, n_seq, H, hd=32)
+    torch.cuda.synchronize()
+    # (the kernels differ by the number of sequences, and with them the orders of sums: their
+    # float32 differences, and the half steps that two roundings of nearly the same may differ by)
+    for a, b in ((out, rep(one_out)), (dq, rep(dq1))):
+        a, b = a.float(), b.float()
+        assert float((a - b).abs().max()) <= 2 * U["bf16"] * float(b.abs().max())
+    want = dt1.double() * n_seq
+    err = (dt.double() - want).abs()
+    # dt1 and dt are rounded once each, and dS is summed in float32, 2^-24 a term of at most
+    # T^2 n_seq.  The gradients take D from the outputs as they were rounded: either's is off by
+    # at most u (P |V| + |O|) <= 2.1 u P |V|, so the two D by twice the sum of |dO| times that,
+    # in every sequence alike, which dS_ij takes P_ij times
+    r = ft.relpos_attention(c.x, c.t, idx, 1, H, 32, dout=c.g)
+    e_D = 2 * 2.1 * U["bf16"] * (np.abs(c.g) * r["abs_pv"]).reshape(T, H, 32).sum(2)
+    e_t = np.zeros((n, H))
+    for h in range(H):
+        np.add.at(e_t[:, h], idx, r["P"][0, h] * e_D[:, h][:, None])
+    bound = 2 * U["bf16"] * want.abs() + 2 ** -16 * T * n_seq + torch.from_numpy(n_seq * e_t).cuda()
+    assert bool((err <= bound).all())
 
 
 @pytest.mark.parametrize("T", [49, 100])
