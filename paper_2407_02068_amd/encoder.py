@@ -14,6 +14,8 @@ this chains the standard pre-norm block around them:
                 P   = Hd Wfc2~^T + b
                 x   = x + P;  A = LN(x)      (the next block's first LN)
 
+With a position bias (one table of buckets per block) the attention is the
+position-biased one, in windows or over regions of tokens if labels are given.
 Every layer norm uses the same gamma / beta.  The residual stream alternates
 between two buffers, so a run never overwrites its own input and every run
 computes the same function of ``x0``.
@@ -46,11 +48,20 @@ class EncoderChain:
     """``blocks`` DeiT encoder blocks over M = n_seq * T tokens of width D.
 
     linears: 4 * blocks Linear objects in the order (qkv, proj, fc1, fc2) per
-    block; gamma, beta: the layer norms' D-element parameters."""
+    block; gamma, beta: the layer norms' D-element parameters.  relpos (a
+    lpv.RelPos of T tokens) with tables (one n_buckets x H table per block):
+    attention with that position bias; region: its labels, as
+    lpv.relpos_attention takes them."""
 
-    def __init__(self, linears, n_seq, T, H, gamma, beta, eps=1e-6):
+    def __init__(self, linears, n_seq, T, H, gamma, beta, eps=1e-6, relpos=None, tables=None,
+                 region=None):
         if len(linears) % 4:
             raise ValueError("four linear layers per block")
+        if relpos is None and (tables is not None or region is not None):
+            raise ValueError("tables and region need relpos")
+        if relpos is not None and (relpos.T != T or tables is None
+                                   or len(tables) * 4 != len(linears)):
+            raise ValueError("relpos of T tokens, with one table per block")
         self.linears, self.n_seq, self.T, self.H = linears, n_seq, T, H
         self.gamma, self.beta, self.eps = gamma, beta, eps
         D = linears[0].W.shape[1]
@@ -61,6 +72,11 @@ class EncoderChain:
         self.A, self.O, self.P = new(D), new(D), new(D)
         self.qkv, self.Hd = new(linears[0].W.shape[0]), new(linears[2].W.shape[0])
         self.R = [new(D), new(D)]
+        self.relpos, self.tables, self.region = relpos, tables, region
+        self.relpos_ws = None
+        if relpos is not None:
+            self.relpos_ws = torch.empty(lpv.relpos_workspace_size(relpos, n_seq, H),
+                                         dtype=torch.uint8, device=dv)
 
     @property
     def blocks(self):
@@ -96,7 +112,11 @@ class EncoderChain:
         for blk in range(self.blocks):
             q, pr, f1, f2 = self.linears[4 * blk:4 * blk + 4]
             lin(q, A, qkv)
-            lpv.attention(qkv, self.n_seq, self.T, self.H, out=O)
+            if self.relpos is None:
+                lpv.attention(qkv, self.n_seq, self.T, self.H, out=O)
+            else:
+                lpv.relpos_attention(self.relpos, self.tables[blk], qkv, self.n_seq, self.H,
+                                     region=self.region, out=O, workspace=self.relpos_ws)
             if trace:
                 trace("%d.attention" % blk, {"qkv": qkv}, O)
             lin(pr, O, P)
@@ -115,7 +135,7 @@ class EncoderChain:
     def capture(self, x0, sparse=True):
         """The forward pass from x0 captured once into a HIP graph (through
         torch.cuda.CUDAGraph): replaying it relaunches the same 1 + 6 * blocks
-        kernels on the same buffers with no host work per launch.  Every call
+        calls' kernels on the same buffers with no host work per launch.  Every call
         of the chain is capturable (no allocation, no host synchronisation, no
         memset); one eager pass first settles the kernels' one-time set-up.
         Returns (graph, (x, A)): the outputs the replays rewrite."""
@@ -132,14 +152,16 @@ class EncoderChain:
             layer.close()
 
 
-def deit_chain(layers, to_dev, n_seq, T=197, H=12, eps=1e-6):
+def deit_chain(layers, to_dev, n_seq, T=197, H=12, eps=1e-6, relpos=None, tables=None,
+               region=None):
     """An EncoderChain from generated layer inputs (objects with W, mask, bias,
     b_r, b_c, gelu, name as numpy arrays; ``to_dev`` moves an array of the
-    element type to the GPU).  Layer norms: gamma = 1, beta = 0."""
+    element type to the GPU).  Layer norms: gamma = 1, beta = 0.
+    relpos, tables, region: as EncoderChain takes them."""
     lins = [Linear(w.name, to_dev(w.W), torch.from_numpy(w.mask).cuda(), to_dev(w.bias),
                    w.b_r, w.b_c, w.gelu) for w in layers]
     D = lins[0].W.shape[1]
     dt = lins[0].W.dtype
     gamma = torch.ones(D, dtype=dt, device="cuda")
     beta = torch.zeros(D, dtype=dt, device="cuda")
-    return EncoderChain(lins, n_seq, T, H, gamma, beta, eps)
+    return EncoderChain(lins, n_seq, T, H, gamma, beta, eps, relpos, tables, region)

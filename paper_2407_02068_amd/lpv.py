@@ -7,6 +7,7 @@ ctypes and turns status codes into exceptions.  There is no fallback: without
 the built library every call raises.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -615,6 +616,7 @@ def relpos_attention_grad(rp, table, qkv, out, lse, dout, n_seq, H, region=None,
     return dqkv, dtable
 
 
+@functools.lru_cache(maxsize=256)
 def distill_workspace_size(M, V, k, dtype):
     """lpv_distill_workspace_size: bytes of the workspace of ``distill_loss`` and
     ``distill_grad``."""
@@ -644,10 +646,13 @@ def _distill(logits, ids, teacher, temperature, dloss, loss, dlogits, Vd, worksp
     _on_current(("logits", logits), ("ids", ids), ("teacher", teacher), ("dloss", dloss),
                 ("loss", loss), ("dlogits", dlogits), ("workspace", workspace))
     zp, ldz = _rows(logits, "logits", M, V, logits.dtype)
-    dp, ldd = _rows(dlogits, "dlogits", M, V, logits.dtype) if dlogits is not None else (None, 0)
+    if dlogits is not None:  # (the columns behind the classes, up to Vd, are its padding)
+        dp, ldd = _rows(dlogits, "dlogits", M, dlogits.shape[-1], logits.dtype)
+    else:
+        dp, ldd = None, 0
     if M == 1:  # (one row's stride says nothing: any that covers it)
         pad = 16 // logits.element_size()
-        ldz, ldd = (V + pad - 1) // pad * pad, (max(V, Vd) + pad - 1) // pad * pad
+        ldz = ldd = (max(V, Vd) + pad - 1) // pad * pad
     wp, nbytes, keep = _workspace(workspace, distill_workspace_size(M, V, k, logits.dtype), logits.device,
                                   stream)
     _check(lib().lpv_distill(zp, ldz, M, V, DTYPES[logits.dtype], ids.data_ptr(), teacher.data_ptr(), ldt, k,
@@ -667,9 +672,14 @@ def distill_grad(logits, ids, teacher, temperature, dloss=None, loss=None, dlogi
                  workspace=None, stream=None):
     """lpv_distill: (loss, dlogits), for the gradient ``dloss`` at each row's loss (M float32;
     None: 1).  dlogits is allocated in rows padded to 16 columns, the padding zero, as the
-    linear calls take it; it may be given, and may be the logits themselves."""
-    Vd = logits.shape[1]
-    if dlogits is None:
+    linear calls take it; it may be given, M x V or wider (the columns past V are zeroed),
+    and may be the logits themselves."""
+    V = Vd = logits.shape[1]
+    if dlogits is not None:
+        if not isinstance(dlogits, torch.Tensor) or dlogits.dim() != 2 or dlogits.shape[1] < V:
+            raise ValueError("dlogits must be a 2-D tensor with a column for each of the %d classes" % V)
+        Vd = dlogits.shape[1]
+    else:
         Vd = (Vd + 15) // 16 * 16
         wide = torch.empty((logits.shape[0], Vd), dtype=logits.dtype, device=logits.device)
         dlogits = wide[:, :logits.shape[1]]

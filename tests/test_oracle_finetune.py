@@ -100,3 +100,31 @@ def test_distill_gradient_against_differences():
         dz = r.normal(size=z.shape)
         f = lambda h: (ft.distill(z + h * dz, ids, t, 3.0) * g).sum()
         assert abs((f(1e-5) - f(-1e-5)) / 2e-5 - (d * dz).sum()) < 1e-8
+
+
+def test_gradients_of_the_step_against_differences():
+    """The operators behind each other: the loss's central differences in directions of the
+    table and of qkv against the oracle's gradients."""
+    r = np.random.default_rng(5)
+    idx, nb = np.clip(np.arange(9)[None, :] - np.arange(9)[:, None] + 3, 0, 5), 6
+    H, hd, V, n_seq = 2, 4, 11, 2
+    x, t = r.normal(0, 1, (n_seq * 9, 3 * H * hd)), r.normal(0, 0.5, (nb, H))
+    W = r.normal(0, 0.4, (V, H * hd))
+    ids = np.stack([r.permutation(V)[:3] for _ in range(n_seq * 9)])
+    top = r.normal(0, 2, ids.shape)
+    g = np.ones(n_seq * 9)
+
+    def loss(x, t):
+        out = ft.relpos_attention(x, t, idx, n_seq, H, hd)["out"]
+        return ft.distill(out @ W.T, ids, top, 2.0).sum()
+    out = ft.relpos_attention(x, t, idx, n_seq, H, hd)["out"]
+    dz = ft.distill(out @ W.T, ids, top, 2.0, g)[1]
+    grads = ft.relpos_attention(x, t, idx, n_seq, H, hd, dout=dz @ W)
+    eps = 1e-5
+    for _ in range(4):
+        ux, ut = r.normal(0, 1, x.shape), r.normal(0, 1, t.shape)
+        diff = (loss(x + eps * ux, t + eps * ut) - loss(x - eps * ux, t - eps * ut)) / (2 * eps)
+        exact = (grads["dqkv"] * ux).sum() + (grads["dtable"] * ut).sum()
+        # the third derivative's term, eps^2 of values of order 10, and the loss's own 2^-53
+        # over eps
+        assert abs(diff - exact) <= 1e-7 * max(1.0, abs(exact)) + 1e-8
