@@ -90,6 +90,7 @@ __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, 
 // workgroup takes a head and `per` tiles; a head's column of the table is made ready in
 // LDS once, where its gathers cost no more than reads of consecutive values do (the lanes of
 // a tile's row differ by a constant in most indexes); larger tables are gathered in memory.
+// (Forward of 8 x 1024 tokens, 12 heads, 2000 buckets: 61 us, 71 gathered; 11000: 84 and 88.)
 constexpr int BIAS_LDS = 12288;  // buckets
 
 template <int DT>
@@ -290,7 +291,8 @@ template <int QW_, int KS_> struct Shape {
 };
 
 // Workgroups of a launch in an order in which each XCD (workgroup L runs on XCD L % 8) takes
-// one run of neighbours, which find each other's rows and bias in its L2.
+// one run of neighbours, which find each other's rows and bias in its L2.  (8 x 1000 tokens,
+// 12 heads of 64: forward 59 us, 80 in the launch's order; gradients 230 and 247.)
 __device__ inline uint32_t xcd_order(uint32_t n, uint32_t id)
 {
     const uint32_t per = n / 8, rest = n % 8, x = id % 8;
@@ -299,7 +301,8 @@ __device__ inline uint32_t xcd_order(uint32_t n, uint32_t id)
 
 // Workgroup -> (sequence, head, block of row tiles).  A head's blocks of a sequence follow
 // each other while its bias is small (they share K and V); else the sequences of a block do
-// (they share its bias: 4 KB a pair of tiles).
+// (they share its bias: 4 KB a pair of tiles).  Gradients of 64 x 300 tokens, 12 heads:
+// 196 us the first way, 205 the second; of 4 x 2000 tokens 650 and 633; 8 x 1000: the same.
 constexpr int BIAS_SMALL = 256;  // tiles of a head's bias: 1 MB
 struct Place {
     int64_t seq;
@@ -894,6 +897,8 @@ __global__ __launch_bounds__(256, 2) void k_relpos_grad(Rp p, Gp c, uint32_t n_t
 // The chunks' sums of each pair: CL threads of a workgroup share a pair's chunks (each in
 // order, then the threads'), 4 pairs to a thread.  per > 0: of a head's slots, those that
 // k_relpos_mid_grad's workgroups have filled, which take `per` of all heads' sequences each.
+// CL = 16 from 16 chunks on: gradients of 64 x 100 tokens, 2 heads (65 chunks) 26 us, with
+// CL = 1 39; of 64 x 300 tokens, 12 heads (4 chunks) 202 and 197.
 template <int CL>
 __global__ __launch_bounds__(256) void k_relpos_fold(const float* __restrict__ part, int32_t slots,
                                                      uint32_t n_seq, uint32_t per, int64_t n_pos,
@@ -1366,9 +1371,10 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // formed once, with five products, where the general kernels form it three times with nine.
 // LDS holds all rows of Q and dO, two key tiles and the two buffers.  Bound: LDS reads and
 // the chain of a tile at two waves to a SIMD (the sums leave registers for no more).
+constexpr int MID_TILES = 7;  // with the wave more two waves to a SIMD, which the sums' registers allow
 constexpr int MID_XS = 72;  // bytes of a row of P or dS, 32 keys: the writes of 32 rows' 8 bytes meet all banks
-template <int DT, int HD, int NT, bool REG>
-__global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
+template <int DT, int HD, bool REG>
+__global__ __launch_bounds__(64 * (MID_TILES + 1)) void k_relpos_mid_grad(
     Rp p, const uint16_t* __restrict__ out, int64_t ldo, const float* __restrict__ lse,
     const uint16_t* __restrict__ dout, int64_t ldg, uint16_t* __restrict__ dqkv, int64_t lddq,
     float* __restrict__ part, int32_t per, int32_t slots, float scale, float rroot)
@@ -1467,9 +1473,9 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
     for (uint32_t unit = u0; unit < u1;) {  // a head
         const uint32_t h = unit / seqs, end = min(u1, (h + 1) * seqs);
         float* slot = part + (((int64_t)h * slots + (wg - h * seqs / per)) * nt + wave) * nt * 1024 + lane * 4;
-        f32x16 sum[NT];
+        f32x16 sum[MID_TILES];
 #pragma unroll
-        for (int b = 0; b < NT; ++b)
+        for (int b = 0; b < MID_TILES; ++b)
             sum[b] = f32x16{};
         for (; unit < end; ++unit) {
             const int64_t seq = unit - h * seqs;
@@ -1571,7 +1577,7 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
             for (int d = 0; d < ND; ++d)
                 dq[d] = f32x16{};
 #pragma unroll
-            for (int sk = 0; sk < NT; ++sk) {
+            for (int sk = 0; sk < MID_TILES; ++sk) {
                 if (sk >= nt)
                     break;
                 int kt = sk;  // (as no constant, for the same reason)
@@ -1635,9 +1641,8 @@ __global__ __launch_bounds__(64 * (NT + 1)) void k_relpos_mid_grad(
 constexpr int WINDOW_TILES = 2;  // tiles of 32 tokens that the window kernels take
 bool is_window(const lpv_relpos* h) { return h->nt <= WINDOW_TILES; }
 
-// The longest sequences of k_relpos_mid_grad, in tiles: with the wave more, two waves to a
-// SIMD, which their sums' registers allow.
-constexpr int MID_TILES = 7;
+// Against the general kernels (us of both passes' calls): 64 sequences of 197 tokens, 12 heads
+// of 64, 89 / 123; 224 tokens, heads of 32, 71 / 89; 66 tokens 32 / 39; 8 sequences 41 / 44.
 bool is_mid(const lpv_relpos* h) { return !is_window(h) && h->nt <= MID_TILES; }
 size_t mid_lds_bytes(int nt, int hd)
 {
@@ -1703,7 +1708,14 @@ hipError_t expand_bias(const lpv_relpos* h, const void* table, int32_t H, int32_
 }
 
 // The general kernels' layout: a wave to a 32-row tile, four tiles to a workgroup; where
-// that leaves the chip with fewer than two waves to a SIMD, two waves to a tile.
+// that leaves the chip with few waves, two waves to a tile: `few` below six tiles to a
+// compute unit in the forward pass, below two in the gradients, whose other parts fill the
+// chip.  (us of the call, two waves / one, 600 tokens, 8 heads of 64: forward 20.6 / 23.8 with
+// 304 tiles, 27.5 / 28.5 with 1216, 37.4 / 36.7 with 1976; gradients 49.7 / 51.1 with 304,
+// 62.0 / 57.1 with 608, 122 / 108 with 1976.  Four waves to a tile: 777 tokens, 4 sequences,
+// 8 heads, the forward kernel 26.8 against 19.8.)
+bool few_tiles(const lpv_relpos* h, const RelposCall& c, int64_t few) { return c.n_seq * c.H * h->nt < few; }
+
 template <int DT, int HD, bool REG, typename Sh>
 hipError_t forward_tiles(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
 {
@@ -1714,8 +1726,6 @@ hipError_t forward_tiles(const lpv_relpos* h, const RelposCall& c, hipStream_t s
                        (uint16_t*)c.out, c.ldo, c.lse, LOG2E / sqrtf((float)HD));
     return hipGetLastError();
 }
-
-bool few_tiles(const lpv_relpos* h, const RelposCall& c) { return c.n_seq * c.H * h->nt < 2048; }
 
 // Workgroups of four windows: at most two (32 dimensions) or one to a compute unit at once.
 template <int DT, int HD, bool REG, int NT>
@@ -1747,8 +1757,8 @@ template <int DT, int HD, bool REG> hipError_t forward_as(const lpv_relpos* h, c
     const hipError_t e = expand_bias<DT>(h, c.table, c.H, HD, (float*)c.ws, nullptr, s);
     if (e != hipSuccess)
         return e;
-    return few_tiles(h, c) ? forward_tiles<DT, HD, REG, Shape<2, 2>>(h, c, s)
-                           : forward_tiles<DT, HD, REG, Shape<4, 1>>(h, c, s);
+    return few_tiles(h, c, 1536) ? forward_tiles<DT, HD, REG, Shape<2, 2>>(h, c, s)
+                                 : forward_tiles<DT, HD, REG, Shape<4, 1>>(h, c, s);
 }
 
 template <int DT, int HD>
@@ -1774,21 +1784,23 @@ hipError_t grad_tiles(const lpv_relpos* h, const RelposCall& c, const Ws& w, int
     return hipGetLastError();
 }
 
-template <int DT, int HD, bool REG, int NT>
+template <int DT, int HD, bool REG>
 hipError_t grad_mid(const lpv_relpos* h, const RelposCall& c, const Ws& w, int chunks, hipStream_t s)
 {
-    static bool allowed = false;  // (idempotent: a race between threads is harmless)
-    if (!allowed) {
-        const hipError_t e = hipFuncSetAttribute((const void*)k_relpos_mid_grad<DT, HD, NT, REG>,
+    // LDS beyond 64 KB is allowed per kernel and device (idempotent: a race is harmless)
+    static bool allowed[64] = {};
+    if (h->device >= 64 || !allowed[h->device]) {
+        const hipError_t e = hipFuncSetAttribute((const void*)k_relpos_mid_grad<DT, HD, REG>,
                                                  hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)mid_lds_bytes(NT, HD));
+                                                 (int)mid_lds_bytes(MID_TILES, HD));
         if (e != hipSuccess)
             return e;
-        allowed = true;
+        if (h->device < 64)
+            allowed[h->device] = true;
     }
     const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
     const int32_t per = mid_per(c.n_seq, c.H);
-    hipLaunchKernelGGL((k_relpos_mid_grad<DT, HD, NT, REG>), dim3((uint32_t)((c.n_seq * c.H + per - 1) / per)),
+    hipLaunchKernelGGL((k_relpos_mid_grad<DT, HD, REG>), dim3((uint32_t)((c.n_seq * c.H + per - 1) / per)),
                        dim3(64 * (h->nt + 1)), mid_lds_bytes(h->nt, HD), s, p, (const uint16_t*)c.out, c.ldo, c.lse,
                        (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, w.part, per, chunks,
                        LOG2E / sqrtf((float)HD), 1.0f / sqrtf((float)HD));
@@ -1808,15 +1820,14 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
     } else if (chunks > 0 && is_mid(h)) {
         e = expand_bias<DT>(h, c.table, c.H, HD, w.bias, nullptr, s);
         if (e == hipSuccess)
-            e = h->nt <= 5 ? grad_mid<DT, HD, REG, 5>(h, c, w, chunks, s)
-                           : grad_mid<DT, HD, REG, MID_TILES>(h, c, w, chunks, s);
+            e = grad_mid<DT, HD, REG>(h, c, w, chunks, s);
     } else if (chunks > 0) {  // (n_seq > 0)
         e = expand_bias<DT>(h, c.table, c.H, HD, w.bias, w.bias_t, s);
         if (e == hipSuccess)
             e = launch_row_products<DT, HD>(h, c, w.D, s);
         if (e == hipSuccess)
-            e = few_tiles(h, c) ? grad_tiles<DT, HD, REG, Shape<2, 2>>(h, c, w, chunks, s)
-                                : grad_tiles<DT, HD, REG, Shape<4, 1>>(h, c, w, chunks, s);
+            e = few_tiles(h, c, 512) ? grad_tiles<DT, HD, REG, Shape<2, 2>>(h, c, w, chunks, s)
+                                     : grad_tiles<DT, HD, REG, Shape<4, 1>>(h, c, w, chunks, s);
     }
     if (e != hipSuccess)
         return e;

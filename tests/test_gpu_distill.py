@@ -130,7 +130,8 @@ def test_each_kernel_is_reached():
                                  (128, 40000, 4, "f16", "k_distill_row<1, 512, 12>"),
                                  (128, 100000, 4, "bf16", "k_distill_row<2, 1024, 16>"),
                                  (128, 65540, 4, "f32", "k_distill_join<0>"),
-                                 (127, 16400, 4, "bf16", "k_distill_join<2>")):
+                                 (127, 65545, 4, "bf16", "k_distill_join<2>"),
+                                 (127, 65536, 4, "bf16", "k_distill_row<2, 512, 16>")):
         assert want in names(M, V, k, dtype)
 
 
@@ -274,3 +275,58 @@ def test_refusals_of_the_binding():
         lpv.distill_loss(c.logits, ids, t, 0.0)
     with pytest.raises(lpv.LpvError):
         lpv.distill_loss(c.logits, ids, t, float("nan"))
+
+
+@pytest.mark.parametrize("M,V,k,dtype", [(2, 2 ** 22, 64, "bf16"), (1, 2 ** 22 - 5, 1000, "f16")])
+def test_the_widest_rows(M, V, k, dtype):
+    say("distill", dtype, "M=%d V=%d k=%d" % (M, V, k))
+    Case(M, V, k, dtype, seed=180).run()
+
+
+def test_rows_past_32_bits():
+    """Rows at the largest stride: the last lie over 2^31 elements behind the first."""
+    M, V, ld = 600, 1003, 2 ** 22
+    c = Case(M, V, 9, "bf16", seed=181, ragged=True)
+    loss, d = lpv.distill_grad(c.logits, *c.dev, c.tau, c.dloss)
+
+    def wide():
+        return torch.empty(M * ld, dtype=torch.bfloat16, device="cuda").as_strided((M, 1008), (ld, 1))
+    assert (M - 1) * ld > 2 ** 31
+    z, dz = wide(), wide()
+    z[:, :V] = c.logits
+    got, same = lpv.distill_grad(z[:, :V], *c.dev, c.tau, c.dloss, dlogits=dz)
+    torch.cuda.synchronize()
+    assert same is dz and torch.equal(got, loss) and torch.equal(dz[:, :V], d) and not dz[:, V:].any()
+
+
+@pytest.mark.parametrize("M", [1, 3])
+def test_gradient_with_padding_columns(M):
+    """dlogits wider than the classes: its padding is cleared; in place too."""
+    c = Case(M, 1003, 9, "bf16", seed=182)
+    loss, d = lpv.distill_grad(c.logits, *c.dev, c.tau, c.dloss)
+    wide = torch.full((M, 1024), 5.0, dtype=torch.bfloat16, device="cuda")
+    lpv.distill_grad(c.logits, *c.dev, c.tau, c.dloss, dlogits=wide[:, :1016])
+    torch.cuda.synchronize()
+    assert torch.equal(wide[:, :1003], d) and not wide[:, 1003:1016].any() and (wide[:, 1016:] == 5).all()
+    wide[:, :1003] = c.logits
+    lpv.distill_grad(wide[:, :1003], *c.dev, c.tau, c.dloss, dlogits=wide)
+    torch.cuda.synchronize()
+    assert torch.equal(wide[:, :1003], d) and not wide[:, 1003:].any()
+    for bad in (wide[:, :1000], wide[0], 3):
+        with pytest.raises(ValueError):
+            lpv.distill_grad(c.logits, *c.dev, c.tau, c.dloss, dlogits=bad)
+
+
+def test_two_streams():
+    cases = [Case(6, 131101, 30, "bf16", seed=183), Case(6, 131101, 30, "bf16", seed=184)]
+    ref = [lpv.distill_grad(c.logits, *c.dev, c.tau, c.dloss) for c in cases]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [[], []]
+    for _ in range(4):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(lpv.distill_grad(c.logits, *c.dev, c.tau, c.dloss))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for r in got[i]:
+            assert torch.equal(r[0], ref[i][0]) and torch.equal(r[1], ref[i][1])

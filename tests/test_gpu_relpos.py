@@ -380,3 +380,108 @@ def test_refusals_of_the_binding():
         c.grad(out, lse, dqkv=c.qkv)
     with pytest.raises(lpv.LpvError):
         c.grad(out, lse, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+def test_each_kernel_is_reached():
+    """The rules' sides: windows up to 64 tokens, scores in one pass up to 224, one or two waves
+    to a tile behind that, the sequences' sums folded by 1 or 16 threads."""
+    def names(T, n_seq, H):
+        c = Case(*line_index(T, 9), 1, H, 32, "bf16", seed=157)
+        qkv, dout = c.qkv.repeat(n_seq, 1), c.dout.repeat(n_seq, 1)
+        lse = torch.empty((n_seq, H, T), device="cuda")
+        res = []
+
+        def calls():
+            res.append(lpv.relpos_attention(c.rp, c.table, qkv, n_seq, H, lse=lse, hd=32))
+            lpv.relpos_attention_grad(c.rp, c.table, qkv, res[-1], lse, dout, n_seq, H, hd=32)
+        return {n.replace("lpv::(anonymous namespace)::", "").replace(" ", "") for n in kernels(calls, args=True)}
+    one, two = "Shape<4,1>", "Shape<2,2>"
+    for T, n_seq, H, there, absent in (
+            (32, 40, 2, ("window_fwd<2,32,1", "window_grad<2,32,1", "fold<16>"), ("bias", "rows")),
+            (64, 3, 2, ("window_fwd<2,32,2", "window_grad<2,32,2", "fold<1>"), ("bias", "mid_grad")),
+            (65, 3, 2, ("k_relpos_fwd<2,32", two, "mid_grad", "bias"), ("window", "rows")),
+            (224, 70, 4, ("k_relpos_fwd<2,32", one, "mid_grad"), ("window", "k_relpos_grad")),
+            (225, 2, 2, ("k_relpos_grad<2,32", two, "k_relpos_rows"), (one, "mid_grad")),
+            (225, 16, 4, ("k_relpos_grad<2,32", one, two, "k_relpos_rows"), ("mid_grad",))):
+        got = names(T, n_seq, H)
+        for n in there:
+            assert any(n in g for g in got), (T, n, got)
+        for n in absent:
+            assert not any(n in g for g in got), (T, n, got)
+
+
+@pytest.mark.parametrize("T,n_seq,H,labels", [(230, 20, 4, True), (230, 20, 4, False), (225, 37, 2, True)])
+def test_labels_with_many_tiles(T, n_seq, H, labels):
+    """One wave to a tile in the general gradients, with and without labels."""
+    region = None
+    if labels:
+        region = np.random.default_rng(T).integers(0, 2, (5, T))
+        region[1, T // 2:] = -1
+        region[4] = -1
+        region[3] = 8
+    Case(*line_index(T, 12), n_seq, H, 32, "bf16", region=region, seed=158).run()
+
+
+@pytest.mark.parametrize("T,n_buckets", [(60, 20000), (130, 20000), (130, 12288), (130, 12289), (240, 65535)])
+def test_many_buckets(T, n_buckets):
+    """Tables around and past the size whose column LDS holds; most buckets without a pair."""
+    idx = np.random.default_rng(T).integers(-1, n_buckets, (T, T)).astype(np.int32)
+    idx[5, 5] = n_buckets - 1
+    c = Case(idx, n_buckets, 2, 2, 32, "bf16", seed=159)
+    dtable = c.run()[3]
+    unused = np.ones(n_buckets, bool)
+    unused[idx[idx >= 0]] = False
+    assert not dtable[torch.from_numpy(unused).cuda()].any()
+
+
+def test_longest_sequence():
+    say("relpos T=2048")
+    Case(*line_index(2048, 64), 1, 1, 32, "bf16", seed=160).run()
+
+
+@pytest.mark.parametrize("T,n_seq", [(49, 12), (100, 6), (260, 3)])
+def test_rows_past_32_bits(T, n_seq):
+    """Rows at the largest stride, so that the last lie over 2^31 elements behind the first:
+    the same bits as packed."""
+    say("relpos strides", T, n_seq)
+    c = Case(*line_index(T, 9), n_seq, 2, 32, "bf16", seed=161)
+    ref = c.forward()
+    ref += c.grad(*ref)
+    M, ld = n_seq * T, 2 ** 22
+
+    def wide(t):
+        w = torch.empty(M * ld, dtype=torch.bfloat16, device="cuda").as_strided((M, t.shape[1]), (ld, 1))
+        return w.copy_(t)
+    assert (M - 1) * ld > 2 ** 31
+    out = wide(torch.zeros_like(ref[0]))
+    lse = torch.empty_like(ref[1])
+    qkv, dqkv = wide(c.qkv), wide(torch.zeros_like(c.qkv))
+    lpv.relpos_attention(c.rp, c.table, qkv, n_seq, 2, out=out, lse=lse, hd=32)
+    dout = wide(c.dout)
+    dtable = lpv.relpos_attention_grad(c.rp, c.table, qkv, out, lse, dout, n_seq, 2, dqkv=dqkv, hd=32)[1]
+    torch.cuda.synchronize()
+    for a, b in ((out, ref[0]), (lse, ref[1]), (dqkv, ref[2]), (dtable, ref[3])):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", [49, 130, 230])
+def test_two_streams_share_a_handle(T):
+    """Calls at once on two streams, each with its own workspace."""
+    a = Case(*line_index(T, 9), 30, 3, 32, "bf16", seed=162)
+    b = Case(*line_index(T, 9), 30, 3, 32, "bf16", seed=163)
+    b.rp = a.rp
+    ref = [c.forward() for c in (a, b)]
+    ref = [r + c.grad(*r) for c, r in zip((a, b), ref)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(4):
+        for i, c in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                r = c.forward()
+                got[i].append(r + c.grad(*r))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for r in got[i]:
+            for x, y in zip(r, ref[i]):
+                assert torch.equal(x, y)
