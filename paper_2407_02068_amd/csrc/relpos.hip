@@ -91,6 +91,9 @@ __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, 
 // LDS once, where its gathers cost no more than reads of consecutive values do (the lanes of
 // a tile's row differ by a constant in most indexes); larger tables are gathered in memory.
 // (Forward of 8 x 1024 tokens, 12 heads, 2000 buckets: 61 us, 71 gathered; 11000: 84 and 88.)
+// Bound: writes.  1025 tokens, 12 heads (52 MB): 18 us, 2.9 TB/s; more tiles or threads to a
+// workgroup, or the next tile's buckets asked for ahead, gained there what they lost on
+// smaller ones.
 constexpr int BIAS_LDS = 12288;  // buckets
 
 template <int DT>
@@ -381,6 +384,11 @@ __device__ inline void pass_blocks(const Rp& p, const uint16_t* a, int64_t lda, 
 // of O^T = V^T P^T (V^T by transposing LDS reads).  The row's sum adds the weights before
 // that rounding, so that lse is exact to float32; each lane adds its own, the two of a row
 // meet at the end.  With KS = 2 two waves share a tile's keys and join their rows in LDS.
+// Bound: waits between a tile's dependent steps at three waves to a SIMD (the softmax's vector
+// instructions take 37% of a SIMD's time, the matrix cores 14%).  64 x 197 tokens, 12 heads
+// of 64: 28 us, 272 TFLOP/s; 8 x 1025, fp16, padded: 62 us, 417 TFLOP/s.  Four waves to a
+// SIMD, at 128 registers, gained nothing (28.9 and 68), nor did five to a workgroup where
+// fewer would be idle (64 x 144 tokens, 12 heads of 64: 26.0 against 24.0).
 template <int DT, int HD, typename Sh, bool REG>
 __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, uint16_t* __restrict__ out, int64_t ldo,
                                                        float* __restrict__ lse, float scale)
@@ -557,7 +565,8 @@ template <int HD> struct GradLds {
     int32_t states[2][2];
 };
 
-// D = dO . O of every row and head, hd / 8 lanes to a row.
+// D = dO . O of every row and head, hd / 8 lanes to a row.  Bound: its launch (4 x 777 tokens,
+// 8 heads of 64, 6 MB: 4 us).
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_relpos_rows(const uint16_t* __restrict__ out, int64_t ldo,
                                                      const uint16_t* __restrict__ dout, int64_t ldg, int64_t M,
@@ -871,7 +880,10 @@ __device__ inline void grad_bias(const Rp& p, const Gp& c, uint32_t id, GradLds<
 }
 
 // All gradients of longer sequences in one launch, so that its parts fill the chip together:
-// workgroups of dQ, then of dK and dV, then of the bias's.
+// workgroups of dQ, then of dK and dV, then of the bias's.  Nine products of T^2 hd in all, of
+// which five would do where dS could stay in registers.  Bound: chains of dependent steps at
+// two waves to a SIMD (registers).  4 x 777 tokens, 8 heads of 64: 52 us, 428 TFLOP/s of the
+// nine; in a launch each they made forward and gradients 115 us long, together 107.
 template <int DT, int HD, typename Sh, bool REG>
 __global__ __launch_bounds__(256, 2) void k_relpos_grad(Rp p, Gp c, uint32_t n_tiles, uint32_t n_pairs)
 {
@@ -936,7 +948,8 @@ __global__ __launch_bounds__(256) void k_relpos_fold(const float* __restrict__ p
 // The pairs of a bucket, in segments: order[seg_ptr[g] .. seg_ptr[g + 1]) are places in a
 // head's tiles.  A wave adds one segment, each lane its pairs in order, then a fixed tree; out:
 // [segment][head], or the table's gradient where every bucket is one segment.  sum NULL: no
-// sequences, all zero.
+// sequences, all zero.  Bound: reads of 4 bytes where a bucket's pairs lie on diagonals (777
+// tokens, 8 heads, 32 buckets: 11 us; 197 tokens, 12 heads, 732 buckets: 5).
 template <int DT>
 __global__ __launch_bounds__(256) void k_relpos_segments(const int32_t* __restrict__ order,
                                                          const int32_t* __restrict__ seg_ptr, int32_t n_segs,
@@ -996,7 +1009,9 @@ __global__ __launch_bounds__(256) void k_relpos_buckets(const int32_t* __restric
 // Windows of at most 64 tokens: everything of a window and head fits a wave's (forward) or a
 // small workgroup's (gradients) registers and LDS, so a workgroup stays with one head, whose
 // bias its registers hold as the accumulators' start, and takes one window after the other,
-// the next one's rows in flight.  Bound: HBM.
+// the next one's rows in flight.  Against the general kernels (us of a call): 2048 x 49
+// tokens, 3 heads of 32, forward 20 / 28, gradients 42 / 111; 4096 x 16 tokens, 6 heads, 19 /
+// 61 and 47 / 281; 512 x 64 tokens, 6 heads of 64, 24 / 26 and 54 / 110.
 
 // Workgroup -> head and run of windows.  Workgroups L and L + 8 share an XCD: the heads of a
 // run of windows are 8 apart, so that the lines that rows of two heads share are fetched and
@@ -1027,7 +1042,8 @@ int window_runs(int64_t n_seq, int32_t H, int64_t most, int each)
 }
 
 // Forward: a wave to a window, four windows to a workgroup.  Q is read as the operand that it
-// is, K and V pass through the wave's LDS rows.
+// is, K and V pass through the wave's LDS rows.  Bound: HBM.  4096 x 49 tokens, 3 heads of 32,
+// labels: 37 us, 4.1 TB/s.
 template <int DT, int HD, int NT, bool REG>
 __global__ __launch_bounds__(256, HD == 32 ? 2 : 1) void k_relpos_window_fwd(
     Rp p, const uint16_t* __restrict__ idx, const uint16_t* __restrict__ table, uint16_t* __restrict__ out,
@@ -1169,7 +1185,9 @@ __global__ __launch_bounds__(256, HD == 32 ? 2 : 1) void k_relpos_window_fwd(
 // wave holds a 32-query tile (lane = query): S^T, dP^T, D from the weights themselves, dS^T,
 // which its registers add up over the windows for the bias's gradient, and dQ^T = K^T dS^T.
 // P and dS, rounded once, cross to the other operand order through LDS; then a wave holds a
-// 32-key tile: dV^T = dO^T P, dK^T = Q^T dS.
+// 32-key tile: dV^T = dO^T P, dK^T = Q^T dS.  Bound: HBM as far as four workgroups to a
+// compute unit (LDS and registers) keep it busy.  4096 x 49 tokens, 3 heads of 32, labels: 81
+// us, 3.3 TB/s.
 template <int DT, int HD, int NT, bool REG>
 __global__ __launch_bounds__(64 * NT, HD == 32 ? 2 : 1) void k_relpos_window_grad(
     Rp p, const uint16_t* __restrict__ idx, const uint16_t* __restrict__ table,
@@ -1370,7 +1388,8 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // the tile before into dV^T = dO^T P and dK^T = Q^T dS over all queries.  So every score is
 // formed once, with five products, where the general kernels form it three times with nine.
 // LDS holds all rows of Q and dO, two key tiles and the two buffers.  Bound: LDS reads and
-// the chain of a tile at two waves to a SIMD (the sums leave registers for no more).
+// the chain of a tile at two waves to a SIMD (the sums leave registers for no more).  64 x
+// 197 tokens, 12 heads of 64: 72 us, 264 TFLOP/s; 256 x 144, 6 heads of 32, labels: 64 us.
 constexpr int MID_TILES = 7;  // with the wave more two waves to a SIMD, which the sums' registers allow
 constexpr int MID_XS = 72;  // bytes of a row of P or dS, 32 keys: the writes of 32 rows' 8 bytes meet all banks
 template <int DT, int HD, bool REG>
@@ -1895,12 +1914,6 @@ void relpos_tables(const int32_t* index, int32_t T, int32_t n_buckets, int32_t n
     }
     bucket_seg[n_buckets] = seg;
     seg_ptr[seg] = at;
-    for (int32_t i = 0; i < T; ++i)
-        for (int32_t j = 0; j < T; ++j)
-            if (index[(int64_t)i * T + j] >= 0) {
-                idx[i * Tp + j] = (uint16_t)index[(int64_t)i * T + j];
-                idx_t[j * Tp + i] = (uint16_t)index[(int64_t)i * T + j];
-            }
     // a bucket's pairs in the order of their places (so that neighbours are read together):
     // tile after tile, in one [c / 8][lane][c % 4] with row i % 32 in the lanes
     for (int32_t a = 0; a < nt; ++a)
@@ -1908,9 +1921,12 @@ void relpos_tables(const int32_t* index, int32_t T, int32_t n_buckets, int32_t n
             for (int32_t at = 0; at < 1024; ++at) {
                 const int32_t lane = at / 4 % 64, i = 32 * a + lane % 32;
                 const int32_t j = 32 * c + at / 256 * 8 + lane / 32 * 4 + at % 4;
-                const uint16_t b = idx[i * Tp + j];
-                if (b != 0xffff)
+                const int32_t b = i < T && j < T ? index[(int64_t)i * T + j] : -1;
+                if (b >= 0) {
+                    idx[i * Tp + j] = (uint16_t)b;
+                    idx_t[j * Tp + i] = (uint16_t)b;
                     order[count[b]++] = (a * nt + c) * 1024 + at;
+                }
             }
 }
 
