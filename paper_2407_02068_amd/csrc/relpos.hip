@@ -387,8 +387,8 @@ __device__ inline void pass_blocks(const Rp& p, const uint16_t* a, int64_t lda, 
 // Bound: waits between a tile's dependent steps at three waves to a SIMD (the softmax's vector
 // instructions take 37% of a SIMD's time, the matrix cores 14%).  64 x 197 tokens, 12 heads
 // of 64: 28 us, 272 TFLOP/s; 8 x 1025, fp16, padded: 62 us, 417 TFLOP/s.  Four waves to a
-// SIMD, at 128 registers, gained nothing (28.9 and 68), nor did five to a workgroup where
-// fewer would be idle (64 x 144 tokens, 12 heads of 64: 26.0 against 24.0).
+// SIMD, at 128 registers, gained nothing (28.9 and 68), nor did five to a workgroup (64 x 144
+// tokens, 12 heads of 64: 26.0, four 24.0, three 22.9).
 template <int DT, int HD, typename Sh, bool REG>
 __global__ __launch_bounds__(Sh::NT, HD == 32 ? 4 : 3) void k_relpos_fwd(Rp p, uint16_t* __restrict__ out, int64_t ldo,
                                                        float* __restrict__ lse, float scale)
@@ -1735,6 +1735,12 @@ hipError_t expand_bias(const lpv_relpos* h, const void* table, int32_t H, int32_
 // 8 heads, the forward kernel 26.8 against 19.8.)
 bool few_tiles(const lpv_relpos* h, const RelposCall& c, int64_t few) { return c.n_seq * c.H * h->nt < few; }
 
+// Three tiles to a workgroup of the forward pass where that takes a quarter of the waves
+// fewer, the others being idle (3, 5, 6 and 9 tiles): smaller groups stage K and V more often.
+// (us of the call, three / four, 12 heads of 64: 256 x 144 tokens 59.9 / 69.2, 64 x 190 25.7 /
+// 27.5, 64 x 280 41.5 / 46.4; with 17 tiles, a tenth fewer, 67.0 / 63.4.)
+bool groups_of_three(int nt) { return (nt + 2) / 3 * 3 * 4 <= (nt + 3) / 4 * 4 * 3; }
+
 template <int DT, int HD, bool REG, typename Sh>
 hipError_t forward_tiles(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
 {
@@ -1776,8 +1782,10 @@ template <int DT, int HD, bool REG> hipError_t forward_as(const lpv_relpos* h, c
     const hipError_t e = expand_bias<DT>(h, c.table, c.H, HD, (float*)c.ws, nullptr, s);
     if (e != hipSuccess)
         return e;
-    return few_tiles(h, c, 1536) ? forward_tiles<DT, HD, REG, Shape<2, 2>>(h, c, s)
-                                 : forward_tiles<DT, HD, REG, Shape<4, 1>>(h, c, s);
+    if (few_tiles(h, c, 1536))
+        return forward_tiles<DT, HD, REG, Shape<2, 2>>(h, c, s);
+    return groups_of_three(h->nt) ? forward_tiles<DT, HD, REG, Shape<3, 1>>(h, c, s)
+                                  : forward_tiles<DT, HD, REG, Shape<4, 1>>(h, c, s);
 }
 
 template <int DT, int HD>

@@ -400,6 +400,7 @@ def test_each_kernel_is_reached():
             (32, 40, 2, ("window_fwd<2,32,1", "window_grad<2,32,1", "fold<16>"), ("bias", "rows")),
             (64, 3, 2, ("window_fwd<2,32,2", "window_grad<2,32,2", "fold<1>"), ("bias", "mid_grad")),
             (65, 3, 2, ("k_relpos_fwd<2,32", two, "mid_grad", "bias"), ("window", "rows")),
+            (140, 80, 4, ("k_relpos_fwd<2,32", "Shape<3,1>", "mid_grad"), ("window", one, two)),
             (224, 70, 4, ("k_relpos_fwd<2,32", one, "mid_grad"), ("window", "k_relpos_grad")),
             (225, 2, 2, ("k_relpos_grad<2,32", two, "k_relpos_rows"), (one, "mid_grad")),
             (225, 16, 4, ("k_relpos_grad<2,32", one, two, "k_relpos_rows"), ("mid_grad",))):
@@ -420,6 +421,18 @@ def test_labels_with_many_tiles(T, n_seq, H, labels):
         region[4] = -1
         region[3] = 8
     Case(*line_index(T, 12), n_seq, H, 32, "bf16", region=region, seed=158).run()
+
+
+@pytest.mark.parametrize("T,n_seq,H,hd,labels", [(140, 80, 4, 32, True), (170, 70, 4, 64, False),
+                                                 (81, 130, 4, 64, True), (200, 60, 4, 32, True)])
+def test_forward_with_many_tiles(T, n_seq, H, hd, labels):
+    """Three and four tiles to a workgroup, one wave each."""
+    region = None
+    if labels:
+        region = np.random.default_rng(T).integers(0, 2, (3, T))
+        region[1, T // 2:] = -1
+        region[2] = 8
+    Case(*line_index(T, 12), n_seq, H, hd, "bf16", region=region, seed=164).run()
 
 
 @pytest.mark.parametrize("T,n_buckets", [(60, 20000), (130, 20000), (130, 12288), (130, 12289), (240, 65535)])
