@@ -949,7 +949,7 @@ __global__ __launch_bounds__(256) void k_relpos_fold(const float* __restrict__ p
 // head's tiles.  A wave adds one segment, each lane its pairs in order, then a fixed tree; out:
 // [segment][head], or the table's gradient where every bucket is one segment.  sum NULL: no
 // sequences, all zero.  Bound: reads of 4 bytes where a bucket's pairs lie on diagonals (777
-// tokens, 8 heads, 32 buckets: 11 us; 197 tokens, 12 heads, 732 buckets: 5).
+// tokens, 8 heads, 32 buckets: 8 us; 197 tokens, 12 heads, 732 buckets: 5).
 template <int DT>
 __global__ __launch_bounds__(256) void k_relpos_segments(const int32_t* __restrict__ order,
                                                          const int32_t* __restrict__ seg_ptr, int32_t n_segs,
@@ -963,15 +963,20 @@ __global__ __launch_bounds__(256) void k_relpos_segments(const int32_t* __restri
     float v = 0.0f;
     if (sum) {
         const float* at = sum + h * n_pos;
-        const int end = seg_ptr[g + 1];
-        for (int i = seg_ptr[g] + lane; i < end; i += 256) {
-            float w[4];
+        const int begin = seg_ptr[g], end = seg_ptr[g + 1], i = begin + lane;
+        static_assert(RELPOS_SEG == 512, "a segment is one turn");
+        if (begin < end) {  // (all loads at once: those past the segment ask for its last pair)
+            int o[8];
+            float w[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = i + 64 * j < end ? at[order[i + 64 * j]] : 0.0f;
+            for (int j = 0; j < 8; ++j)
+                o[j] = order[min(i + 64 * j, end - 1)];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                v += w[j];
+            for (int j = 0; j < 8; ++j)
+                w[j] = at[o[j]];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v += i + 64 * j < end ? w[j] : 0.0f;
         }
     }
 #pragma unroll
