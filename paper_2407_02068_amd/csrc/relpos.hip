@@ -86,7 +86,37 @@ __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, 
     return o;
 }
 
-// The bias tiles of every head: blockIdx.z 0 those of idx, 1 those of its transpose.  A
+// D = dO . O of every row and head, hd / 8 lanes to a row, by `wgs` workgroups.  (4 x 777
+// tokens, 8 heads of 64: beside the bias's tiles 1 us, in a launch of its own 4.)
+struct RowsCall {
+    const uint16_t *out, *dout;
+    int64_t ldo, ldg, M;
+    int32_t T;
+    float* Dv;
+};
+template <int DT, int HD> __device__ inline void row_products(const RowsCall& c, int H, uint32_t wg, uint32_t wgs)
+{
+    using F = typename Elem<DT>::frag;
+    constexpr int CH = HD / 8;
+    // (the lanes of a row leave together)
+    for (int64_t i = (int64_t)wg * 256 + threadIdx.x; i / CH < c.M * H; i += (int64_t)wgs * 256) {
+        const int64_t r = i / CH, row = r / H, seq = row / c.T;
+        const int h = (int)(r - row * H), k = (int)(i % CH) * 8;
+        const F g = *(const F*)(c.dout + row * c.ldg + h * HD + k), o = *(const F*)(c.out + row * c.ldo + h * HD + k);
+        float v = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v = fmaf((float)g[j], (float)o[j], v);
+#pragma unroll
+        for (int d = 1; d < CH; d <<= 1)
+            v += __shfl_xor(v, d, 64);
+        if (k == 0)
+            c.Dv[(seq * H + h) * c.T + (row - seq * c.T)] = v;
+    }
+}
+
+// The bias tiles of every head: blockIdx.z 0 those of idx, 1 those of its transpose; 2 (with
+// HD): the rows' products, which the gradients that take both wait for as well.  A
 // workgroup takes a head and `per` tiles; a head's column of the table is made ready in
 // LDS once, where its gathers cost no more than reads of consecutive values do (the lanes of
 // a tile's row differ by a constant in most indexes); larger tables are gathered in memory.
@@ -96,15 +126,24 @@ __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, 
 // smaller ones.
 constexpr int BIAS_LDS = 12288;  // buckets
 
-template <int DT>
+template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_relpos_bias(const uint16_t* __restrict__ idx,
                                                      const uint16_t* __restrict__ idx_t, int32_t nt,
                                                      const uint16_t* __restrict__ table, int32_t n_buckets,
                                                      int32_t H, float root, int32_t per,
-                                                     float* __restrict__ bias, float* __restrict__ bias_t)
+                                                     float* __restrict__ bias, float* __restrict__ bias_t,
+                                                     RowsCall rows)
 {
     extern __shared__ float column[];  // n_buckets, or none
+    if constexpr (HD > 0) {
+        if (blockIdx.z == 2) {
+            row_products<DT, HD>(rows, H, blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
+            return;
+        }
+    }
     const int n_tiles = nt * nt, h = blockIdx.y, lane = threadIdx.x & 63;
+    if ((int)blockIdx.x * per >= n_tiles)
+        return;
     const bool in_lds = n_buckets <= BIAS_LDS;
     if (in_lds) {
         constexpr uint16_t LOWEST = DT == LPV_BF16 ? 0xff7f : 0xfbff, NEG_INF = DT == LPV_BF16 ? 0xff80 : 0xfc00;
@@ -564,32 +603,6 @@ template <int HD> struct GradLds {
     __attribute__((aligned(16))) int32_t lab[2][64];
     int32_t states[2][2];
 };
-
-// D = dO . O of every row and head, hd / 8 lanes to a row.  Bound: its launch (4 x 777 tokens,
-// 8 heads of 64, 6 MB: 4 us).
-template <int DT, int HD>
-__global__ __launch_bounds__(256) void k_relpos_rows(const uint16_t* __restrict__ out, int64_t ldo,
-                                                     const uint16_t* __restrict__ dout, int64_t ldg, int64_t M,
-                                                     int32_t T, int32_t H, float* __restrict__ Dv)
-{
-    using F = typename Elem<DT>::frag;
-    constexpr int CH = HD / 8;
-    // (the lanes of a row leave together)
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i / CH < M * H; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / CH, row = r / H, seq = row / T;
-        const int h = (int)(r - row * H), k = (int)(i % CH) * 8;
-        const F g = *(const F*)(dout + row * ldg + h * HD + k), o = *(const F*)(out + row * ldo + h * HD + k);
-        float v = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v = fmaf((float)g[j], (float)o[j], v);
-#pragma unroll
-        for (int d = 1; d < CH; d <<= 1)
-            v += __shfl_xor(v, d, 64);
-        if (k == 0)
-            Dv[(seq * H + h) * T + (row - seq * T)] = v;
-    }
-}
 
 // dQ, tiled as the forward: the weights come back from lse, dP^T = V dO^T, and dS^T,
 // rounded once, is the B operand of dQ^T = K^T dS^T.
@@ -1717,17 +1730,21 @@ Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
     return w;
 }
 
-template <int DT>
+// bias_t, rows: for the gradients that take the transposed tiles and the rows' products (HD,
+// else 0).
+template <int DT, int HD>
 hipError_t expand_bias(const lpv_relpos* h, const void* table, int32_t H, int32_t hd, float* bias,
-                       float* bias_t, hipStream_t s)
+                       float* bias_t, const RowsCall& rows, hipStream_t s)
 {
     // (a tile to a wave, or more of them where that makes over 1024 workgroups, each of which
     // makes the column ready for itself)
     const int tiles = h->nt * h->nt, per = std::max(4, (tiles * H + 1023) / 1024);
-    const dim3 grid((tiles + per - 1) / per, H, bias_t ? 2 : 1);
-    hipLaunchKernelGGL((k_relpos_bias<DT>), grid, dim3(256), h->n_buckets <= BIAS_LDS ? h->n_buckets * 4 : 0, s,
+    // (rows: hd / 8 lanes each, up to 4096 workgroups' of them at once)
+    const int64_t lanes = rows.M * H * (HD / 8), wgs = std::min<int64_t>(4096, (lanes + 255) / 256);
+    const dim3 grid(std::max((tiles + per - 1) / per, (int)((wgs + H - 1) / H)), H, HD ? 3 : 1);
+    hipLaunchKernelGGL((k_relpos_bias<DT, HD>), grid, dim3(256), h->n_buckets <= BIAS_LDS ? h->n_buckets * 4 : 0, s,
                        h->idx, h->idx_t, h->nt, (const uint16_t*)table, h->n_buckets, H, sqrtf((float)hd), per,
-                       bias, bias_t);
+                       bias, bias_t, rows);
     return hipGetLastError();
 }
 
@@ -1784,22 +1801,13 @@ template <int DT, int HD, bool REG> hipError_t forward_as(const lpv_relpos* h, c
 {
     if (is_window(h))
         return h->nt == 1 ? forward_windows<DT, HD, REG, 1>(h, c, s) : forward_windows<DT, HD, REG, 2>(h, c, s);
-    const hipError_t e = expand_bias<DT>(h, c.table, c.H, HD, (float*)c.ws, nullptr, s);
+    const hipError_t e = expand_bias<DT, 0>(h, c.table, c.H, HD, (float*)c.ws, nullptr, {}, s);
     if (e != hipSuccess)
         return e;
     if (few_tiles(h, c, 1536))
         return forward_tiles<DT, HD, REG, Shape<2, 2>>(h, c, s);
     return groups_of_three(h->nt) ? forward_tiles<DT, HD, REG, Shape<3, 1>>(h, c, s)
                                   : forward_tiles<DT, HD, REG, Shape<4, 1>>(h, c, s);
-}
-
-template <int DT, int HD>
-hipError_t launch_row_products(const lpv_relpos* h, const RelposCall& c, float* D, hipStream_t s)
-{
-    const int64_t n = c.n_seq * h->T * c.H * (HD / 8), wgs = (n + 255) / 256;
-    hipLaunchKernelGGL((k_relpos_rows<DT, HD>), dim3((uint32_t)(wgs < 4096 ? wgs : 4096)), dim3(256), 0, s,
-                       (const uint16_t*)c.out, c.ldo, (const uint16_t*)c.dout, c.ldg, c.n_seq * h->T, h->T, c.H, D);
-    return hipGetLastError();
 }
 
 template <int DT, int HD, bool REG, typename Sh>
@@ -1850,13 +1858,13 @@ hipError_t grad_as(const lpv_relpos* h, const RelposCall& c, hipStream_t s)
         e = h->nt == 1 ? grad_windows<DT, HD, REG, 1>(h, c, w, chunks, s)
                        : grad_windows<DT, HD, REG, 2>(h, c, w, chunks, s);
     } else if (chunks > 0 && is_mid(h)) {
-        e = expand_bias<DT>(h, c.table, c.H, HD, w.bias, nullptr, s);
+        e = expand_bias<DT, 0>(h, c.table, c.H, HD, w.bias, nullptr, {}, s);
         if (e == hipSuccess)
             e = grad_mid<DT, HD, REG>(h, c, w, chunks, s);
     } else if (chunks > 0) {  // (n_seq > 0)
-        e = expand_bias<DT>(h, c.table, c.H, HD, w.bias, w.bias_t, s);
-        if (e == hipSuccess)
-            e = launch_row_products<DT, HD>(h, c, w.D, s);
+        const RowsCall rows = {(const uint16_t*)c.out, (const uint16_t*)c.dout, c.ldo, c.ldg, c.n_seq * h->T, h->T,
+                               w.D};
+        e = expand_bias<DT, HD>(h, c.table, c.H, HD, w.bias, w.bias_t, rows, s);
         if (e == hipSuccess)
             e = few_tiles(h, c, 512) ? grad_tiles<DT, HD, REG, Shape<2, 2>>(h, c, w, chunks, s)
                                      : grad_tiles<DT, HD, REG, Shape<4, 1>>(h, c, w, chunks, s);

@@ -397,13 +397,13 @@ def test_each_kernel_is_reached():
         return {n.replace("lpv::(anonymous namespace)::", "").replace(" ", "") for n in kernels(calls, args=True)}
     one, two = "Shape<4,1>", "Shape<2,2>"
     for T, n_seq, H, there, absent in (
-            (32, 40, 2, ("window_fwd<2,32,1", "window_grad<2,32,1", "fold<16>"), ("bias", "rows")),
+            (32, 40, 2, ("window_fwd<2,32,1", "window_grad<2,32,1", "fold<16>"), ("bias",)),
             (64, 3, 2, ("window_fwd<2,32,2", "window_grad<2,32,2", "fold<1>"), ("bias", "mid_grad")),
-            (65, 3, 2, ("k_relpos_fwd<2,32", two, "mid_grad", "bias"), ("window", "rows")),
+            (65, 3, 2, ("k_relpos_fwd<2,32", two, "mid_grad", "bias<2,0>"), ("window", "bias<2,32>")),
             (140, 80, 4, ("k_relpos_fwd<2,32", "Shape<3,1>", "mid_grad"), ("window", one, two)),
             (224, 70, 4, ("k_relpos_fwd<2,32", one, "mid_grad"), ("window", "k_relpos_grad")),
-            (225, 2, 2, ("k_relpos_grad<2,32", two, "k_relpos_rows"), (one, "mid_grad")),
-            (225, 16, 4, ("k_relpos_grad<2,32", one, two, "k_relpos_rows"), ("mid_grad",))):
+            (225, 2, 2, ("k_relpos_grad<2,32", two, "bias<2,0>", "bias<2,32>"), (one, "mid_grad")),
+            (225, 16, 4, ("k_relpos_grad<2,32", one, two, "bias<2,0>", "bias<2,32>"), ("mid_grad",))):
         got = names(T, n_seq, H)
         for n in there:
             assert any(n in g for g in got), (T, n, got)
