@@ -452,7 +452,9 @@ lpv_status lpv_relpos_workspace_size(const lpv_relpos* p, int64_t n_seq, int32_t
  * the handle's T tokens (a window each, or a whole image):
  *   s_ij = q_i . k_j / sqrt(hd) + table[index_ij][h],   out_h = softmax_j(s) V_h.
  * table   device, n_buckets x H, row-major, of the element type.  A bias of -inf or of the
- *         type's lowest finite value takes its pairs out.
+ *         type's lowest finite value takes its pairs out; other finite ones beyond +-2^15
+ *         count as +-2^15 (beside smaller ones -2^15 leaves a pair no weight; a row of such
+ *         pairs alone keeps its accuracy).
  * qkv     device, (n_seq T) x (3 H hd), row stride ldq; a row holds q, k, v, each H heads
  *         of hd elements (as in lpv_attention).
  * region  device, n_region x T int32, or NULL: sequence s has the labels of row

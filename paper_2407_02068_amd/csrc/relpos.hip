@@ -61,11 +61,15 @@ __device__ inline uint32_t lds32(const void* p)
 // column 8 (r / 4) + 4 (l / 32) + r % 4; in memory [r / 4][lane][r % 4], so that a wave's
 // loads and stores are whole lines.
 
-// A bias as the accumulator's start.  (A finite one stays finite: the product's overflow
-// would mask the pair.)
-__device__ inline float ready_bias(uint16_t t, uint16_t lowest, uint16_t neg_inf, float f)
+// A bias as the accumulator's start.  Finite ones saturate at 2^15: in a row whose every pair
+// has one of -1e9, say, the weights would be differences of numbers whose float32 steps are
+// far over 1, and infinite where the gradients take them from lse; at 2^15 they are right to 2^-9.
+constexpr float MOST_BIAS = 32768.0f;
+template <int DT> __device__ inline float ready_bias(uint16_t t, float root)
 {
-    return t == lowest || t == neg_inf ? -INFINITY : fminf(fmaxf(f, -3e38f), 3e38f);
+    constexpr uint16_t LOWEST = DT == LPV_BF16 ? 0xff7f : 0xfbff, NEG_INF = DT == LPV_BF16 ? 0xff80 : 0xfc00;
+    return t == LOWEST || t == NEG_INF ? -INFINITY
+                                       : fminf(fmaxf(Elem<DT>::to_f32(t), -MOST_BIAS), MOST_BIAS) * root;
 }
 
 // Elements 4 g .. 4 g + 3 of this lane.
@@ -73,7 +77,7 @@ template <int DT>
 __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, int g, int lane,
                                      const uint16_t* table, int H, int h, float root)
 {
-    constexpr uint16_t LOWEST = DT == LPV_BF16 ? 0xff7f : 0xfbff, NEG_INF = DT == LPV_BF16 ? 0xff80 : 0xfc00;
+    constexpr uint16_t NEG_INF = DT == LPV_BF16 ? 0xff80 : 0xfc00;
     const uint2 v = *(const uint2*)(idx + ((int64_t)a * 32 + (lane & 31)) * (nt * 32) + b * 32 + 4 * (lane >> 5) + 8 * g);
     const uint16_t* e = (const uint16_t*)&v;
     float4 o;
@@ -81,7 +85,7 @@ __device__ inline float4 gather_bias(const uint16_t* idx, int nt, int a, int b, 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint16_t t = e[j] == 0xffff ? NEG_INF : table[(int64_t)e[j] * H + h];
-        of[j] = ready_bias(t, LOWEST, NEG_INF, Elem<DT>::to_f32(t) * root);
+        of[j] = ready_bias<DT>(t, root);
     }
     return o;
 }
@@ -146,11 +150,8 @@ __global__ __launch_bounds__(256) void k_relpos_bias(const uint16_t* __restrict_
         return;
     const bool in_lds = n_buckets <= BIAS_LDS;
     if (in_lds) {
-        constexpr uint16_t LOWEST = DT == LPV_BF16 ? 0xff7f : 0xfbff, NEG_INF = DT == LPV_BF16 ? 0xff80 : 0xfc00;
-        for (int i = threadIdx.x; i < n_buckets; i += 256) {
-            const uint16_t t = table[(int64_t)i * H + h];
-            column[i] = ready_bias(t, LOWEST, NEG_INF, Elem<DT>::to_f32(t) * root);
-        }
+        for (int i = threadIdx.x; i < n_buckets; i += 256)
+            column[i] = ready_bias<DT>(table[(int64_t)i * H + h], root);
         __syncthreads();
     }
     const uint16_t* from = blockIdx.z ? idx_t : idx;

@@ -205,6 +205,23 @@ def test_masks_that_leave_nothing(dtype):
     assert not dtable[list(bad)].any()
 
 
+@pytest.mark.parametrize("dtype,value", [("bf16", -2.0 ** 30), ("bf16", -2.0 ** 100), ("bf16", 2.0 ** 60),
+                                         ("f16", -60000.0), ("bf16", -2.0 ** 15), ("bf16", -16384.0)])
+@pytest.mark.parametrize("T", [30, 49, 100, 240])
+def test_rows_of_large_biases_alone(T, dtype, value):
+    """Rows whose every pair has one large bias are as without it, beside rows where a few pairs
+    have it: beyond 2^15 it counts as that."""
+    idx, n = line_index(T, 9)
+    idx[T // 2] = 8
+    idx[3] = 8
+    idx[:3] = np.minimum(idx[:3], 7)  # (rows without it)
+
+    def edit(c):
+        c.t[8] = np.clip(value, -2.0 ** 15, 2.0 ** 15)
+        c.table[8] = value
+    Case(idx, n, 3, 2, 32, dtype, seed=165, edit=edit).run()
+
+
 def test_every_pair_masked():
     c = Case(np.full((40, 40), -1, np.int32), 5, 3, 2, 64, "bf16", seed=151)
     out, lse, dqkv, dtable = c.run()
