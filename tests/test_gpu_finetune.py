@@ -175,13 +175,13 @@ def test_finetuning_step_captured():
     s.close()
 
 
-@pytest.mark.parametrize("labels", [False, True])
-def test_encoder_chain_with_a_position_bias(labels):
+@pytest.mark.parametrize("side,class_token,n_seq,labels", [(14, True, 2, False), (14, True, 2, True),
+                                                           (7, False, 5, True)])
+def test_encoder_chain_with_a_position_bias(side, class_token, n_seq, labels):
     """Every attention of the chain against the oracle on its own input, and graph replays."""
-    side, H = 14, 12
-    idx, n = window_index(side, True)
-    T = side * side + 1
-    blocks, n_seq = 2, 2
+    H, blocks = 12, 2
+    idx, n = window_index(side, class_token)
+    T = len(idx)
     layers = wl.b_stack(M=n_seq * T, layers=blocks)
     region = None
     if labels:
