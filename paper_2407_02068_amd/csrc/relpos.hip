@@ -587,6 +587,7 @@ template <int N> __device__ inline bool join_sums(char* buf, f32x16* o, int wave
 struct Gp {
     const float* lse;
     const float* Dv;  // dO . O of each row, in lse's layout (anything for a row without pairs)
+    float* Dc;        // the same without the rounding of O: grad_q's, for the bias's sums
     const uint16_t* dout;
     int64_t ldg;
     uint16_t* dqkv;
@@ -606,7 +607,8 @@ template <int HD> struct GradLds {
 };
 
 // dQ, tiled as the forward: the weights come back from lse, dP^T = V dO^T, and dS^T,
-// rounded once, is the B operand of dQ^T = K^T dS^T.
+// rounded once, is the B operand of dQ^T = K^T dS^T.  A row of dS sums to zero; what it sums
+// to here is what D is off by, O having been rounded: with it D is right for the bias's sums.
 template <int DT, int HD, typename Sh, bool REG>
 __device__ inline void grad_q(const Rp& p, const Gp& c, uint32_t id, GradLds<HD>& sh)
 {
@@ -641,6 +643,7 @@ __device__ inline void grad_q(const Rp& p, const Gp& c, uint32_t id, GradLds<HD>
 #pragma unroll
     for (int d = 0; d < ND; ++d)
         dq[d] = f32x16{};
+    float off[2] = {0.0f, 0.0f};
     int32_t lv = -1;
     pass_blocks<HD, Sh, REG>(
         p, base + hw, ldq, base + 2 * hw, ldq, reg,
@@ -673,9 +676,13 @@ __device__ inline void grad_q(const Rp& p, const Gp& c, uint32_t id, GradLds<HD>
                 mask_region(s, mine, lab[b] + row0, half);
             uint32_t db[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                db[j] = pack2<DT>(__builtin_amdgcn_exp2f(fmaf(s[2 * j], scale, nl)) * (dp[2 * j] - D),
-                                  __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], scale, nl)) * (dp[2 * j + 1] - D));
+            for (int j = 0; j < 8; ++j) {
+                const float f0 = __builtin_amdgcn_exp2f(fmaf(s[2 * j], scale, nl)) * (dp[2 * j] - D);
+                const float f1 = __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], scale, nl)) * (dp[2 * j + 1] - D);
+                off[0] += f0;
+                off[1] += f1;
+                db[j] = pack2<DT>(f0, f1);
+            }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const F df = as_frag<F>(uint4{db[4 * u], db[4 * u + 1], db[4 * u + 2], db[4 * u + 3]});
@@ -684,13 +691,21 @@ __device__ inline void grad_q(const Rp& p, const Gp& c, uint32_t id, GradLds<HD>
                     dq[d] = E::mma(tr_frag<F, HD>(kt, 16 * u, d), df, dq[d]);
             }
         });
+    float miss = half_add(off[0] + off[1]);
     if constexpr (Sh::KS == 2) {
         static_assert(Sh::QW * ND * 4096 <= (int)sizeof(sh.rows), "the joined rows fit");
+        float* other = (float*)sh.stats + wave / 2 * 32 + l32;
+        if (part == 1 && half == 0)
+            *other = miss;
         if (!join_sums<ND>(kv, dq, wave))
             return;
+        miss += *other;
     }
-    if (busy && q < T)
+    if (busy && q < T) {
         store_rows<DT, HD>(c.dqkv + (at.seq * T + q) * lddq + at.h * HD, dq, rroot, half);
+        if (half == 0)
+            c.Dc[stat + q] = D + miss;
+    }
 }
 
 // dK and dV: a wave holds a 32-key tile, the queries pass in blocks with their lse and D.
@@ -814,12 +829,12 @@ __device__ inline void grad_kv(const Rp& p, const Gp& c, uint32_t id, GradLds<HD
 // four waves (a 32 x 32 tile each, summed in its accumulators' places in float32), the four
 // matrices' rows staged in LDS a sequence ahead.  part: [head][chunk][tile][r / 4][lane][r % 4].
 template <int DT, int HD, bool REG>
-__device__ inline void grad_bias(const Rp& p, const Gp& c, uint32_t id, GradLds<HD>& sh)
+__device__ inline void grad_bias(const Rp& p, const Gp& c, const float* Dv, uint32_t id, char* lds)
 {
     using E = Elem<DT>;
     using F = typename E::frag;
     constexpr int RS = Row<HD>::RS, KS = Row<HD>::KS;
-    char(&rows)[4][64 * RS] = *(char(*)[4][64 * RS])sh.rows;  // Q, dO, K, V
+    char(&rows)[4][64 * RS] = *(char(*)[4][64 * RS])lds;  // Q, dO, K, V
     const int64_t ldg = c.ldg;
     const int32_t chunks = c.chunks;
     const float scale = c.scale;
@@ -855,7 +870,7 @@ __device__ inline void grad_bias(const Rp& p, const Gp& c, uint32_t id, GradLds<
         sq.store(rows[0], rows[1]);
         sk.store(rows[2], rows[3]);
         const int64_t stat = (seq * p.H + h) * T;
-        const float v = c.lse[stat + qc], D = v == -INFINITY ? 0.0f : c.Dv[stat + qc];
+        const float v = c.lse[stat + qc], D = v == -INFINITY ? 0.0f : Dv[stat + qc];
         // (a query past T: every weight 2^-inf)
         const float nl = v == -INFINITY || q >= T ? -INFINITY : -v * LOG2E;
         __syncthreads();
@@ -894,10 +909,11 @@ __device__ inline void grad_bias(const Rp& p, const Gp& c, uint32_t id, GradLds<
 }
 
 // All gradients of longer sequences in one launch, so that its parts fill the chip together:
-// workgroups of dQ, then of dK and dV, then of the bias's.  Nine products of T^2 hd in all, of
-// which five would do where dS could stay in registers.  Bound: chains of dependent steps at
-// two waves to a SIMD (registers).  4 x 777 tokens, 8 heads of 64: 52 us, 428 TFLOP/s of the
-// nine; in a launch each they made forward and gradients 115 us long, together 107.
+// workgroups of dQ, then of dK and dV, then (unless n_pairs is 0) of the bias's.  Nine products
+// of T^2 hd in all, of which five would do where dS could stay in registers.  Bound: chains of
+// dependent steps at two waves to a SIMD (registers).  4 x 777 tokens, 8 heads of 64: 52 us, 428
+// TFLOP/s of the nine; in a launch each they made forward and gradients 115 us long, together
+// 107.
 template <int DT, int HD, typename Sh, bool REG>
 __global__ __launch_bounds__(256, 2) void k_relpos_grad(Rp p, Gp c, uint32_t n_tiles, uint32_t n_pairs)
 {
@@ -916,8 +932,21 @@ __global__ __launch_bounds__(256, 2) void k_relpos_grad(Rp p, Gp c, uint32_t n_t
     } else {
         const uint32_t i = xcd_order(n_pairs, id - 2 * span);
         if (i < n_pairs)
-            grad_bias<DT, HD, REG>(p, c, i, sh);
+            grad_bias<DT, HD, REG>(p, c, c.Dv, i, sh.rows);
     }
+}
+
+// The bias's part alone, behind the others, with the D that grad_q has put right: for tables
+// of fewer buckets than a row has pairs, whose gradient D's error would show in.  (The same
+// case: 40 us and 20 for this; the table's gradient off by its rounding alone, against up to
+// 1.7 times that.)
+template <int DT, int HD, bool REG>
+__global__ __launch_bounds__(256) void k_relpos_pairs(Rp p, Gp c, uint32_t n_pairs)
+{
+    __shared__ __attribute__((aligned(16))) char rows[4 * 64 * Row<HD>::RS];
+    const uint32_t i = xcd_order(n_pairs, blockIdx.y * gridDim.x + blockIdx.x);
+    if (i < n_pairs)
+        grad_bias<DT, HD, REG>(p, c, c.Dc, i, rows);
 }
 
 // The chunks' sums of each pair: CL threads of a workgroup share a pair's chunks (each in
@@ -1707,7 +1736,7 @@ int bias_chunks(const lpv_relpos* h, int64_t n_seq, int32_t H)
 }
 
 struct Ws {  // places in a gradient's workspace
-    float *bias, *bias_t, *D, *part, *sum, *sums;
+    float *bias, *bias_t, *D, *Dc, *part, *sum, *sums;
     size_t bytes;
 };
 Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
@@ -1724,6 +1753,7 @@ Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
     w.bias = take(window ? 0 : (size_t)(H * tile_floats(h)));
     w.bias_t = take(window || mid ? 0 : (size_t)(H * tile_floats(h)));
     w.D = take(window || mid ? 0 : (size_t)(n_seq * H * h->T));
+    w.Dc = take(window || mid ? 0 : (size_t)(n_seq * H * h->T));
     w.part = take((size_t)(H * chunks * tile_floats(h)));
     w.sum = chunks > 1 ? take((size_t)(H * tile_floats(h))) : w.part;
     w.sums = take((size_t)((int64_t)h->n_segs * H));
@@ -1815,13 +1845,17 @@ template <int DT, int HD, bool REG, typename Sh>
 hipError_t grad_tiles(const lpv_relpos* h, const RelposCall& c, const Ws& w, int chunks, hipStream_t s)
 {
     const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
-    const Gp g = {c.lse, w.D, (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, w.bias_t, w.part, chunks,
+    const Gp g = {c.lse, w.D, w.Dc, (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, w.bias_t, w.part, chunks,
                   LOG2E / sqrtf((float)HD), 1.0f / sqrtf((float)HD)};
     const int64_t n_tiles = c.n_seq * c.H * ((h->nt + Sh::QW - 1) / Sh::QW), n_blk = (h->nt + 1) / 2;
     const int64_t n_pairs = (int64_t)c.H * n_blk * n_blk * chunks;
-    const Grid2 grid = grid_of(2 * ((n_tiles + 7) / 8 * 8) + n_pairs);
-    hipLaunchKernelGGL((k_relpos_grad<DT, HD, Sh, REG>), dim3(grid.x, grid.y), dim3(256), 0, s, p, g,
-                       (uint32_t)n_tiles, (uint32_t)n_pairs);
+    const bool behind = h->T > h->n_buckets;  // (a full row has a bucket of several pairs)
+    const Grid2 t = grid_of(2 * ((n_tiles + 7) / 8 * 8) + (behind ? 0 : n_pairs)), q = grid_of(n_pairs);
+    hipLaunchKernelGGL((k_relpos_grad<DT, HD, Sh, REG>), dim3(t.x, t.y), dim3(256), 0, s, p, g, (uint32_t)n_tiles,
+                       behind ? 0u : (uint32_t)n_pairs);
+    if (behind)
+        hipLaunchKernelGGL((k_relpos_pairs<DT, HD, REG>), dim3(q.x, q.y), dim3(256), 0, s, p, g,
+                           (uint32_t)n_pairs);
     return hipGetLastError();
 }
 

@@ -419,13 +419,15 @@ def test_each_kernel_is_reached():
             (65, 3, 2, ("k_relpos_fwd<2,32", two, "mid_grad", "bias<2,0>"), ("window", "bias<2,32>")),
             (140, 80, 4, ("k_relpos_fwd<2,32", "Shape<3,1>", "mid_grad"), ("window", one, two)),
             (224, 70, 4, ("k_relpos_fwd<2,32", one, "mid_grad"), ("window", "k_relpos_grad")),
-            (225, 2, 2, ("k_relpos_grad<2,32", two, "bias<2,0>", "bias<2,32>"), (one, "mid_grad")),
+            (225, 2, 2, ("k_relpos_grad<2,32", two, "bias<2,0>", "bias<2,32>", "pairs"), (one, "mid_grad")),
             (225, 16, 4, ("k_relpos_grad<2,32", one, two, "bias<2,0>", "bias<2,32>"), ("mid_grad",))):
         got = names(T, n_seq, H)
         for n in there:
             assert any(n in g for g in got), (T, n, got)
         for n in absent:
             assert not any(n in g for g in got), (T, n, got)
+    c = Case(*window_index(16), 1, 1, 32, "bf16", seed=157)  # (more buckets than tokens)
+    assert not any("pairs" in n for n in kernels(lambda: c.grad(*c.forward())))
 
 
 @pytest.mark.parametrize("T,n_seq,H,labels", [(230, 20, 4, True), (230, 20, 4, False), (225, 37, 2, True)])
@@ -515,3 +517,26 @@ def test_two_streams_share_a_handle(T):
         for r in got[i]:
             for x, y in zip(r, ref[i]):
                 assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("T,n_seq,H", [(40, 3, 2), (230, 3, 2), (300, 2, 2), (520, 1, 1), (290, 17, 4)])
+def test_few_buckets_keep_the_tables_gradient(T, n_seq, H):
+    """Every bucket takes many pairs of each row, so an error of D would add up along the row: the
+    sums take D without the rounding of the outputs.  What is left: float32, and the rounding."""
+    say("relpos few buckets", T, n_seq, H)
+    c = Case(*line_index(T, 4), n_seq, H, 32, "bf16", seed=166)
+    out, lse = c.forward()
+    dtable = c.grad(out, lse)[1]
+    torch.cuda.synchronize()
+    r = ft.relpos_attention(c.x, c.t, c.idx, n_seq, H, 32, dout=c.g)
+    # a weight is off by f (the module's text); D, as the weights have it, by f and the sums'
+    # (T + 32) 2^-24 of sum_j P |dP|; twice that for D's two places
+    f = 2 * 34 * 2.0 ** -24 * r["abs_s"] + 2.0 ** -20 + 2.0 ** -22 * (1 + np.abs(r["lse"]))
+    P, dP, B = r["P"], r["dP"], r["abs_dP"]
+    size = (P * B).sum(3)
+    e = P * ((f + (T + 40) * 2.0 ** -24)[..., None] * (B + 3 * size[..., None]))
+    e_t = np.zeros(c.t.shape)
+    pairs = (e + (n_seq * T + 8) * 2.0 ** -24 * P * (B + size[..., None])).sum(0)
+    for h in range(H):
+        np.add.at(e_t[:, h], c.idx, pairs[h])
+    c.within(f64(dtable), r["dtable"], 1.02 * e_t + U["bf16"] * np.abs(r["dtable"]), "dtable")
