@@ -919,7 +919,7 @@ lpv_status lpv_relpos_create(const int32_t* index, int32_t T, int32_t n_buckets,
     const hipStream_t s = (hipStream_t)stream;
     RelposHost host;
     host.index = new (std::nothrow) int32_t[(size_t)T * T];
-    host.count = new (std::nothrow) int32_t[n_buckets];
+    host.count = new (std::nothrow) int32_t[2 * (size_t)n_buckets];
     if (!host.index || !host.count)
         return fail(LPV_ERR_ALLOC, "host allocation failed");
     hipError_t e = hipMemcpyAsync(host.index, index, (size_t)T * T * 4, hipMemcpyDeviceToHost, s);
@@ -927,7 +927,7 @@ lpv_status lpv_relpos_create(const int32_t* index, int32_t T, int32_t n_buckets,
         e = hipStreamSynchronize(s);
     if (e != hipSuccess)
         return hip_fail(e, "index copy");
-    const lpv::RelposSizes z = lpv::relpos_sizes(host.index, T, n_buckets, host.count);
+    const lpv::RelposSizes z = lpv::relpos_sizes(host.index, T, n_buckets, host.count, host.count + n_buckets);
     if (z.bad >= 0)
         return fail(LPV_ERR_INVALID_ARG, "index[%lld][%lld] = %d is outside [-1, %d)",
                     (long long)(z.bad / T), (long long)(z.bad % T), host.index[z.bad], n_buckets);
@@ -963,6 +963,7 @@ lpv_status lpv_relpos_create(const int32_t* index, int32_t T, int32_t n_buckets,
     h->nt = nt;
     h->n_buckets = n_buckets;
     h->n_segs = z.n_segs;
+    h->crowded = z.crowded;
     e = hipGetDevice(&h->device);
     if (e == hipSuccess)
         e = hipMemcpyAsync(h->mem, host.tables, bytes, hipMemcpyHostToDevice, s);

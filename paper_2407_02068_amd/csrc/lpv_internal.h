@@ -81,6 +81,8 @@ struct lpv_relpos {
     int32_t* order;
     int32_t* seg_ptr;     // n_segs + 1
     int32_t* bucket_seg;  // n_buckets + 1
+    // the tiles of rows (a bit each) with a row that gives some bucket two pairs or more
+    uint64_t crowded;
 };
 
 namespace lpv {
@@ -207,13 +209,15 @@ struct RelposCall {
     void* dtable;
     void* ws;
 };
-// The pairs and segments of an index, the pairs of each bucket (count), and the place of
-// the first entry outside [-1, n_buckets) (bad, -1 if there is none); host memory.
+// The pairs and segments of an index, its crowded tiles, the pairs of each bucket (count), and
+// the place of the first entry outside [-1, n_buckets) (bad, -1 if there is none); host memory
+// (last: n_buckets of scratch).
 struct RelposSizes {
     int64_t bad, n_pairs;
+    uint64_t crowded;
     int32_t n_segs;
 };
-RelposSizes relpos_sizes(const int32_t* index, int32_t T, int32_t n_buckets, int32_t* count);
+RelposSizes relpos_sizes(const int32_t* index, int32_t T, int32_t n_buckets, int32_t* count, int32_t* last);
 // The handle's arrays (host memory; count as relpos_sizes left it, overwritten).
 void relpos_tables(const int32_t* index, int32_t T, int32_t n_buckets, int32_t nt, int32_t* count,
                    uint16_t* idx, uint16_t* idx_t, int32_t* order, int32_t* seg_ptr,

@@ -1436,18 +1436,23 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // the tile before into dV^T = dO^T P and dK^T = Q^T dS over all queries.  So every score is
 // formed once, with five products, where the general kernels form it three times with nine.
 // LDS holds all rows of Q and dO, two key tiles and the two buffers.  D is dO . O with O as it
-// was rounded: a row's last tile alone would tell its error, when the others' dS are summed;
-// for tables of few buckets that makes the table's gradient off by 1.1 to 1.7 times its own
-// rounding (32 buckets, bf16), for others by nothing that shows.  Bound: LDS reads and
-// the chain of a tile at two waves to a SIMD (the sums leave registers for no more).  64 x
-// 197 tokens, 12 heads of 64: 72 us, 264 TFLOP/s; 256 x 144, 6 heads of 32, labels: 64 us.
+// was rounded, so that it is off by E = dO . (O's rounding) and dS_ij by P_ij E: a rounding like
+// others where a row's pairs go to distinct buckets, but a bucket that takes several pairs of a
+// row adds P_ij E over them while the sum of their dS cancels (a class token's row is one bucket: at
+// 197 tokens its gradient was off by 3% in bf16).  A row of dS sums to -E, which is known behind
+// its last tile: the waves of crowded tiles leave P, rounded once, in `kept` as they go and
+// then take P_ij times that sum off their sums (64 x 197 tokens, 12 heads of 64: 74 us without,
+// 77 for the class token's tile, 83 for all seven).  Bound: LDS reads and the chain of a tile at two
+// waves to a SIMD (the sums leave registers for no more).  64 x 197 tokens, 12 heads of 64: 247
+// TFLOP/s; 256 x 144, 6 heads of 32, labels: 64 us.
 constexpr int MID_TILES = 7;  // with the wave more two waves to a SIMD, which the sums' registers allow
 constexpr int MID_XS = 72;  // bytes of a row of P or dS, 32 keys: the writes of 32 rows' 8 bytes meet all banks
 template <int DT, int HD, bool REG>
 __global__ __launch_bounds__(64 * (MID_TILES + 1)) void k_relpos_mid_grad(
     Rp p, const uint16_t* __restrict__ out, int64_t ldo, const float* __restrict__ lse,
     const uint16_t* __restrict__ dout, int64_t ldg, uint16_t* __restrict__ dqkv, int64_t lddq,
-    float* __restrict__ part, int32_t per, int32_t slots, float scale, float rroot)
+    float* __restrict__ part, int32_t per, int32_t slots, uint32_t crowded, char* __restrict__ kept,
+    float scale, float rroot)
 {
     using E = Elem<DT>;
     using F = typename E::frag;
@@ -1539,6 +1544,10 @@ __global__ __launch_bounds__(64 * (MID_TILES + 1)) void k_relpos_mid_grad(
         return;
     }
     const int q = 32 * wave + l32;
+    // P of this wave's rows of a sequence: [key tile][r / 4][lane][r % 4], read by the lane that wrote it
+    const bool crowd = (crowded >> wave) & 1;
+    uint2* mine_p = (uint2*)kept +
+                    ((int64_t)wg * __popc(crowded) + __popc(crowded & ((1u << wave) - 1))) * nt * 256 + lane;
     const uint32_t qa = lds32(Qr) + q * RS + half * 16, ga = lds32(Gr) + q * RS + half * 16;
     for (uint32_t unit = u0; unit < u1;) {  // a head
         const uint32_t h = unit / seqs, end = min(u1, (h + 1) * seqs);
@@ -1547,6 +1556,13 @@ __global__ __launch_bounds__(64 * (MID_TILES + 1)) void k_relpos_mid_grad(
 #pragma unroll
         for (int b = 0; b < MID_TILES; ++b)
             sum[b] = f32x16{};
+        auto store_sum = [&](const f32x16& v, int kt) {  // to this workgroup's slot of the head
+            int at = 1024 * kt;
+            asm volatile("" : "+v"(at));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(float4*)(slot + at + 256 * i) = float4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+        };
         for (; unit < end; ++unit) {
             const int64_t seq = unit - h * seqs;
             const uint16_t* base = p.qkv + seq * T * ldq + h * HD;
@@ -1603,6 +1619,7 @@ __global__ __launch_bounds__(64 * (MID_TILES + 1)) void k_relpos_mid_grad(
             const int lab = REG && q < T ? max(reg[q], -1) : -1;
             const int mine = !REG ? 0 : lab < 0 ? NO_LABEL : lab;
             float D = 0.0f, nl = -INFINITY;
+            float miss = 0.0f;  // the sum of this lane's row of dS: -E
             F qf[KS], gf[KS];
             {
                 F of[KS];
@@ -1677,8 +1694,13 @@ __global__ __launch_bounds__(64 * (MID_TILES + 1)) void k_relpos_mid_grad(
                     db[2 * i] = pack2<DT>(f[0], f[1]);
                     db[2 * i + 1] = pack2<DT>(f[2], f[3]);
                     const int at = q * XS + (8 * i + 4 * half) * 2;
-                    *(uint2*)(x + at) = uint2{pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3])};
+                    const uint2 pb = {pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3])};
+                    *(uint2*)(x + at) = pb;
                     *(uint2*)(x + 32 * nt * XS + at) = uint2{db[2 * i], db[2 * i + 1]};
+                    if (crowd) {
+                        miss += (f[0] + f[1]) + (f[2] + f[3]);
+                        mine_p[(4 * kt + i) * 64] = pb;
+                    }
                 }
                 if (kt + 1 < nt) {
                     s = load_bias(bias + (kt + 1) * 1024);
@@ -1693,17 +1715,38 @@ __global__ __launch_bounds__(64 * (MID_TILES + 1)) void k_relpos_mid_grad(
                     for (int d = 0; d < ND; ++d)
                         dq[d] = E::mma(tr_frag<F, HD>(ktr, 16 * u, d), df, dq[d]);
                 }
-                if (unit + 1 == end) {  // the tile's sum is whole: to this workgroup's slot of the head
-                    float* dst = slot + kt * 1024;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *(float4*)(dst + 256 * i) = float4{sum[sk][4 * i], sum[sk][4 * i + 1], sum[sk][4 * i + 2],
-                                                           sum[sk][4 * i + 3]};
-                }
+                if (unit + 1 == end && !crowd)  // the tile's sum is whole
+                    store_sum(sum[sk], kt);
                 __syncthreads();
             }
             if (q < T)
                 store_rows<DT, HD>(dqkv + (seq * T + q) * lddq + h * HD, dq, rroot, half);
+            if (crowd) {
+                miss = half_add(miss);
+                uint2 pb[2][4];
+                auto load_p = [&](uint2* to, int kt) {
+                    int at = 256 * kt;
+                    asm volatile("" : "+v"(at));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        to[i] = mine_p[at + 64 * i];
+                };
+                load_p(pb[0], 0);
+#pragma unroll
+                for (int sk = 0; sk < MID_TILES; ++sk) {
+                    if (sk >= nt)
+                        break;
+                    load_p(pb[~sk & 1], sk + 1 < nt ? sk + 1 : sk);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const uint2 v = pb[sk & 1][r >> 2];
+                        sum[sk][r] -= Elem<DT>::to_f32((uint16_t)((r & 2 ? v.y : v.x) >> (16 * (r & 1)))) * miss;
+                    }
+                    if (unit + 1 == end)
+                        store_sum(sum[sk], sk);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
     }
 }
@@ -1721,6 +1764,11 @@ size_t mid_lds_bytes(int nt, int hd)
 }
 // Sequences of a head to a workgroup, one to a compute unit.
 int32_t mid_per(int64_t n_seq, int32_t H) { return (int32_t)((n_seq * H + 255) / 256); }
+int64_t mid_workgroups(int64_t n_seq, int32_t H)
+{
+    const int32_t per = mid_per(n_seq, H);
+    return (n_seq * H + per - 1) / per;
+}
 
 // Chunks of sequences of the bias gradient: 1024 workgroups, four to a compute unit.
 int bias_chunks(const lpv_relpos* h, int64_t n_seq, int32_t H)
@@ -1739,7 +1787,7 @@ int bias_chunks(const lpv_relpos* h, int64_t n_seq, int32_t H)
 }
 
 struct Ws {  // places in a gradient's workspace
-    float *bias, *bias_t, *D, *Dc, *part, *sum, *sums;
+    float *bias, *bias_t, *D, *Dc, *kept, *part, *sum, *sums;
     size_t bytes;
 };
 Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
@@ -1757,6 +1805,7 @@ Ws grad_ws(const lpv_relpos* h, int64_t n_seq, int32_t H, void* ws)
     w.bias_t = take(window || mid ? 0 : (size_t)(H * tile_floats(h)));
     w.D = take(window || mid ? 0 : (size_t)(n_seq * H * h->T));
     w.Dc = take(window || mid ? 0 : (size_t)(n_seq * H * h->T));
+    w.kept = take(mid && chunks ? (size_t)mid_workgroups(n_seq, H) * __builtin_popcountll(h->crowded) * h->nt * 512 : 0);
     w.part = take((size_t)(H * chunks * tile_floats(h)));
     w.sum = chunks > 1 ? take((size_t)(H * tile_floats(h))) : w.part;
     w.sums = take((size_t)((int64_t)h->n_segs * H));
@@ -1878,10 +1927,10 @@ hipError_t grad_mid(const lpv_relpos* h, const RelposCall& c, const Ws& w, int c
     }
     const Rp p = {(const uint16_t*)c.qkv, c.ldq, c.region, c.n_region, c.n_seq, h->T, c.H, h->nt, w.bias};
     const int32_t per = mid_per(c.n_seq, c.H);
-    hipLaunchKernelGGL((k_relpos_mid_grad<DT, HD, REG>), dim3((uint32_t)((c.n_seq * c.H + per - 1) / per)),
+    hipLaunchKernelGGL((k_relpos_mid_grad<DT, HD, REG>), dim3((uint32_t)mid_workgroups(c.n_seq, c.H)),
                        dim3(64 * (h->nt + 1)), mid_lds_bytes(h->nt, HD), s, p, (const uint16_t*)c.out, c.ldo, c.lse,
                        (const uint16_t*)c.dout, c.ldg, (uint16_t*)c.dqkv, c.lddq, w.part, per, chunks,
-                       LOG2E / sqrtf((float)HD), 1.0f / sqrtf((float)HD));
+                       (uint32_t)h->crowded, (char*)w.kept, LOG2E / sqrtf((float)HD), 1.0f / sqrtf((float)HD));
     return hipGetLastError();
 }
 
@@ -1935,19 +1984,30 @@ size_t relpos_workspace_bytes(const lpv_relpos* h, int64_t n_seq, int32_t H, boo
     return is_window(h) ? 0 : up256((size_t)(H * tile_floats(h)) * sizeof(float));
 }
 
-RelposSizes relpos_sizes(const int32_t* index, int32_t T, int32_t n_buckets, int32_t* count)
+RelposSizes relpos_sizes(const int32_t* index, int32_t T, int32_t n_buckets, int32_t* count, int32_t* last)
 {
     RelposSizes z = {};
     z.bad = -1;
-    for (int32_t b = 0; b < n_buckets; ++b)
+    for (int32_t b = 0; b < n_buckets; ++b) {
         count[b] = 0;
-    for (int64_t i = 0; i < (int64_t)T * T; ++i) {
-        if (index[i] < -1 || index[i] >= n_buckets) {
-            z.bad = i;
-            return z;
+        last[b] = -1;  // the last row with a pair of the bucket
+    }
+    for (int32_t i = 0; i < T; ++i) {
+        bool twice = false;
+        for (int32_t j = 0; j < T; ++j) {
+            const int32_t b = index[(int64_t)i * T + j];
+            if (b < -1 || b >= n_buckets) {
+                z.bad = (int64_t)i * T + j;
+                return z;
+            }
+            if (b >= 0) {
+                ++count[b];
+                twice |= last[b] == i;
+                last[b] = i;
+            }
         }
-        if (index[i] >= 0)
-            ++count[index[i]];
+        if (twice)
+            z.crowded |= (uint64_t)1 << (i / 32);
     }
     for (int32_t b = 0; b < n_buckets; ++b) {
         z.n_pairs += count[b];

@@ -540,3 +540,81 @@ def test_few_buckets_keep_the_tables_gradient(T, n_seq, H):
     for h in range(H):
         np.add.at(e_t[:, h], c.idx, pairs[h])
     c.within(f64(dtable), r["dtable"], 1.02 * e_t + U["bf16"] * np.abs(r["dtable"]), "dtable")
+
+
+def class_index(s):
+    """window_index(s, True): the first row gives one bucket all its pairs but one."""
+    return window_index(s, True)
+
+
+def diagonal_index(T):
+    return 1 - np.eye(T, dtype=np.int32), 2
+
+
+def between_steps(c):
+    """Values of 1 and, a quarter of them, one step of the type above: outputs lie a quarter of a
+    step above 1 and are rounded to it in every row, so that with gradients around 1 all rows' dout .
+    out are too small by about as much (bf16: 2^-9 of their size, far over what float32 leaves)."""
+    step, D = 2 * U[c.dtype], c.H * c.hd
+    r = np.random.default_rng(175)
+    c.x[:, 2 * D:] = 1 + step * (r.random((len(c.x), D)) < 0.25)
+    c.g[:] = 1 + 0.25 * r.integers(-2, 3, c.g.shape)
+    c.qkv[:, 2 * D:] = torch.from_numpy(c.x[:, 2 * D:])
+    c.dout[:] = torch.from_numpy(c.g)
+
+
+def table_bound(c, n_seq, H, r):
+    """What float32 leaves of the table's gradient (as in the test of few buckets): a weight is
+    off by f; D, as the weights have it, by f and the sums' (T + 32) 2^-24 of sum_j P |dP|; twice
+    that for D's two places."""
+    T, hd = c.T, c.hd
+    f = 2 * (hd + 2) * 2.0 ** -24 * r["abs_s"] + 2.0 ** -20 + 2.0 ** -22 * (1 + np.abs(r["lse"]))
+    P, B = r["P"], r["abs_dP"]
+    size = (P * B).sum(3)
+    e = P * ((f + (T + hd + 8) * 2.0 ** -24)[..., None] * (B + 3 * size[..., None]))
+    pairs = (e + (n_seq * T + 8) * 2.0 ** -24 * P * (B + size[..., None])).sum(0)
+    e_t = np.zeros(c.t.shape)
+    for h in range(H):
+        np.add.at(e_t[:, h], c.idx, pairs[h])
+    return 1.02 * e_t + U[c.dtype] * np.abs(r["dtable"]) + TINY[c.dtype]
+
+
+@pytest.mark.parametrize("index,T,n_seq,H,hd,dtype", [
+    ("line", 65, 5, 2, 32, "bf16"), ("line", 100, 3, 2, 32, "bf16"), ("line", 100, 70, 4, 64, "f16"),
+    ("line", 160, 2, 3, 64, "bf16"), ("line", 197, 9, 2, 32, "f16"), ("line", 224, 2, 2, 64, "bf16"),
+    ("diagonal", 70, 3, 2, 64, "bf16"), ("diagonal", 200, 4, 2, 32, "bf16"),
+    ("distances", 130, 4, 2, 32, "bf16")])
+def test_crowded_rows_keep_the_tables_gradient(index, T, n_seq, H, hd, dtype):
+    """Every row gives a bucket many of its pairs, or a few: an error of D would add up."""
+    say("relpos crowded rows", index, T, n_seq, H, hd, dtype)
+    idx, n = {"line": lambda: line_index(T, 4), "diagonal": lambda: diagonal_index(T),
+              "distances": lambda: (np.abs(line_index(T, 2 * T)[0] - T).astype(np.int32), T + 1)}[index]()
+    c = Case(idx, n, n_seq, H, hd, dtype, seed=170, q_std=0.3, edit=between_steps)
+    out, lse = c.forward()
+    dqkv, dtable = c.grad(out, lse)
+    torch.cuda.synchronize()
+    c.check(out, lse, dqkv, dtable)
+    r = ft.relpos_attention(c.x, c.t, c.idx, n_seq, H, hd, dout=c.g)
+    c.within(f64(dtable), r["dtable"], table_bound(c, n_seq, H, r), "dtable")
+
+
+@pytest.mark.parametrize("side,n_seq,H,hd,dtype", [
+    (8, 6, 2, 32, "bf16"), (10, 40, 3, 64, "bf16"), (14, 8, 3, 64, "bf16"), (14, 3, 2, 32, "f16")])
+def test_the_class_tokens_buckets_keep_their_gradient(side, n_seq, H, hd, dtype):
+    """The class token's row is one bucket, in a table of many more: its gradient is what little is
+    left of a row that sums to zero.  (Its label apart, the same with padding.)"""
+    idx, n = class_index(side)
+    T = len(idx)
+    say("relpos class token", side, n_seq, H, hd, dtype)
+    pad = np.zeros((2, T), np.int64)
+    pad[1, T - T // 3:] = -1
+    for region in (None, pad):
+        c = Case(idx, n, n_seq, H, hd, dtype, region=region, seed=171, q_std=0.3, edit=between_steps)
+        out, lse = c.forward()
+        dtable = c.grad(out, lse)[1]
+        torch.cuda.synchronize()
+        r = ft.relpos_attention(c.x, c.t, c.idx, n_seq, H, hd, region=region, dout=c.g)
+        r["lse"] = np.where(r["lse"] == -np.inf, 0.0, r["lse"])
+        bound = table_bound(c, n_seq, H, r)
+        row = [n - 3, n - 1]  # the buckets of the first row
+        c.within(f64(dtable)[row], r["dtable"][row], bound[row], "dtable's class token")
