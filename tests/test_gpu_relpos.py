@@ -582,8 +582,8 @@ def table_bound(c, n_seq, H, r):
 @pytest.mark.parametrize("index,T,n_seq,H,hd,dtype", [
     ("line", 65, 5, 2, 32, "bf16"), ("line", 100, 3, 2, 32, "bf16"), ("line", 100, 70, 4, 64, "f16"),
     ("line", 160, 2, 3, 64, "bf16"), ("line", 197, 9, 2, 32, "f16"), ("line", 224, 2, 2, 64, "bf16"),
-    ("diagonal", 70, 3, 2, 64, "bf16"), ("diagonal", 200, 4, 2, 32, "bf16"),
-    ("distances", 130, 4, 2, 32, "bf16")])
+    ("diagonal", 70, 3, 2, 64, "bf16"), ("diagonal", 200, 4, 2, 32, "bf16"), ("diagonal", 260, 3, 2, 32, "f16"),
+    ("distances", 130, 4, 2, 32, "bf16"), ("distances", 300, 4, 2, 32, "bf16")])
 def test_crowded_rows_keep_the_tables_gradient(index, T, n_seq, H, hd, dtype):
     """Every row gives a bucket many of its pairs, or a few: an error of D would add up."""
     say("relpos crowded rows", index, T, n_seq, H, hd, dtype)
@@ -599,7 +599,8 @@ def test_crowded_rows_keep_the_tables_gradient(index, T, n_seq, H, hd, dtype):
 
 
 @pytest.mark.parametrize("side,n_seq,H,hd,dtype", [
-    (8, 6, 2, 32, "bf16"), (10, 40, 3, 64, "bf16"), (14, 8, 3, 64, "bf16"), (14, 3, 2, 32, "f16")])
+    (8, 6, 2, 32, "bf16"), (10, 40, 3, 64, "bf16"), (14, 8, 3, 64, "bf16"), (14, 3, 2, 32, "f16"),
+    (15, 2, 2, 32, "bf16"), (17, 8, 2, 32, "bf16"), (23, 2, 1, 64, "f16")])
 def test_the_class_tokens_buckets_keep_their_gradient(side, n_seq, H, hd, dtype):
     """The class token's row is one bucket, in a table of many more: its gradient is what little is
     left of a row that sums to zero.  (Its label apart, the same with padding.)"""
@@ -618,3 +619,9 @@ def test_the_class_tokens_buckets_keep_their_gradient(side, n_seq, H, hd, dtype)
         bound = table_bound(c, n_seq, H, r)
         row = [n - 3, n - 1]  # the buckets of the first row
         c.within(f64(dtable)[row], r["dtable"][row], bound[row], "dtable's class token")
+
+
+def test_the_pairs_launch_is_for_crowded_rows():
+    """Past 224 tokens: a class token's row is one bucket, though the table is larger than the row."""
+    c = Case(*class_index(16), 1, 1, 32, "bf16", seed=172)
+    assert any("pairs" in n for n in kernels(lambda: c.grad(*c.forward())))
