@@ -352,12 +352,14 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill_row(Ds a)
 }
 
 // A chunk's maximum and sum: part[row][chunk] = (m, sum exp((z - m) / tau)).  The first
-// chunk's workgroup also leaves what the teacher's entries add to the loss (row_cross with
-// m = 0; a NaN for a row without any): the logits may be overwritten in the next launch.
+// chunk's workgroup also leaves what the teacher's entries add to the loss (a NaN for a row
+// without any): the logits may be overwritten in the next launch.  The row's maximum is not known
+// yet: row_cross is taken from the largest z of the entries, left beside it, so that only
+// differences of logits are formed and a common offset costs no accuracy.
 // Bound: the two launches.  4 rows of 131072 fp32 classes: 3.5 us and 6 for the second.
 template <int DT>
 __global__ __launch_bounds__(256) void k_distill_part(Ds a, int32_t chunks, int32_t per,
-                                                      float2* __restrict__ part, float* __restrict__ cross)
+                                                      float2* __restrict__ part, float2* __restrict__ cross)
 {
     using C = Chunk<DT>;
     __shared__ float red[4];
@@ -389,10 +391,22 @@ __global__ __launch_bounds__(256) void k_distill_part(Ds a, int32_t chunks, int3
     if (chunk == 0) {
         Teacher<256> e;
         load_teacher<DT, 256>(a, row, threadIdx.x, e, red, 0, a.V);
-        const float v = row_cross<256>(a, e, 0.0f, red);
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < Teacher<256>::KPT; ++i)
+            top = e.q[i] > 0.0f ? fmaxf(top, e.zi[i]) : top;
+        top = row_reduce<256, true>(top, red);
+        const float ref = top == -INFINITY ? 0.0f : top;  // (no entries, or left out by the student)
+        const float v = row_cross<256>(a, e, ref, red);
         if (threadIdx.x == 0)
-            cross[row] = e.some ? v : NAN;
+            cross[row] = float2{e.some ? v : NAN, ref};
     }
+}
+
+// The loss of a row from its (m, sum) and cross.
+__device__ inline float joined_loss(const Ds& a, float2 ml, float2 cross)
+{
+    return (cross.x + (ml.x - cross.y) * a.c + __log2f(ml.y)) * LN2 * a.tau * a.tau;
 }
 
 // (m, sum) of a row from its chunks'.
@@ -413,7 +427,7 @@ __device__ inline float2 join_parts(const Ds& a, const float2* part, int chunks,
 template <int DT>
 __global__ __launch_bounds__(256) void k_distill_join(Ds a, int32_t chunks, int32_t per,
                                                       const float2* __restrict__ part,
-                                                      const float* __restrict__ cross)
+                                                      const float2* __restrict__ cross)
 {
     using C = Chunk<DT>;
     __shared__ Shared<256> sh;
@@ -430,7 +444,7 @@ __global__ __launch_bounds__(256) void k_distill_join(Ds a, int32_t chunks, int3
     const float2 ml = join_parts(a, part + row * chunks, chunks, red);
     const float m = ml.x, l = ml.y;
     if (chunk == 0 && threadIdx.x == 0)
-        a.loss[row] = e.some ? (cross[row] + m * a.c + __log2f(l)) * LN2 * a.tau * a.tau : 0.0f;
+        a.loss[row] = e.some ? joined_loss(a, ml, cross[row]) : 0.0f;
     const char* z = a.z + row * a.ldz * C::ES;
     char* dz = a.dz + row * a.ldd * C::ES;
     const float w = (a.dloss ? a.dloss[row] : 1.0f) * a.tau, f = e.some ? w / l : 0.0f;
@@ -449,16 +463,16 @@ __global__ __launch_bounds__(256) void k_distill_join(Ds a, int32_t chunks, int3
 
 // The same for the loss alone.
 __global__ __launch_bounds__(256) void k_distill_loss(Ds a, int32_t chunks, const float2* __restrict__ part,
-                                                      const float* __restrict__ cross)
+                                                      const float2* __restrict__ cross)
 {
     __shared__ float red[4];
     const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (row >= a.M)
         return;
     const float2 ml = join_parts(a, part + row * chunks, chunks, red);
-    const float x = cross[row];
+    const float2 x = cross[row];
     if (threadIdx.x == 0)
-        a.loss[row] = x == x ? (x + ml.x * a.c + __log2f(ml.y)) * LN2 * a.tau * a.tau : 0.0f;
+        a.loss[row] = x.x == x.x ? joined_loss(a, ml, x) : 0.0f;
 }
 
 // How a call is cut: threads to a row in registers (0: chunks), chunks a row, 16-byte
@@ -526,7 +540,7 @@ template <int DT> hipError_t distill_as(const Ds& a, void* ws, hipStream_t s)
     }
     const Grid2 g = grid_of(a.M * cut.chunks);
     float2* part = (float2*)ws;
-    float* cross = (float*)(part + a.M * cut.chunks);
+    float2* cross = part + a.M * cut.chunks;
     hipLaunchKernelGGL((k_distill_part<DT>), dim3(g.x, g.y), dim3(256), 0, s, a, cut.chunks, cut.per, part,
                        cross);
     if (a.dz) {
@@ -546,7 +560,7 @@ size_t distill_workspace_bytes(int64_t M, int64_t V, int32_t k, int dtype)
     if (M == 0)
         return 0;
     const Cut cut = cut_of(M, V, k, dtype);
-    return cut.nt ? 0 : (size_t)M * (cut.chunks * sizeof(float2) + sizeof(float));
+    return cut.nt ? 0 : (size_t)M * (cut.chunks + 1) * sizeof(float2);
 }
 
 hipError_t launch_distill(const DistillCall& c, hipStream_t s)

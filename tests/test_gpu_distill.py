@@ -330,3 +330,47 @@ def test_two_streams():
     for i in range(2):
         for r in got[i]:
             assert torch.equal(r[0], ref[i][0]) and torch.equal(r[1], ref[i][1])
+
+
+@pytest.mark.parametrize("M,V,k,dtype,tau,offset", [
+    # rows in a wave's, a workgroup's and 1024 threads' registers, and rows cut into chunks
+    (6, 777, 20, "f32", 1.0, 30000.0), (6, 9000, 64, "f32", 2.0, -30000.0), (130, 60000, 30, "f32", 1.0, 30000.0),
+    (3, 70000, 64, "f32", 1.0, 30000.0), (2, 70001, 9, "f32", 4.0, -30000.0), (1, 131072, 128, "f32", 0.5, 1000.0),
+    (3, 70000, 64, "f16", 1.0, 1500.0), (6, 777, 20, "f16", 1.0, 1500.0)])
+def test_a_common_offset_of_the_logits_costs_nothing(M, V, k, dtype, tau, offset):
+    """p does not change with it, and the kernels take differences of the row's logits only: the
+    loss's error is made of their sizes, |log q| and d = (z_max - z) / tau, not of z's."""
+    def edit(c):
+        a = wl.quantize((c.z + offset).astype(np.float32), dtype)
+        c.z = oracle.decode(a, dtype).reshape(M, V)
+    c = Case(M, V, k, dtype, tau=tau, seed=186, std=1.0, edit=edit)
+    # (the teacher's logits are the student's own, but for a little: a loss near 0)
+    c.t = np.take_along_axis(c.z - offset, c.ids.astype(np.int64), 1).astype(np.float32)
+    c.t += np.random.default_rng(187).normal(0, 0.1, c.t.shape).astype(np.float32)
+    c.dev = (c.dev[0], torch.from_numpy(c.t).cuda())
+    say("distill offset", dtype, M, V, k, tau, offset)
+    loss, d = c.run()
+    alone = lpv.distill_loss(c.logits, *c.dev, tau)
+    want = ft.distill(c.z, c.ids, c.t, tau)
+    bound = np.zeros(M)
+    for r in range(M):
+        z, t = c.z[r] / tau, c.t[r].astype(np.float64) / tau
+        dz, dt = z.max() - z, t.max() - t
+        p = np.exp(-dz)
+        lp = np.log(p.sum())
+        q = np.exp(-dt)
+        lq = np.log(q.sum())
+        q /= q.sum()
+        p /= p.sum()
+        # the module's errors of a weight and of the two sums; a term of the cross sum holds
+        # -dt - lq and d, and behind it log sum: off by 2^-22 of each, and of up to 2^-20 of them by
+        # the sum over the entries (16 additions each)
+        e_sum = (p * 2.0 ** -22 * (2 + 2 * dz)).sum() + 2.0 ** -16
+        e_qs = (q * 2.0 ** -22 * (2 + 2 * dt)).sum() + 2.0 ** -18
+        at = c.ids[r]
+        size = dt + lq + dz[at] + lp
+        term = np.abs(-dt - lq + dz[at] + lp)
+        e = q * ((2.0 ** -22 * (2 + 2 * dt) + e_qs) * term + (2.0 ** -22 + 2.0 ** -20) * (size + 2))
+        bound[r] = tau ** 2 * (e.sum() + e_qs + e_sum) + 2.0 ** -22 * abs(want[r])
+    c.within(f64(loss), want, bound, "loss")
+    c.within(f64(alone), want, bound, "loss alone")
