@@ -532,8 +532,9 @@ lpv_status lpv_relpos_attention_grad(const lpv_relpos* p, const void* table, con
  *          has finished.  Needs no clearing.
  * Every element type; float32 inside, dlogits rounded once.  k in [1, 1024], V in
  * [1, 2^22], ldz, ldd multiples of 16 bytes and at most 2^22 elements, as is ldt.  Apart
- * from the above, non-finite inputs are outside the contract.  A call gives the same bits
- * every time.  No allocation, no host synchronisation.  M = 0 is a no-op.
+ * from the above, non-finite inputs are outside the contract (a NaN among a row's logits or
+ * entries makes its loss NaN).  A call gives the same bits every time.  No allocation, no host
+ * synchronisation.  M = 0 is a no-op.
  * Errors: INVALID_ARG, SHAPE, DTYPE, ALIAS, HIP.
  */
 lpv_status lpv_distill(const void* logits, int64_t ldz, int64_t M, int64_t V, lpv_dtype dt,

@@ -13,6 +13,7 @@
 // is worked out while the row's own loads are in flight.  Rows too long for registers, or
 // too few to fill the chip, are cut into chunks: one launch for each chunk's maximum and
 // sum, a second that joins a row's and forms the gradient.
+#include <float.h>
 #include <math.h>
 
 #include "lpv_device.h"
@@ -189,7 +190,8 @@ __device__ inline void load_teacher(const Ds& a, int64_t row, int tid, Teacher<N
                     e.zi[i] = C::load1(z, id);
             }
         }
-        top = fmaxf(top, tv[i]);
+        // (an entry's NaN leaves it an entry, and is the loss's)
+        top = fmaxf(top, e.id[i] < 0 ? -INFINITY : fmaxf(tv[i], -FLT_MAX));
     }
     top = row_reduce<NT, true>(top, red);
     e.some = top > -INFINITY;
@@ -261,7 +263,7 @@ template <int NT> __device__ inline float row_cross(const Ds& a, const Teacher<N
     float v = 0.0f;
 #pragma unroll
     for (int i = 0; i < Teacher<NT>::KPT; ++i)
-        if (e.q[i] > 0.0f)
+        if (e.q[i] != 0.0f)
             v += e.q[i] * (e.lq[i] - (e.zi[i] - m) * a.c);
     return row_reduce<NT, false>(v, red);
 }
@@ -352,10 +354,11 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill_row(Ds a)
 }
 
 // A chunk's maximum and sum: part[row][chunk] = (m, sum exp((z - m) / tau)).  The first
-// chunk's workgroup also leaves what the teacher's entries add to the loss (a NaN for a row
-// without any): the logits may be overwritten in the next launch.  The row's maximum is not known
-// yet: row_cross is taken from the largest z of the entries, left beside it, so that only
-// differences of logits are formed and a common offset costs no accuracy.
+// chunk's workgroup also leaves what the teacher's entries add to the loss: the logits may be
+// overwritten in the next launch.  The row's maximum is not known yet: row_cross is taken from
+// the largest z of the entries, left beside it (NaN for a row without any, which a maximum never
+// is: a NaN among the logits is the loss's), so that only differences of logits are formed and a
+// common offset costs no accuracy.
 // Bound: the two launches.  4 rows of 131072 fp32 classes: 3.5 us and 6 for the second.
 template <int DT>
 __global__ __launch_bounds__(256) void k_distill_part(Ds a, int32_t chunks, int32_t per,
@@ -399,7 +402,7 @@ __global__ __launch_bounds__(256) void k_distill_part(Ds a, int32_t chunks, int3
         const float ref = top == -INFINITY ? 0.0f : top;  // (no entries, or left out by the student)
         const float v = row_cross<256>(a, e, ref, red);
         if (threadIdx.x == 0)
-            cross[row] = float2{e.some ? v : NAN, ref};
+            cross[row] = float2{v, e.some ? ref : NAN};
     }
 }
 
@@ -472,7 +475,7 @@ __global__ __launch_bounds__(256) void k_distill_loss(Ds a, int32_t chunks, cons
     const float2 ml = join_parts(a, part + row * chunks, chunks, red);
     const float2 x = cross[row];
     if (threadIdx.x == 0)
-        a.loss[row] = x.x == x.x ? joined_loss(a, ml, x) : 0.0f;
+        a.loss[row] = x.y == x.y ? joined_loss(a, ml, x) : 0.0f;
 }
 
 // How a call is cut: threads to a row in registers (0: chunks), chunks a row, 16-byte

@@ -374,3 +374,26 @@ def test_a_common_offset_of_the_logits_costs_nothing(M, V, k, dtype, tau, offset
         bound[r] = tau ** 2 * (e.sum() + e_qs + e_sum) + 2.0 ** -22 * abs(want[r])
     c.within(f64(loss), want, bound, "loss")
     c.within(f64(alone), want, bound, "loss alone")
+
+
+@pytest.mark.parametrize("M,V", [(7, 1000), (7, 9000), (7, 120000)])
+def test_a_diverged_row_does_not_read_as_zero(M, V):
+    """A NaN among the student's logits, under one of the teacher's classes, beside them or
+    everywhere, or among the teacher's: the loss is NaN, alone and with the gradient; rows without
+    entries stay 0, and a class of the teacher's that the student leaves out is infinite."""
+    def edit(c):
+        c.z[0, c.ids[0, 2]] = np.nan
+        c.z[1] = np.nan
+        c.z[2, (c.ids[2].max() + 1) % V] = np.nan
+        c.z[3, c.ids[3]] = -np.inf
+        c.ids[4] = -1
+        c.z[4, 5] = np.nan
+        c.t[5, 3] = np.nan
+        c.t[6] = np.nan
+    c = Case(M, V, 12, "f32", seed=188, edit=edit)
+    alone = lpv.distill_loss(c.logits, *c.dev, c.tau)
+    loss, d = lpv.distill_grad(c.logits, *c.dev, c.tau, c.dloss)
+    torch.cuda.synchronize()
+    for x in (alone, loss):
+        assert bool(torch.isnan(x[[0, 1, 2, 5, 6]]).all()) and x[3] == float("inf") and x[4] == 0
+    assert not d[4].any()
