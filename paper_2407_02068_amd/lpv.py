@@ -650,7 +650,7 @@ def _distill(logits, ids, teacher, temperature, dloss, loss, dlogits, Vd, worksp
         dp, ldd = _rows(dlogits, "dlogits", M, dlogits.shape[-1], logits.dtype)
     else:
         dp, ldd = None, 0
-    if M == 1:  # (one row's stride says nothing: any that covers it)
+    if M <= 1:  # (one row's stride says nothing, nor does none's: any that covers it)
         pad = 16 // logits.element_size()
         ldz = ldd = (max(V, Vd) + pad - 1) // pad * pad
     wp, nbytes, keep = _workspace(workspace, distill_workspace_size(M, V, k, logits.dtype), logits.device,

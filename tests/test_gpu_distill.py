@@ -397,3 +397,15 @@ def test_a_diverged_row_does_not_read_as_zero(M, V):
     for x in (alone, loss):
         assert bool(torch.isnan(x[[0, 1, 2, 5, 6]]).all()) and x[3] == float("inf") and x[4] == 0
     assert not d[4].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [1, 10, 1003, 21841])
+def test_no_rows_of_any_number_of_classes(V, dtype):
+    z = torch.empty((0, V), dtype=TORCH[dtype], device="cuda")
+    ids, t = torch.empty((0, 3), dtype=torch.int32, device="cuda"), torch.empty((0, 3), device="cuda")
+    assert lpv.distill_loss(z, ids, t, 1.0).shape == (0,)
+    loss, d = lpv.distill_grad(z, ids, t, 1.0)
+    assert loss.shape == (0,) and d.shape == (0, V)
+    loss, d = lpv.distill_grad(z, ids, t, 1.0, dlogits=z)
+    assert d is z
