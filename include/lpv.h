@@ -461,8 +461,8 @@ lpv_status lpv_relpos_workspace_size(const lpv_relpos* p, int64_t n_seq, int32_t
  *         s % n_region.  Tokens attend to tokens of the same label only (the parts of a
  *         shifted window); a token with a negative label is padding: it attends to
  *         nothing, nothing attends to it, and its values are not used (they may be NaN).
- * out     device, (n_seq T) x (H hd), row stride ldo; must not overlap qkv.  A row that
- *         no pair is left for is zero.
+ * out     device, (n_seq T) x (H hd), row stride ldo; neither it nor lse overlaps an input
+ *         or the other.  A row that no pair is left for is zero.
  * lse     device, n_seq x H x T float32, or NULL: receives log sum_j exp(s_ij) (-inf for a
  *         row without pairs), for the gradient.
  * workspace  device, 16-byte aligned, at least lpv_relpos_workspace_size bytes (may be

@@ -1012,8 +1012,11 @@ lpv_status lpv_relpos_attention(const lpv_relpos* p, const void* table, const vo
         return LPV_OK;
     const int64_t D = (int64_t)H * hd, M = n_seq * p->T;
     const int64_t nq = ((M - 1) * ldq + 3 * D) * 2, no = ((M - 1) * ldo + D) * 2, nl = M * H * 4;
-    if (overlap(out, no, qkv, nq) || (lse && (overlap(lse, nl, qkv, nq) || overlap(lse, nl, out, no))))
-        return fail(LPV_ERR_ALIAS, "qkv, out and lse must not overlap");
+    const int64_t nt = (int64_t)p->n_buckets * H * 2, nr = region ? n_region * p->T * 4 : 0;
+    if (overlap(out, no, qkv, nq) || overlap(out, no, table, nt) || overlap(out, no, region, nr) ||
+        (lse && (overlap(lse, nl, qkv, nq) || overlap(lse, nl, out, no) || overlap(lse, nl, table, nt) ||
+                 overlap(lse, nl, region, nr))))
+        return fail(LPV_ERR_ALIAS, "out and lse must not overlap an input or each other");
     st = check_relpos_device(p, n_seq, H, false, workspace, workspace_bytes);
     if (st != LPV_OK)
         return st;
@@ -1051,19 +1054,22 @@ lpv_status lpv_relpos_attention_grad(const lpv_relpos* p, const void* table, con
                                          "and at most 2^22");
     if (!dtable || (uintptr_t)dtable % 2)
         return fail(LPV_ERR_INVALID_ARG, "dtable must be non-NULL and aligned to its element size");
+    const int64_t nt = (int64_t)p->n_buckets * H * 2, nr = region ? n_region * p->T * 4 : 0;
+    bool alias = overlap(dtable, nt, table, nt) || overlap(dtable, nt, region, nr);
     if (n_seq > 0) {
         if (!lse || (uintptr_t)lse % 4 || !dout || !dqkv || !aligned16(dout) || !aligned16(dqkv))
             return fail(LPV_ERR_INVALID_ARG, "lse, dout and dqkv must be non-NULL and aligned to 4, 16 "
                                              "and 16 bytes");
         const int64_t nq = ((M - 1) * ldq + 3 * D) * 2, no = ((M - 1) * ldo + D) * 2;
         const int64_t ng = ((M - 1) * ldg + D) * 2, nd = ((M - 1) * lddq + 3 * D) * 2;
-        const int64_t nt = (int64_t)p->n_buckets * H * 2, nl = M * H * 4;
-        if (overlap(dqkv, nd, qkv, nq) || overlap(dqkv, nd, out, no) || overlap(dqkv, nd, dout, ng) ||
-            overlap(dqkv, nd, lse, nl) || overlap(dqkv, nd, table, nt) || overlap(dqkv, nd, dtable, nt) ||
-            overlap(dtable, nt, qkv, nq) || overlap(dtable, nt, out, no) || overlap(dtable, nt, dout, ng) ||
-            overlap(dtable, nt, lse, nl))
-            return fail(LPV_ERR_ALIAS, "dqkv and dtable must not overlap an input or each other");
+        const int64_t nl = M * H * 4;
+        alias |= overlap(dqkv, nd, qkv, nq) || overlap(dqkv, nd, out, no) || overlap(dqkv, nd, dout, ng) ||
+                 overlap(dqkv, nd, lse, nl) || overlap(dqkv, nd, table, nt) || overlap(dqkv, nd, dtable, nt) ||
+                 overlap(dqkv, nd, region, nr) || overlap(dtable, nt, qkv, nq) || overlap(dtable, nt, out, no) ||
+                 overlap(dtable, nt, dout, ng) || overlap(dtable, nt, lse, nl);
     }
+    if (alias)
+        return fail(LPV_ERR_ALIAS, "dqkv and dtable must not overlap an input or each other");
     st = check_relpos_device(p, n_seq, H, true, workspace, workspace_bytes);
     if (st != LPV_OK)
         return st;

@@ -145,3 +145,32 @@ def test_distill_without_rows_and_its_workspace(L):
     assert size(0, 100000) == OK and b.value == 0
     assert size(2, 0) == SHAPE and size(-1, 5) == SHAPE and size(2, 5, 0) == SHAPE and size(2, 5, 4, 7) == DTYPE
     assert L.lpv_distill_workspace_size(2, 5, 4, 2, None) == INVALID
+
+
+# 49 tokens x 4 windows of labels; 169 buckets x 3 heads of 2 bytes
+REGION = dict(region=FAKE + 4 * G, nr=4)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(out=FAKE), dict(out=FAKE - 4 * 49 * 96 * 2 + 16), dict(lse=FAKE + 169 * 6 - 6),
+    dict(out=FAKE + 4 * G, **REGION), dict(out=FAKE + 4 * G + 4 * 49 * 4 - 16, **REGION),
+    dict(lse=FAKE + 4 * G + 4 * 49 * 4 - 4, **REGION)])
+def test_relpos_attention_refuses_outputs_over_what_it_reads(L, kw):
+    assert attention(L, **kw) == ALIAS
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtable=FAKE), dict(dtable=FAKE + 169 * 6 - 2), dict(dtable=FAKE - 169 * 6 + 2),
+    dict(dtable=FAKE, n=0), dict(dtable=FAKE + 4 * G + 4 * 49 * 4 - 4, **REGION),
+    dict(dqkv=FAKE + 4 * G, **REGION), dict(dqkv=FAKE + 4 * G + 4 * 49 * 4 - 16, **REGION), dict(dqkv=FAKE)])
+def test_relpos_grad_refuses_outputs_over_what_it_reads(L, kw):
+    assert grad(L, **kw) == ALIAS
+
+
+def test_neighbours_are_not_overlaps(L):
+    """Right beside the table or the labels: not ALIAS (what refuses is the missing workspace)."""
+    table = dict(dtable=FAKE + 169 * 6)
+    labels = dict(dqkv=FAKE + 4 * G + 4 * 49 * 4, **REGION)
+    assert (4 * 49 * 4) % 16 == 0
+    for kw in (table, labels, dict(dtable=FAKE + 4 * G + 4 * 49 * 4, **REGION)):
+        assert grad(L, wsb=16, **kw) == INVALID
