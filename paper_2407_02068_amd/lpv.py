@@ -477,7 +477,7 @@ def _rows(t, name, M, cols, dtype):
     ld, unit = t.stride()
     if cols > 1 and unit != 1:
         raise ValueError("%s must have unit stride along its columns" % name)
-    return t.data_ptr(), ld if M > 1 else max(ld, cols)
+    return t.data_ptr(), ld if M > 1 else cols  # (nor does one row's)
 
 
 class RelPos:

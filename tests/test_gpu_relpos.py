@@ -625,3 +625,22 @@ def test_the_pairs_launch_is_for_crowded_rows():
     """Past 224 tokens: a class token's row is one bucket, though the table is larger than the row."""
     c = Case(*class_index(16), 1, 1, 32, "bf16", seed=172)
     assert any("pairs" in n for n in kernels(lambda: c.grad(*c.forward())))
+
+
+def test_one_row_of_any_stride():
+    """A matrix of one row has no stride to speak of: that of a slice of a wider tensor is not
+    looked at."""
+    c = Case(np.zeros((1, 1), np.int32), 1, 1, 2, 32, "bf16", seed=173)
+    ref = c.run()
+    D = 64
+    room = torch.full((2, 3 * D + 9), 5.0, dtype=torch.bfloat16, device="cuda")
+    far = torch.full((1, 2 ** 22 + 24), 5.0, dtype=torch.bfloat16, device="cuda")
+    qkv, dqkv = room[:1, :3 * D], far[:, 8:8 + 3 * D]
+    qkv.copy_(c.qkv)
+    lse = torch.empty((1, 2, 1), device="cuda")
+    out = lpv.relpos_attention(c.rp, c.table, qkv, 1, 2, lse=lse, hd=32)
+    dtable = lpv.relpos_attention_grad(c.rp, c.table, qkv, out, lse, c.dout, 1, 2, dqkv=dqkv, hd=32)[1]
+    torch.cuda.synchronize()
+    for a, b in zip((out, lse, dqkv, dtable), ref):
+        assert torch.equal(a, b)
+    assert (far[:, :8] == 5).all() and (far[:, 8 + 3 * D:] == 5).all()
