@@ -50,8 +50,8 @@ class EncoderChain:
     linears: 4 * blocks Linear objects in the order (qkv, proj, fc1, fc2) per
     block; gamma, beta: the layer norms' D-element parameters.  relpos (a
     lpv.RelPos of T tokens) with tables (one n_buckets x H table per block):
-    attention with that position bias; region: its labels, as
-    lpv.relpos_attention takes them."""
+    attention with that position bias, heads of D / H = 32 or 64 dimensions (64
+    without); region: its labels, as lpv.relpos_attention takes them."""
 
     def __init__(self, linears, n_seq, T, H, gamma, beta, eps=1e-6, relpos=None, tables=None,
                  region=None):
@@ -116,7 +116,8 @@ class EncoderChain:
                 lpv.attention(qkv, self.n_seq, self.T, self.H, out=O)
             else:
                 lpv.relpos_attention(self.relpos, self.tables[blk], qkv, self.n_seq, self.H,
-                                     region=self.region, out=O, workspace=self.relpos_ws)
+                                     region=self.region, out=O, workspace=self.relpos_ws,
+                                     hd=self.D // self.H)
             if trace:
                 trace("%d.attention" % blk, {"qkv": qkv}, O)
             lin(pr, O, P)

@@ -230,3 +230,55 @@ def test_encoder_chain_with_a_position_bias(side, class_token, n_seq, labels):
     with pytest.raises(ValueError):
         EncoderChain(chain.linears, n_seq, T - 1, H, chain.gamma, chain.beta, relpos=rp, tables=tables)
     chain.close()
+
+
+def check_chain(H, regions, region):
+    """A chain of 768 / H dimensions to a head: every attention against the oracle on its own input
+    and its block's labels, and graph replays."""
+    n_seq, T, blocks, hd = 2, 40, len(regions), 768 // H
+    idx, n = line_index(T, 16)
+    layers = wl.b_stack(M=n_seq * T, layers=blocks)
+    bits = [wl.quantize(wl.rng(126, i, 50).normal(0, 0.5, (n, H)).astype(np.float32), "bf16")
+            for i in range(blocks)]
+    tables = [dev(b, "bf16") for b in bits]
+    rp = lpv.relpos(torch.from_numpy(idx).cuda(), n)
+    chain = deit_chain(layers, lambda a: dev(a, "bf16"), n_seq, T, H, relpos=rp, tables=tables, region=region)
+    seen = []
+
+    def trace(name, ins, out):
+        if not name.endswith("attention"):
+            return
+        torch.cuda.synchronize()
+        blk = int(name.split(".")[0])
+        x = oracle.decode(host(ins["qkv"], "bf16"), "bf16").reshape(n_seq * T, -1)
+        t = oracle.decode(bits[blk], "bf16").reshape(n, H)
+
+        def edit(c):
+            c.x, c.t = x, t
+
+        c = Attention(idx, n, n_seq, H, hd, "bf16", region=regions[blk], edit=edit)
+        lse = torch.empty((n_seq, H, T), device="cuda")
+        again = lpv.relpos_attention(rp, tables[blk], ins["qkv"], n_seq, H, region=c.reg, lse=lse, hd=hd)
+        assert torch.equal(again, out)
+        c.check(out, lse)
+        seen.append(blk)
+    x0 = dev(layers[0].X, "bf16")
+    x, A = chain.run(x0, trace=trace)
+    torch.cuda.synchronize()
+    assert seen == list(range(blocks))
+    ref = x.clone(), A.clone()
+    graph, (xg, Ag) = chain.capture(x0)
+    for _ in range(3):
+        chain.run(x0, sparse=False)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(xg, ref[0]) and torch.equal(Ag, ref[1])
+    return chain, rp, tables
+
+
+@pytest.mark.parametrize("H", [12, 24])
+def test_encoder_chain_of_other_heads(H):
+    """The position bias with heads of 64 and of 32 dimensions."""
+    say("encoder chain", H, "heads")
+    check_chain(H, [None, None], None)[0].close()
