@@ -51,7 +51,9 @@ class EncoderChain:
     block; gamma, beta: the layer norms' D-element parameters.  relpos (a
     lpv.RelPos of T tokens) with tables (one n_buckets x H table per block):
     attention with that position bias, heads of D / H = 32 or 64 dimensions (64
-    without); region: its labels, as lpv.relpos_attention takes them."""
+    without); region: its labels, as lpv.relpos_attention takes them, or a list
+    of them, one for each block (None: a block without), as plain and shifted
+    windows alternate."""
 
     def __init__(self, linears, n_seq, T, H, gamma, beta, eps=1e-6, relpos=None, tables=None,
                  region=None):
@@ -62,6 +64,8 @@ class EncoderChain:
         if relpos is not None and (relpos.T != T or tables is None
                                    or len(tables) * 4 != len(linears)):
             raise ValueError("relpos of T tokens, with one table per block")
+        if isinstance(region, (list, tuple)) and len(region) * 4 != len(linears):
+            raise ValueError("one region for all blocks, or one for each")
         self.linears, self.n_seq, self.T, self.H = linears, n_seq, T, H
         self.gamma, self.beta, self.eps = gamma, beta, eps
         D = linears[0].W.shape[1]
@@ -115,8 +119,9 @@ class EncoderChain:
             if self.relpos is None:
                 lpv.attention(qkv, self.n_seq, self.T, self.H, out=O)
             else:
+                region = self.region[blk] if isinstance(self.region, (list, tuple)) else self.region
                 lpv.relpos_attention(self.relpos, self.tables[blk], qkv, self.n_seq, self.H,
-                                     region=self.region, out=O, workspace=self.relpos_ws,
+                                     region=region, out=O, workspace=self.relpos_ws,
                                      hd=self.D // self.H)
             if trace:
                 trace("%d.attention" % blk, {"qkv": qkv}, O)

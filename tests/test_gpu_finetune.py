@@ -282,3 +282,17 @@ def test_encoder_chain_of_other_heads(H):
     """The position bias with heads of 64 and of 32 dimensions."""
     say("encoder chain", H, "heads")
     check_chain(H, [None, None], None)[0].close()
+
+
+def test_encoder_chain_with_labels_by_block():
+    """The plain and the shifted windows of a row of tokens in turn, and all tokens in a block without
+    labels."""
+    at = np.arange(40)
+    regions = [(at // 8)[None], None, np.stack([(at + 4) // 8, np.where(at < 30, (at + 4) // 8, -1)])]
+    regs = [None if r is None else torch.from_numpy(r.astype(np.int32)).cuda() for r in regions]
+    say("encoder chain, labels by block")
+    chain, rp, tables = check_chain(24, regions, regs)
+    for bad in (regs[:2], regs + [None], []):
+        with pytest.raises(ValueError):
+            EncoderChain(chain.linears, 2, 40, 24, chain.gamma, chain.beta, relpos=rp, tables=tables, region=bad)
+    chain.close()
