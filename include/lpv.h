@@ -493,10 +493,11 @@ lpv_status lpv_relpos_attention(const lpv_relpos* p, const void* table, const vo
  * dtable  device, n_buckets x H: receives the bias's gradient (not added to; zero for
  *         buckets without pairs and where n_seq = 0).
  * dqkv and dtable overlap neither an input nor each other.  rowsum(P dP) is taken as dout .
- * out, with out as rounded (up to 64 tokens, and for dtable in the 32 rows, or past 224 tokens
- * all, beside one that gives some bucket several pairs, without that rounding).  P and dS are rounded once to the element type for the products; the sums over sequences and pairs are float32 in a
- * fixed order, rounded once.  Types, sizes, strides and workspace as above.  No allocation,
- * no host synchronisation.
+ * out, with out as rounded; without that rounding up to 64 tokens, and for dtable where a row
+ * gives some bucket several pairs (from 65 to 224 tokens: in that row's tile of 32).  P and dS are
+ * rounded once to the element type for the products (fp16: |dS| past 65504 is infinite); the
+ * sums over sequences and pairs are float32 in a fixed order, rounded once.  Types, sizes,
+ * strides and workspace as above.  No allocation, no host synchronisation.
  * Errors: INVALID_ARG, SHAPE, DTYPE, ALIAS, HIP.
  */
 lpv_status lpv_relpos_attention_grad(const lpv_relpos* p, const void* table, const void* qkv,

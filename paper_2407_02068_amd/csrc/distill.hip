@@ -285,8 +285,9 @@ __device__ inline void fix_entries(const Ds& a, const Teacher<NT>& e, char* dz, 
 }
 
 // Rows in registers: NT threads to a row (a wave's rows four to a workgroup), NC chunks of
-// 16 bytes to a thread.  Bound: HBM.  The loss of 16384 rows of 1000 fp16 classes: 11 us, 3.0
-// TB/s; with the gradient, 2048 rows of 21841 bf16 classes: 41 us, 4.4 TB/s.
+// 16 bytes to a thread.  Bound: HBM where a row has many loads in flight (with the gradient, 2048
+// rows of 21841 bf16 classes: 41 us, 4.4 TB/s), else a row's one round trip (the loss of 16384
+// rows of 1000 fp16 classes: 11 us, 3.0 TB/s).
 template <int DT, int NT, int NC>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill_row(Ds a)
 {
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_distill_row(Ds a)
 // the largest z of the entries, left beside it (NaN for a row without any, which a maximum never
 // is: a NaN among the logits is the loss's), so that only differences of logits are formed and a
 // common offset costs no accuracy.
-// Bound: the two launches.  4 rows of 131072 fp32 classes: 3.5 us and 6 for the second.
+// Bound: the two launches.  4 rows of 131072 fp32 classes: 4 us and 6 for the second.
 template <int DT>
 __global__ __launch_bounds__(256) void k_distill_part(Ds a, int32_t chunks, int32_t per,
                                                       float2* __restrict__ part, float2* __restrict__ cross)

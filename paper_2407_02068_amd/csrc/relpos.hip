@@ -911,9 +911,9 @@ __device__ inline void grad_bias(const Rp& p, const Gp& c, const float* Dv, uint
 // All gradients of longer sequences in one launch, so that its parts fill the chip together:
 // workgroups of dQ, then of dK and dV, then (unless n_pairs is 0) of the bias's.  Nine products
 // of T^2 hd in all, of which five would do where dS could stay in registers.  Bound: chains of
-// dependent steps at two waves to a SIMD (registers).  4 x 777 tokens, 8 heads of 64: 52 us, 428
-// TFLOP/s of the nine; in a launch each they made forward and gradients 115 us long, together
-// 107.
+// dependent steps at two waves to a SIMD (registers).  4 x 777 tokens, 8 heads of 64, distinct
+// buckets along a row: 51 us, 435 TFLOP/s of the nine; in a launch each the parts made forward and
+// gradients 115 us long, together 107.  With 32 buckets, whose sums follow: 36 and 18 us.
 template <int DT, int HD, typename Sh, bool REG>
 __global__ __launch_bounds__(256, 2) void k_relpos_grad(Rp p, Gp c, uint32_t n_tiles, uint32_t n_pairs)
 {
@@ -1444,7 +1444,7 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // then take P_ij times that sum off their sums (64 x 197 tokens, 12 heads of 64: 74 us without,
 // 77 for the class token's tile, 83 for all seven).  Bound: LDS reads and the chain of a tile at two
 // waves to a SIMD (the sums leave registers for no more).  64 x 197 tokens, 12 heads of 64: 247
-// TFLOP/s; 256 x 144, 6 heads of 32, labels: 64 us.
+// TFLOP/s; 256 x 144, 6 heads of 32, labels: 66 us.
 constexpr int MID_TILES = 7;  // with the wave more two waves to a SIMD, which the sums' registers allow
 constexpr int MID_XS = 72;  // bytes of a row of P or dS, 32 keys: the writes of 32 rows' 8 bytes meet all banks
 template <int DT, int HD, bool REG>
@@ -1833,10 +1833,11 @@ hipError_t expand_bias(const lpv_relpos* h, const void* table, int32_t H, int32_
 
 // The general kernels' layout: a wave to a 32-row tile, four tiles to a workgroup; where
 // that leaves the chip with few waves, two waves to a tile: `few` below six tiles to a
-// compute unit in the forward pass, below two in the gradients, whose other parts fill the
-// chip.  (us of the call, two waves / one, 600 tokens, 8 heads of 64: forward 20.6 / 23.8 with
-// 304 tiles, 27.5 / 28.5 with 1216, 37.4 / 36.7 with 1976; gradients 49.7 / 51.1 with 304,
-// 62.0 / 57.1 with 608, 122 / 108 with 1976.  Four waves to a tile: 777 tokens, 4 sequences,
+// compute unit in the forward pass, below two in the gradients, of which there are two kinds of
+// workgroups.  (us of the call, two waves / one, 600 tokens, 8 heads of 64: forward 20.6 / 23.8 with
+// 304 tiles, 27.5 / 28.5 with 1216, 37.4 / 36.7 with 1976; gradients with the bias's sums behind
+// 55.7 / 57.0 with 304, 58.3 / 59.6 with 456, 69.2 / 67.0 with 608, 132 / 121 with 1976; beside
+// them 51.2 / 52.9, 58.2 / 53.9, 64.1 / 59.2 and 127 / 111.  Four waves to a tile: 777 tokens, 4 sequences,
 // 8 heads, the forward kernel 26.8 against 19.8.)
 bool few_tiles(const lpv_relpos* h, const RelposCall& c, int64_t few) { return c.n_seq * c.H * h->nt < few; }
 
