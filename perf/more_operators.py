@@ -127,9 +127,9 @@ def prepare(case, seed):
     if own:
         from paper_2407_02068_amd import lpv
         if mask is None:
-            s["h"] = lpv.q8_pack(w, ws)
+            s["h"] = lpv.quant_pack(w, ws)
         else:
-            s["h"] = lpv.q8_pack(w, ws, mask, c["b_r"], c["b_c"])
+            s["h"] = lpv.quant_pack(w, ws, mask, c["b_r"], c["b_c"])
     return s
 
 
@@ -146,17 +146,17 @@ def _own_rows(s):
     norm, x, y = s["case"]["norm"], s["x"], s["y"]
     S = torch.empty_like(x) if y is not None else None
     if norm == "rms":
-        q, scale = lpv.add_rmsnorm_q8(x, y, s["gamma"], EPS, S=S)
+        q, scale = lpv.add_rmsnorm_quant(x, y, s["gamma"], EPS, S=S)
     elif norm == "layer":
-        q, scale = lpv.add_layernorm_q8(x, y, s["gamma"], s["beta"], EPS, S=S)
+        q, scale = lpv.add_layernorm_quant(x, y, s["gamma"], s["beta"], EPS, S=S)
     else:
-        q, scale = lpv.rows_q8(x, y, S=S)
+        q, scale = lpv.quant_rows(x, y, S=S)
     return {"values": torch.mul(q, scale[:, None]), "scale": scale, "sum": S}
 
 
 def _own_linear(s):
     from paper_2407_02068_amd import lpv
-    return lpv.q8_linear(s["h"], s["x"], s["xs"], s["bias"], epi="gelu" if s["case"]["gelu"] else None)
+    return lpv.quant_linear(s["h"], s["x"], s["xs"], s["bias"], epi="gelu" if s["case"]["gelu"] else None)
 
 
 def _plain_rows(s):
