@@ -547,6 +547,111 @@ lpv_status lpv_distill(const void* logits, int64_t ldz, int64_t M, int64_t V, lp
  * Errors: INVALID_ARG, SHAPE, DTYPE. */
 lpv_status lpv_distill_workspace_size(int64_t M, int64_t V, int32_t k, lpv_dtype dt, size_t* bytes);
 
+/* ------------------------------------------------------------------------
+ * Serving the pruned model in 8 bits: rows in 8-bit codes with a scale for each (what the
+ * encoder block's norms, attention and GELU hand to the linear layers), and the linear layer
+ * over 8-bit codes, over the kept blocks or dense.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * lpv_quant_rows -- rows in 8-bit codes: per row of M rows of D elements, u = x + y (y may be
+ * NULL: u = x), and
+ *   m = max_j |u_j|,  scale = m / 127,  q_j = rint(127 u_j / m)   (ties to even),
+ * codes of -127 .. 127 of which u_j is q_j scale to half a step.  In float64 inside: the
+ * codes are those of the exact quotient, the scale is rounded once to float32.  A row of zeros
+ * has scale 0 and codes 0; a row with a NaN or an infinity has scale NaN and codes 0.
+ * x, y   device, M x D, row strides ldx, ldy.
+ * S      device, M x D, row stride lds, or NULL: receives u, rounded to dt.  May be x or y
+ *        itself (same address and stride).
+ * q      device, int8 M x D, row stride ldq.
+ * scale  device, float32, M elements.
+ * Every element type, 1 <= D <= 32768, strides in [D, 2^22] (of one row too), addresses aligned to
+ * their element; rows of a multiple of 8 elements with strides that are multiples of 8 and
+ * 16-byte aligned addresses (q: 8-byte) go fastest.  No allocation, no host
+ * synchronisation; M = 0 is a no-op.  A call gives the same bits every time.
+ * Errors: INVALID_ARG, SHAPE, DTYPE, ALIAS, HIP.
+ */
+lpv_status lpv_quant_rows(const void* x, int64_t ldx, const void* y, int64_t ldy, int64_t M, int64_t D,
+                          lpv_dtype dt, void* S, int64_t lds, int8_t* q, int64_t ldq, float* scale,
+                          void* stream);
+
+/*
+ * lpv_add_rmsnorm_quant -- the residual's addition and a root-mean-square norm, in 8-bit
+ * codes: s = x + y,
+ *   u = s / sqrt(mean(s^2) + eps) * gamma,
+ * then codes and scale of u as lpv_quant_rows gives them (the norm's factor divides out of the
+ * codes, which are those of s * gamma).  S receives s.  gamma: device, D elements of
+ * type dt; eps finite and >= 0.  The rest, and the errors, as lpv_quant_rows.
+ */
+lpv_status lpv_add_rmsnorm_quant(const void* x, int64_t ldx, const void* y, int64_t ldy, int64_t M,
+                                 int64_t D, lpv_dtype dt, const void* gamma, double eps, void* S,
+                                 int64_t lds, int8_t* q, int64_t ldq, float* scale, void* stream);
+
+/*
+ * lpv_add_layernorm_quant -- lpv_add_layernorm in 8-bit codes: s = x + y,
+ *   u = (s - mean(s)) / sqrt(var(s) + eps) * gamma + beta,
+ * var the biased variance, then codes and scale of u as lpv_quant_rows gives them.  S
+ * receives s.  The rest, and the errors, as lpv_add_rmsnorm_quant.
+ */
+lpv_status lpv_add_layernorm_quant(const void* x, int64_t ldx, const void* y, int64_t ldy, int64_t M,
+                                   int64_t D, lpv_dtype dt, const void* gamma, const void* beta,
+                                   double eps, void* S, int64_t lds, int8_t* q, int64_t ldq,
+                                   float* scale, void* stream);
+
+/* A weight in 8-bit codes, packed for lpv_quant_linear.  Opaque; owns its device buffers;
+ * immutable after lpv_quant_pack returns, so calls on different streams may share it. */
+typedef struct lpv_quant lpv_quant;
+
+typedef struct {
+    int64_t N, K;       /* weight shape: output x input features */
+    int32_t b_r, b_c;   /* block shape (dense: 16 x 16) */
+    int32_t R, C;       /* block grid: N / b_r x K / b_c */
+    int64_t nnzb;       /* kept blocks */
+    int64_t n_tiles;    /* 32 x 32 tiles with a kept block, 1 KB each */
+    int32_t device;     /* HIP device the buffers live on */
+} lpv_quant_info;
+
+/*
+ * lpv_quant_pack -- a weight in 8-bit codes and the scales of its outputs, W[n][k] =
+ * scale[n] Wq[n][k], packed once: the blocks that the mask keeps, or every one.
+ * W      device, int8 N x K, row stride K <= ldw <= 2^22, 16-byte aligned, ldw a multiple
+ *        of 16.  All 256 codes are taken.
+ * scale  device, float32, N elements (lpv_quant_rows of the masked weight gives both).
+ * mask   device, uint8, (N / b_r) x (K / b_c), row-major; nonzero keeps the block.  NULL: a
+ *        dense weight; N and K are then multiples of 16, and b_r and b_c are not looked at.
+ * out    host; receives a new handle (NULL on failure).
+ * Dropped blocks are never read.  N, K <= 65536.  Allocates device memory (freed by
+ * lpv_quant_destroy) and waits on `stream` twice, as lpv_bsr_pack does; W, scale and mask may
+ * be freed afterwards.
+ * Errors: INVALID_ARG, SHAPE, BLOCK, ALLOC, HIP.
+ */
+lpv_status lpv_quant_pack(const int8_t* W, int64_t ldw, int64_t N, int64_t K, const float* scale,
+                          int32_t b_r, int32_t b_c, const uint8_t* mask, void* stream, lpv_quant** out);
+
+/* Shape and counts of a handle (host struct). */
+lpv_status lpv_quant_info_get(const lpv_quant* h, lpv_quant_info* out);
+
+/*
+ * lpv_quant_linear -- the linear layer over 8-bit codes,
+ *   Y[m][n] = g(xscale[m] scale[n] sum_k X[m][k] Wq[n][k] + bias[n]),
+ * the sum over the kept blocks.
+ * X       device, int8 M x K, row stride K <= ldx <= 2^22, a multiple of 16; all 256 codes.
+ * xscale  device, float32, M elements (a NaN or an infinity is its row's).
+ * bias    device, N elements of type dt, or NULL for no bias.
+ * Y       device, M x N of type dt (each of lpv_dtype), row stride N <= ldy <= 2^22, a multiple of 16
+ *         bytes; must not overlap X, xscale or bias.
+ * epi     LPV_EPI_NONE or LPV_EPI_GELU, as lpv_bsr_linear (float32 outputs: to 1e-6 relative).
+ * The sums are 32-bit integers and exact; they, the scales and the bias meet in float32, and
+ * the result is rounded once, so a row's bits depend on neither the other rows nor M.
+ * No allocation, no host synchronisation.  M = 0 is a no-op.
+ * Errors: INVALID_ARG, SHAPE, DTYPE, ALIAS, HIP.
+ */
+lpv_status lpv_quant_linear(const lpv_quant* h, const int8_t* X, int64_t ldx, const float* xscale, int64_t M,
+                            const void* bias, void* Y, int64_t ldy, lpv_dtype dt, lpv_epilogue epi,
+                            void* stream);
+
+void lpv_quant_destroy(lpv_quant* h);
+
 #ifdef __cplusplus
 }
 #endif

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblpv.so")
 SOURCES = ["api.hip", "pack.hip", "linear.hip", "mask.hip", "backward.hip", "delta.hip", "encoder.hip",
-           "stationary.hip", "relpos.hip", "distill.hip"]
+           "stationary.hip", "relpos.hip", "distill.hip", "quant.hip", "quant_linear.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -27,7 +27,7 @@ FLAGS = [
 # register counts accumulators in AGPRs would be copied across every branch.
 _VGPR_MFMA = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 SOURCE_FLAGS = {"linear.hip": _VGPR_MFMA, "backward.hip": _VGPR_MFMA, "encoder.hip": _VGPR_MFMA,
-                "stationary.hip": _VGPR_MFMA,
+                "stationary.hip": _VGPR_MFMA, "quant_linear.hip": _VGPR_MFMA,
                 # (a maximum then takes its operands as they are, without quieting NaNs first)
                 "relpos.hip": _VGPR_MFMA + ["-fno-honor-nans"]}
 BUILD_DIR = os.path.join(HERE, "_build")

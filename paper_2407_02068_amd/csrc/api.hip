@@ -1171,4 +1171,216 @@ lpv_status lpv_distill(const void* logits, int64_t ldz, int64_t M, int64_t V, lp
     return e == hipSuccess ? LPV_OK : hip_fail(e, "distill launch");
 }
 
+namespace {
+
+// Shared checks of the calls that give rows in 8-bit codes, and the launch.
+lpv_status quant_rows(lpv::QuantRowsCall c, int64_t D, bool gamma, bool beta, void* stream)
+{
+    const int es = elem_size(c.dtype);
+    if (!es)
+        return fail(LPV_ERR_DTYPE, "unknown element type %d", c.dtype);
+    if (D < 1 || D > lpv::QUANT_MAX_D)
+        return fail(LPV_ERR_SHAPE, "D = %lld is out of range [1, %d]", (long long)D, lpv::QUANT_MAX_D);
+    if (c.M < 0 || c.M >= MAX_M)
+        return fail(LPV_ERR_SHAPE, "M = %lld is out of range [0, 2^31)", (long long)c.M);
+    if (!(c.eps >= 0.0) || !std::isfinite(c.eps))
+        return fail(LPV_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    if ((gamma && (!c.gamma || (uintptr_t)c.gamma % es)) || (beta && (!c.beta || (uintptr_t)c.beta % es)))
+        return fail(LPV_ERR_INVALID_ARG, "gamma and beta must be non-NULL and aligned to their element size");
+    if (c.M == 0)
+        return LPV_OK;
+    auto ld = [&](const void* p, int64_t l) { return p && (l < D || l > MAX_LD); };
+    if (ld(c.x, c.ldx) || ld(c.y, c.ldy) || ld(c.S, c.lds) || ld(c.q, c.ldq))
+        return fail(LPV_ERR_INVALID_ARG, "row strides must be in [D, 2^22]");
+    if (!c.x || !c.q || !c.scale || (uintptr_t)c.x % es || (uintptr_t)c.y % es || (uintptr_t)c.S % es ||
+        (uintptr_t)c.scale % 4)
+        return fail(LPV_ERR_INVALID_ARG, "x, q and scale must be non-NULL, and x, y, S and scale aligned "
+                                         "to their element size");
+    auto span = [&](int64_t l, int64_t e) { return ((c.M - 1) * l + D) * e; };
+    const int64_t nx = span(c.ldx, es), ny = c.y ? span(c.ldy, es) : 0, ns = c.S ? span(c.lds, es) : 0;
+    const int64_t nq = span(c.ldq, 1), nc = c.M * 4, ng = gamma ? D * es : 0, nb = beta ? D * es : 0;
+    if (c.S && ((!(c.S == c.x && c.lds == c.ldx) && overlap(c.S, ns, c.x, nx)) ||
+                (c.y && !(c.S == c.y && c.lds == c.ldy) && overlap(c.S, ns, c.y, ny))))
+        return fail(LPV_ERR_ALIAS, "S may be x or y itself, or not overlap them");
+    bool alias = overlap(c.q, nq, c.scale, nc) || (c.S && (overlap(c.S, ns, c.q, nq) || overlap(c.S, ns, c.scale, nc)));
+    const struct {
+        const void* p;
+        int64_t n;
+    } in[4] = {{c.x, nx}, {c.y, ny}, {gamma ? c.gamma : nullptr, ng}, {beta ? c.beta : nullptr, nb}};
+    for (int i = 0; i < 4; ++i)
+        if (in[i].p)
+            alias |= overlap(c.q, nq, in[i].p, in[i].n) || overlap(c.scale, nc, in[i].p, in[i].n) ||
+                     (i >= 2 && c.S && overlap(c.S, ns, in[i].p, in[i].n));
+    if (alias)
+        return fail(LPV_ERR_ALIAS, "q and scale must not overlap the inputs, S or each other, nor S the "
+                                   "norm's parameters");
+    c.D = (int32_t)D;
+    const hipError_t e = lpv::launch_quant_rows(c, (hipStream_t)stream);
+    return e == hipSuccess ? LPV_OK : hip_fail(e, "quant_rows launch");
+}
+
+}  // namespace
+
+lpv_status lpv_quant_rows(const void* x, int64_t ldx, const void* y, int64_t ldy, int64_t M, int64_t D,
+                          lpv_dtype dt, void* S, int64_t lds, int8_t* q, int64_t ldq, float* scale,
+                          void* stream)
+{
+    return quant_rows({lpv::QUANT_PLAIN, x, ldx, y, ldy, M, 0, (int)dt, nullptr, nullptr, 0.0, S, lds, q,
+                       ldq, scale}, D, false, false, stream);
+}
+
+lpv_status lpv_add_rmsnorm_quant(const void* x, int64_t ldx, const void* y, int64_t ldy, int64_t M,
+                                 int64_t D, lpv_dtype dt, const void* gamma, double eps, void* S,
+                                 int64_t lds, int8_t* q, int64_t ldq, float* scale, void* stream)
+{
+    return quant_rows({lpv::QUANT_RMS, x, ldx, y, ldy, M, 0, (int)dt, gamma, nullptr, eps, S, lds, q, ldq,
+                       scale}, D, true, false, stream);
+}
+
+lpv_status lpv_add_layernorm_quant(const void* x, int64_t ldx, const void* y, int64_t ldy, int64_t M,
+                                   int64_t D, lpv_dtype dt, const void* gamma, const void* beta,
+                                   double eps, void* S, int64_t lds, int8_t* q, int64_t ldq,
+                                   float* scale, void* stream)
+{
+    return quant_rows({lpv::QUANT_LAYER, x, ldx, y, ldy, M, 0, (int)dt, gamma, beta, eps, S, lds, q, ldq,
+                       scale}, D, true, true, stream);
+}
+
+lpv_status lpv_quant_pack(const int8_t* W, int64_t ldw, int64_t N, int64_t K, const float* scale,
+                          int32_t b_r, int32_t b_c, const uint8_t* mask, void* stream, lpv_quant** out)
+{
+    g_err[0] = 0;
+    if (!out)
+        return fail(LPV_ERR_INVALID_ARG, "out must not be NULL");
+    *out = nullptr;
+    if (mask && (check_block(b_r) || check_block(b_c)))
+        return fail(LPV_ERR_BLOCK, "block %dx%d: each side must be 16, 32 or 64", b_r, b_c);
+    if (!mask)
+        b_r = b_c = 16;
+    if (N <= 0 || K <= 0 || N > MAX_DIM || K > MAX_DIM)
+        return fail(LPV_ERR_SHAPE, "weight %lldx%lld: each side must be in [1, %lld]", (long long)N,
+                    (long long)K, (long long)MAX_DIM);
+    if (N % b_r || K % b_c)
+        return fail(LPV_ERR_SHAPE, "block %dx%d does not divide weight %lldx%lld", b_r, b_c, (long long)N,
+                    (long long)K);
+    if (!W || !scale || (uintptr_t)scale % 4)
+        return fail(LPV_ERR_INVALID_ARG, "W and scale must be non-NULL, scale 4-byte aligned");
+    if (ldw < K || ldw > MAX_LD || ldw % 16 || !aligned16(W))
+        return fail(LPV_ERR_INVALID_ARG, "W must be 16-byte aligned with K <= ldw <= 2^22 and ldw a multiple "
+                                         "of 16 bytes");
+    hipStream_t s = (hipStream_t)stream;
+    lpv_quant* h = new (std::nothrow) lpv_quant();
+    if (!h)
+        return fail(LPV_ERR_ALLOC, "host allocation failed");
+    h->N = N;
+    h->K = K;
+    h->b_r = b_r;
+    h->b_c = b_c;
+    h->R = (int32_t)(N / b_r);
+    h->C = (int32_t)(K / b_c);
+    h->n_tile_rows = (int32_t)((N + lpv::TILE - 1) / lpv::TILE);
+    h->n_tile_cols = (int32_t)((K + lpv::TILE - 1) / lpv::TILE);
+    h->n_pairs = (h->n_tile_rows + 15) / 16 * 8;
+    h->n_chunks = (h->n_tile_cols + lpv::QUANT_CHUNK - 1) / lpv::QUANT_CHUNK;
+    auto stop = [&](hipError_t e, const char* what) {
+        lpv_quant_destroy(h);
+        return e == hipErrorOutOfMemory ? fail(LPV_ERR_ALLOC, "device allocation failed") : hip_fail(e, what);
+    };
+    const size_t n_scale = (size_t)h->n_pairs * 64, n_bits = (size_t)h->n_pairs * h->n_chunks;
+    const size_t words = n_scale + n_bits + 2 * (size_t)(h->n_pairs + 1) + (size_t)h->n_tile_rows + 1 + 4;
+    hipError_t e = dmalloc(&h->mem, words * 4);
+    if (e == hipSuccess)
+        e = hipGetDevice(&h->device);
+    if (e != hipSuccess)
+        return stop(e, "hipMalloc");
+    h->scale = (float*)h->mem;
+    h->bits = (uint32_t*)(h->scale + n_scale);
+    h->tile0 = (int32_t*)(h->bits + n_bits);
+    h->group0 = h->tile0 + h->n_pairs + 1;
+    h->row_tile0 = h->group0 + h->n_pairs + 1;
+    lpv::QuantTotals* totals_d = (lpv::QuantTotals*)(h->row_tile0 + h->n_tile_rows + 1);
+    lpv::QuantTotals totals = {};
+    e = lpv::launch_quant_plan(h, mask, totals_d, s);
+    if (e == hipSuccess)
+        e = hipMemcpyAsync(&totals, totals_d, sizeof totals, hipMemcpyDeviceToHost, s);
+    if (e == hipSuccess)
+        e = hipStreamSynchronize(s);
+    if (e != hipSuccess)
+        return stop(e, "pack plan");
+    h->n_tiles = totals.n_tiles;
+    h->n_groups = totals.n_groups;
+    h->nnzb = totals.n_blocks;
+    // (two tiles more: the kernels ask for a tile ahead of the last)
+    const size_t n_tiles = ((size_t)h->n_tiles + 2) * 1024;
+    e = dmalloc(&h->data, n_tiles + ((size_t)h->n_tiles + 1) * sizeof(int2) + (size_t)h->n_groups * sizeof(uint2));
+    if (e != hipSuccess)
+        return stop(e, "hipMalloc");
+    h->tiles = (char*)h->data;
+    h->list = (int2*)(h->tiles + n_tiles);
+    h->groups = (uint2*)(h->list + h->n_tiles + 1);
+    e = lpv::launch_quant_fill(h, W, ldw, scale, mask, s);
+    if (e == hipSuccess)
+        e = hipStreamSynchronize(s);
+    if (e != hipSuccess)
+        return stop(e, "pack fill");
+    *out = h;
+    return LPV_OK;
+}
+
+lpv_status lpv_quant_info_get(const lpv_quant* h, lpv_quant_info* out)
+{
+    if (!h || !out)
+        return fail(LPV_ERR_INVALID_ARG, "handle and out must not be NULL");
+    *out = {h->N, h->K, h->b_r, h->b_c, h->R, h->C, h->nnzb, h->n_tiles, h->device};
+    return LPV_OK;
+}
+
+lpv_status lpv_quant_linear(const lpv_quant* h, const int8_t* X, int64_t ldx, const float* xscale, int64_t M,
+                            const void* bias, void* Y, int64_t ldy, lpv_dtype dt, lpv_epilogue epi,
+                            void* stream)
+{
+    if (!h)
+        return fail(LPV_ERR_INVALID_ARG, "handle must not be NULL");
+    const int es = elem_size(dt);
+    if (!es)
+        return fail(LPV_ERR_DTYPE, "unknown element type %d", (int)dt);
+    if (M < 0 || M >= MAX_M)
+        return fail(LPV_ERR_SHAPE, "M = %lld is out of range [0, 2^31)", (long long)M);
+    if (epi != LPV_EPI_NONE && epi != LPV_EPI_GELU)
+        return fail(LPV_ERR_INVALID_ARG, "unknown epilogue %d", (int)epi);
+    if (ldx < h->K || ldx > MAX_LD || ldx % 16 || ldy < h->N || ldy > MAX_LD || (ldy * es) % 16)
+        return fail(LPV_ERR_INVALID_ARG, "ldx and ldy must cover the row, be multiples of 16 bytes and at "
+                                         "most 2^22");
+    if (M == 0)
+        return LPV_OK;
+    if (!X || !Y || !aligned16(X) || !aligned16(Y) || (bias && !aligned16(bias)))
+        return fail(LPV_ERR_INVALID_ARG, "X and Y must be non-NULL, and X, Y and bias 16-byte aligned");
+    if (!xscale || (uintptr_t)xscale % 4)
+        return fail(LPV_ERR_INVALID_ARG, "xscale must be non-NULL and 4-byte aligned");
+    const int64_t ny = ((M - 1) * ldy + h->N) * es;
+    if (overlap(Y, ny, X, (M - 1) * ldx + h->K) || overlap(Y, ny, xscale, M * 4) ||
+        (bias && overlap(Y, ny, bias, h->N * es)))
+        return fail(LPV_ERR_ALIAS, "Y overlaps X, xscale or bias");
+    int dev = -1;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess)
+        return hip_fail(e, "hipGetDevice");
+    if (dev != h->device)
+        return fail(LPV_ERR_INVALID_ARG, "handle lives on device %d, current device is %d", h->device, dev);
+    const lpv::QuantLinearCall c = {X, ldx, xscale, M, bias, Y, ldy, (int)dt, epi == LPV_EPI_GELU};
+    e = lpv::launch_quant_linear(h, c, (hipStream_t)stream);
+    return e == hipSuccess ? LPV_OK : hip_fail(e, "quant_linear launch");
+}
+
+void lpv_quant_destroy(lpv_quant* h)
+{
+    if (!h)
+        return;
+    if (h->mem)
+        (void)hipFree(h->mem);
+    if (h->data)
+        (void)hipFree(h->data);
+    delete h;
+}
+
 }  // extern "C"

@@ -85,6 +85,32 @@ struct lpv_relpos {
     uint64_t crowded;
 };
 
+// A weight in 8-bit codes (lpv_quant_pack).  Its 32 x 32 tiles of codes go in pairs of tile
+// rows (64 outputs) and chunks of QUANT_CHUNK tile columns: pair by pair, chunk by chunk,
+// column by column, the even row's tile first.
+struct lpv_quant {
+    int64_t N, K;
+    int32_t b_r, b_c, R, C;  // (dense: blocks of 16 x 16, all kept)
+    int64_t nnzb, n_tiles, n_groups;
+    int32_t device;
+    int32_t n_tile_rows, n_tile_cols;
+    int32_t n_pairs;   // of tile rows, filled up to a multiple of 8 with empty ones
+    int32_t n_chunks;
+    void* mem;         // one allocation: the arrays whose sizes are known before the kept count is
+    void* data;        // another: tiles, list and groups
+    uint32_t* bits;      // n_pairs x n_chunks: kept columns of the even row | of the odd row << 16
+    int32_t* tile0;      // n_pairs + 1: the first tile of each pair
+    int32_t* group0;     // n_pairs + 1: the first group of each pair
+    int32_t* row_tile0;  // n_tile_rows + 1: the first entry of each tile row in list
+    float* scale;        // 64 n_pairs: the outputs' scales, zero past N
+    char* tiles;         // n_tiles x 1 KB: lane l's 16 codes of row l % 32, from column 16 (l / 32)
+    int2* list;          // n_tiles: by tile row, {tile column, place among the tiles}
+    // up to four columns of a pair's chunk, in order: 6 bits each (column in the chunk, even row
+    // kept << 4, odd row << 5), the chunk's last group << 24, the pair's last << 25; and the
+    // first tile.  A chunk has one at least.
+    uint2* groups;       // n_groups
+};
+
 namespace lpv {
 
 struct PackArgs {
@@ -244,6 +270,48 @@ struct DistillCall {
 };
 size_t distill_workspace_bytes(int64_t M, int64_t V, int32_t k, int dtype);
 hipError_t launch_distill(const DistillCall& c, hipStream_t s);
+// quant.hip
+constexpr int32_t QUANT_MAX_D = 32768;  // the longest row (it stays in registers)
+constexpr int QUANT_PLAIN = 0, QUANT_RMS = 1, QUANT_LAYER = 2;
+struct QuantRowsCall {
+    int kind;
+    const void* x;
+    int64_t ldx;
+    const void* y;  // or NULL
+    int64_t ldy, M;
+    int32_t D;
+    int dtype;
+    const void *gamma, *beta;
+    double eps;
+    void* S;  // or NULL
+    int64_t lds;
+    int8_t* q;
+    int64_t ldq;
+    float* scale;
+};
+hipError_t launch_quant_rows(const QuantRowsCall& c, hipStream_t s);
+// quant_linear.hip
+constexpr int QUANT_CHUNK = 16;  // tile columns of a chunk (512 columns)
+struct QuantTotals {
+    int32_t n_tiles, n_groups, n_blocks;
+};
+// Kept columns, counts and their sums (everything in h->mem but the scales); then tiles, list,
+// groups and scales.
+hipError_t launch_quant_plan(const lpv_quant* h, const uint8_t* mask, QuantTotals* totals, hipStream_t s);
+hipError_t launch_quant_fill(const lpv_quant* h, const int8_t* W, int64_t ldw, const float* scale,
+                             const uint8_t* mask, hipStream_t s);
+struct QuantLinearCall {
+    const int8_t* X;
+    int64_t ldx;
+    const float* xscale;
+    int64_t M;
+    const void* bias;
+    void* Y;
+    int64_t ldy;
+    int dtype;
+    int gelu;
+};
+hipError_t launch_quant_linear(const lpv_quant* h, const QuantLinearCall& c, hipStream_t s);
 hipError_t launch_bias_grad(const void* G, int64_t ldg, int64_t M, int64_t N, int dtype, void* db,
                             hipStream_t s);
 // The same with the partial sums in a fixed device array of this many floats

@@ -26,8 +26,9 @@ EXPORTED = ("lpv_bsr_pack", "lpv_bsr_info_get", "lpv_bsr_export", "lpv_bsr_sched
             "lpv_delta_curve", "lpv_delta_curve_ws", "lpv_delta_curve_workspace_size",
             "lpv_add_layernorm", "lpv_attention", "lpv_relpos_create", "lpv_relpos_destroy",
             "lpv_relpos_workspace_size", "lpv_relpos_attention", "lpv_relpos_attention_grad",
-            "lpv_distill", "lpv_distill_workspace_size", "lpv_bsr_destroy", "lpv_status_str",
-            "lpv_last_error")
+            "lpv_distill", "lpv_distill_workspace_size", "lpv_quant_rows", "lpv_add_rmsnorm_quant",
+            "lpv_add_layernorm_quant", "lpv_quant_pack", "lpv_quant_info_get", "lpv_quant_linear",
+            "lpv_quant_destroy", "lpv_bsr_destroy", "lpv_status_str", "lpv_last_error")
 
 
 class LpvError(RuntimeError):
@@ -43,6 +44,15 @@ class BsrInfo(ctypes.Structure):
                 ("tile_rows", ctypes.c_int32), ("tile_cols", ctypes.c_int32),
                 ("group_tiles", ctypes.c_int32), ("n_groups", ctypes.c_int32),
                 ("n_steps", ctypes.c_int64), ("n_tiles", ctypes.c_int64)]
+
+    def as_dict(self):
+        return {k: getattr(self, k) for k, _ in self._fields_}
+
+
+class QuantInfo(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("K", ctypes.c_int64), ("b_r", ctypes.c_int32),
+                ("b_c", ctypes.c_int32), ("R", ctypes.c_int32), ("C", ctypes.c_int32),
+                ("nnzb", ctypes.c_int64), ("n_tiles", ctypes.c_int64), ("device", ctypes.c_int32)]
 
     def as_dict(self):
         return {k: getattr(self, k) for k, _ in self._fields_}
@@ -91,18 +101,29 @@ def lib():
     L.lpv_distill.argtypes = [vp, i64, i64, i64, i32, vp, vp, i64, i32, ctypes.c_double, vp, vp, vp,
                               i64, i64, vp, ctypes.c_size_t, vp]
     L.lpv_distill_workspace_size.argtypes = [i64, i64, i32, i32, size_p]
+    L.lpv_quant_rows.argtypes = [vp, i64, vp, i64, i64, i64, i32, vp, i64, vp, i64, vp, vp]
+    L.lpv_add_rmsnorm_quant.argtypes = [vp, i64, vp, i64, i64, i64, i32, vp, ctypes.c_double, vp, i64,
+                                        vp, i64, vp, vp]
+    L.lpv_add_layernorm_quant.argtypes = [vp, i64, vp, i64, i64, i64, i32, vp, vp, ctypes.c_double, vp,
+                                          i64, vp, i64, vp, vp]
+    L.lpv_quant_pack.argtypes = [vp, i64, i64, i64, vp, i32, i32, vp, vp, ctypes.POINTER(vp)]
+    L.lpv_quant_info_get.argtypes = [vp, ctypes.POINTER(QuantInfo)]
+    L.lpv_quant_linear.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, i32, i32, vp]
     for f in ("lpv_bsr_pack", "lpv_bsr_info_get", "lpv_bsr_export", "lpv_bsr_schedule_export",
               "lpv_bsr_unpack", "lpv_bsr_linear", "lpv_dense_linear", "lpv_mask_topk",
               "lpv_bsr_transpose", "lpv_bsr_grad_w", "lpv_bias_grad", "lpv_bias_grad_noalloc",
               "lpv_delta_curve", "lpv_delta_curve_ws", "lpv_delta_curve_workspace_size",
               "lpv_add_layernorm", "lpv_attention", "lpv_relpos_create",
               "lpv_relpos_workspace_size", "lpv_relpos_attention", "lpv_relpos_attention_grad",
-              "lpv_distill", "lpv_distill_workspace_size"):
+              "lpv_distill", "lpv_distill_workspace_size", "lpv_quant_rows", "lpv_add_rmsnorm_quant",
+              "lpv_add_layernorm_quant", "lpv_quant_pack", "lpv_quant_info_get", "lpv_quant_linear"):
         getattr(L, f).restype = i32
     L.lpv_bsr_destroy.argtypes = [vp]
     L.lpv_bsr_destroy.restype = None
     L.lpv_relpos_destroy.argtypes = [vp]
     L.lpv_relpos_destroy.restype = None
+    L.lpv_quant_destroy.argtypes = [vp]
+    L.lpv_quant_destroy.restype = None
     L.lpv_status_str.argtypes = [i32]
     L.lpv_status_str.restype = ctypes.c_char_p
     L.lpv_last_error.argtypes = []
@@ -685,3 +706,136 @@ def distill_grad(logits, ids, teacher, temperature, dloss=None, loss=None, dlogi
         dlogits = wide[:, :logits.shape[1]]
     loss = _distill(logits, ids, teacher, temperature, dloss, loss, dlogits, Vd, workspace, stream)
     return loss, dlogits
+
+
+def _quant_rows(where, x, y, params, S, q, scale, stream):
+    """The arguments that the calls that give rows in 8-bit codes share; params: what comes
+    between the element type and S."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in DTYPES:
+        raise ValueError("x must be a 2-D tensor of float32, float16 or bfloat16")
+    M, D = x.shape
+    dt, dev = x.dtype, x.device
+    if q is None:
+        q = torch.empty((M, D), dtype=torch.int8, device=dev)
+    if scale is None:
+        scale = torch.empty(M, dtype=torch.float32, device=dev)
+    elif not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or scale.shape != (M,) \
+            or not scale.is_contiguous():
+        raise ValueError("scale must be a contiguous float32 tensor of M elements")
+    xp, ldx = _rows(x, "x", M, D, dt)
+    yp, ldy = _rows(y, "y", M, D, dt) if y is not None else (None, 0)
+    sp, lds = _rows(S, "S", M, D, dt) if S is not None else (None, 0)
+    qp, ldq = _rows(q, "q", M, D, torch.int8)
+    _on_current(("x", x), ("y", y), ("S", S), ("q", q), ("scale", scale))
+    _check(getattr(lib(), where)(xp, ldx, yp, ldy, M, D, DTYPES[dt], *params, sp, lds, qp, ldq,
+                                 scale.data_ptr(), _stream(stream)), where)
+    return q, scale
+
+
+def quant_rows(x, y=None, S=None, q=None, scale=None, stream=None):
+    """lpv_quant_rows: (q, scale), the rows of x (+ y) in 8-bit codes (int8 M x D) with a
+    scale for each row (M float32); the sum is written to S when given (which may be x or y)."""
+    return _quant_rows("lpv_quant_rows", x, y, (), S, q, scale, stream)
+
+
+def _norm_param(t, name, x):
+    if not isinstance(t, torch.Tensor) or t.dtype != x.dtype or t.shape != x.shape[1:] \
+            or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements" % (name, x.dtype, x.shape[1]))
+    _on_current((name, t))
+    return t.data_ptr()
+
+
+def add_rmsnorm_quant(x, y, gamma, eps, S=None, q=None, scale=None, stream=None):
+    """lpv_add_rmsnorm_quant: s = x + y (y may be None), and (q, scale), the rows of
+    s / sqrt(mean(s^2) + eps) * gamma in 8-bit codes with a scale for each; s is written to
+    S when given (which may be x or y)."""
+    return _quant_rows("lpv_add_rmsnorm_quant", x, y, (_norm_param(gamma, "gamma", x), float(eps)), S, q,
+                       scale, stream)
+
+
+def add_layernorm_quant(x, y, gamma, beta, eps, S=None, q=None, scale=None, stream=None):
+    """lpv_add_layernorm_quant: as ``add_rmsnorm_quant`` with the layer norm of
+    ``add_layernorm``, LN(s) * gamma + beta."""
+    return _quant_rows("lpv_add_layernorm_quant", x, y,
+                       (_norm_param(gamma, "gamma", x), _norm_param(beta, "beta", x), float(eps)), S, q,
+                       scale, stream)
+
+
+class QuantWeight:
+    """A weight in 8-bit codes, packed (owns an lpv_quant handle)."""
+
+    def __init__(self, handle):
+        self._h = ctypes.c_void_p(handle)
+        info = QuantInfo()
+        _check(lib().lpv_quant_info_get(self._h, ctypes.byref(info)), "lpv_quant_info_get")
+        self.info = info.as_dict()
+        self.N, self.K = self.info["N"], self.info["K"]
+
+    @property
+    def handle(self):
+        return self._h
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h.value:
+            lib().lpv_quant_destroy(self._h)
+            self._h = ctypes.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def quant_pack(W, scale, mask=None, b_r=16, b_c=16, stream=None):
+    """lpv_quant_pack: a weight in 8-bit codes (int8 N x K) with a scale for each output (N
+    float32), and a uint8 block mask (N/b_r x K/b_c; None: dense) -> QuantWeight.  Waits for
+    the pack to finish."""
+    if not isinstance(W, torch.Tensor) or W.dim() != 2:
+        raise ValueError("W must be a 2-D int8 tensor")
+    N, K = W.shape
+    wp, ldw = _rows(W, "W", N, K, torch.int8)
+    if not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or scale.shape != (N,) \
+            or not scale.is_contiguous():
+        raise ValueError("scale must be a contiguous float32 tensor of N elements")
+    if mask is not None:
+        if not isinstance(mask, torch.Tensor) or mask.dtype != torch.uint8 or not mask.is_contiguous():
+            raise ValueError("mask must be a contiguous uint8 tensor")
+        if b_r > 0 and b_c > 0 and N % b_r == 0 and K % b_c == 0 \
+                and mask.numel() != (N // b_r) * (K // b_c):
+            raise ValueError("mask has %d entries, expected %d" % (mask.numel(), (N // b_r) * (K // b_c)))
+    _on_current(("W", W), ("scale", scale), ("mask", mask))
+    out = ctypes.c_void_p()
+    _check(lib().lpv_quant_pack(wp, ldw, N, K, scale.data_ptr(), b_r, b_c,
+                                mask.data_ptr() if mask is not None else None, _stream(stream),
+                                ctypes.byref(out)), "lpv_quant_pack")
+    return QuantWeight(out.value)
+
+
+def quant_linear(h, X, xscale, bias=None, Y=None, dtype=None, epi=None, stream=None):
+    """lpv_quant_linear: Y = g(xscale scale (X Wq^T) + b) from 8-bit codes X (int8 M x K) with a
+    scale for each token (M float32).  Y has the type of the bias or ``dtype`` (bfloat16
+    without either); allocated if not given."""
+    if not isinstance(X, torch.Tensor) or X.dim() != 2:
+        raise ValueError("X must be a 2-D int8 tensor")
+    M = X.shape[0]
+    dt = Y.dtype if Y is not None else dtype if dtype is not None else bias.dtype if bias is not None \
+        else torch.bfloat16
+    if dt not in DTYPES or (dtype is not None and dtype != dt):
+        raise TypeError("outputs of %s: float32, float16 or bfloat16, the same as Y's" % dt)
+    if bias is not None and (not isinstance(bias, torch.Tensor) or bias.dtype != dt or bias.shape != (h.N,)
+                             or not bias.is_contiguous()):
+        raise ValueError("bias must be a contiguous %s tensor of N = %d elements" % (dt, h.N))
+    if not isinstance(xscale, torch.Tensor) or xscale.dtype != torch.float32 or xscale.shape != (M,) \
+            or not xscale.is_contiguous():
+        raise ValueError("xscale must be a contiguous float32 tensor of M elements")
+    if Y is None:
+        Y = torch.empty((M, h.N), dtype=dt, device=X.device)
+    xp, ldx = _rows(X, "X", M, h.K, torch.int8)
+    yp, ldy = _rows(Y, "Y", M, h.N, dt)
+    _on_current(("X", X), ("xscale", xscale), ("bias", bias), ("Y", Y))
+    _check(lib().lpv_quant_linear(h.handle, xp, ldx, xscale.data_ptr(), M,
+                                  bias.data_ptr() if bias is not None else None, yp, ldy, DTYPES[dt],
+                                  EPI[epi], _stream(stream)), "lpv_quant_linear")
+    return Y
