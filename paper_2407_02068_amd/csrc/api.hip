@@ -1287,7 +1287,7 @@ lpv_status lpv_quant_pack(const int8_t* W, int64_t ldw, int64_t N, int64_t K, co
         return e == hipErrorOutOfMemory ? fail(LPV_ERR_ALLOC, "device allocation failed") : hip_fail(e, what);
     };
     const size_t n_scale = (size_t)h->n_pairs * 64, n_bits = (size_t)h->n_pairs * h->n_chunks;
-    const size_t words = n_scale + n_bits + 2 * (size_t)(h->n_pairs + 1) + (size_t)h->n_tile_rows + 1 + 4;
+    const size_t words = n_scale + n_bits + (size_t)h->n_pairs + (size_t)h->n_tile_rows + 1 + 2;
     hipError_t e = dmalloc(&h->mem, words * 4);
     if (e == hipSuccess)
         e = hipGetDevice(&h->device);
@@ -1296,8 +1296,7 @@ lpv_status lpv_quant_pack(const int8_t* W, int64_t ldw, int64_t N, int64_t K, co
     h->scale = (float*)h->mem;
     h->bits = (uint32_t*)(h->scale + n_scale);
     h->tile0 = (int32_t*)(h->bits + n_bits);
-    h->group0 = h->tile0 + h->n_pairs + 1;
-    h->row_tile0 = h->group0 + h->n_pairs + 1;
+    h->row_tile0 = h->tile0 + h->n_pairs;
     lpv::QuantTotals* totals_d = (lpv::QuantTotals*)(h->row_tile0 + h->n_tile_rows + 1);
     lpv::QuantTotals totals = {};
     e = lpv::launch_quant_plan(h, mask, totals_d, s);
@@ -1308,11 +1307,10 @@ lpv_status lpv_quant_pack(const int8_t* W, int64_t ldw, int64_t N, int64_t K, co
     if (e != hipSuccess)
         return stop(e, "pack plan");
     h->n_tiles = totals.n_tiles;
-    h->n_groups = totals.n_groups;
     h->nnzb = totals.n_blocks;
     // (two tiles more: the kernels ask for a tile ahead of the last)
     const size_t n_tiles = ((size_t)h->n_tiles + 2) * 1024;
-    e = dmalloc(&h->data, n_tiles + ((size_t)h->n_tiles + 1) * sizeof(int2) + (size_t)h->n_groups * sizeof(uint2));
+    e = dmalloc(&h->data, n_tiles + ((size_t)h->n_tiles + 1) * sizeof(int2) + 4 * n_bits * sizeof(uint2));
     if (e != hipSuccess)
         return stop(e, "hipMalloc");
     h->tiles = (char*)h->data;

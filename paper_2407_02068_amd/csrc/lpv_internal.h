@@ -91,7 +91,7 @@ struct lpv_relpos {
 struct lpv_quant {
     int64_t N, K;
     int32_t b_r, b_c, R, C;  // (dense: blocks of 16 x 16, all kept)
-    int64_t nnzb, n_tiles, n_groups;
+    int64_t nnzb, n_tiles;
     int32_t device;
     int32_t n_tile_rows, n_tile_cols;
     int32_t n_pairs;   // of tile rows, filled up to a multiple of 8 with empty ones
@@ -99,16 +99,15 @@ struct lpv_quant {
     void* mem;         // one allocation: the arrays whose sizes are known before the kept count is
     void* data;        // another: tiles, list and groups
     uint32_t* bits;      // n_pairs x n_chunks: kept columns of the even row | of the odd row << 16
-    int32_t* tile0;      // n_pairs + 1: the first tile of each pair
-    int32_t* group0;     // n_pairs + 1: the first group of each pair
+    int32_t* tile0;      // n_pairs: the first tile of each pair
     int32_t* row_tile0;  // n_tile_rows + 1: the first entry of each tile row in list
     float* scale;        // 64 n_pairs: the outputs' scales, zero past N
     char* tiles;         // n_tiles x 1 KB: lane l's 16 codes of row l % 32, from column 16 (l / 32)
     int2* list;          // n_tiles: by tile row, {tile column, place among the tiles}
     // up to four columns of a pair's chunk, in order: 6 bits each (column in the chunk, even row
     // kept << 4, odd row << 5), the chunk's last group << 24, the pair's last << 25; and the
-    // first tile.  A chunk has one at least.
-    uint2* groups;       // n_groups
+    // first tile.  A chunk has one at least.  Pair p's follow each other from 4 n_chunks p on.
+    uint2* groups;       // 4 n_chunks n_pairs
 };
 
 namespace lpv {
@@ -293,7 +292,7 @@ hipError_t launch_quant_rows(const QuantRowsCall& c, hipStream_t s);
 // quant_linear.hip
 constexpr int QUANT_CHUNK = 16;  // tile columns of a chunk (512 columns)
 struct QuantTotals {
-    int32_t n_tiles, n_groups, n_blocks;
+    int32_t n_tiles, n_blocks;
 };
 // Kept columns, counts and their sums (everything in h->mem but the scales); then tiles, list,
 // groups and scales.

@@ -66,40 +66,34 @@ __global__ __launch_bounds__(64) void k_quant_bits(const lpv_quant h, const uint
 __global__ __launch_bounds__(1024) void k_quant_scan(const lpv_quant h, const uint8_t* __restrict__ mask,
                                                      QuantTotals* __restrict__ totals)
 {
-    __shared__ int s_tiles[1024], s_groups[1024], s_blocks;
+    __shared__ int s_tiles[1024], s_blocks;
     const int p = threadIdx.x;
     if (p == 0)
         s_blocks = 0;
-    int even = 0, odd = 0, groups = 0;
+    int even = 0, odd = 0;
     if (p < h.n_pairs)
         for (int c = 0; c < h.n_chunks; ++c) {
             const uint32_t b = h.bits[(int64_t)p * h.n_chunks + c];
             even += __popc(b & 0xffff);
             odd += __popc(b >> 16);
-            groups += groups_of(b);
         }
     s_tiles[p] = even + odd;
-    s_groups[p] = groups;
     __syncthreads();
     for (int d = 1; d < 1024; d <<= 1) {  // inclusive sums
-        const int t = p >= d ? s_tiles[p - d] : 0, g = p >= d ? s_groups[p - d] : 0;
+        const int t = p >= d ? s_tiles[p - d] : 0;
         __syncthreads();
         s_tiles[p] += t;
-        s_groups[p] += g;
         __syncthreads();
     }
     if (p < h.n_pairs) {
         const int t0 = s_tiles[p] - even - odd;
         h.tile0[p] = t0;
-        h.group0[p] = s_groups[p] - groups;
         if (2 * p < h.n_tile_rows)
             h.row_tile0[2 * p] = t0;
         if (2 * p + 1 < h.n_tile_rows)
             h.row_tile0[2 * p + 1] = t0 + even;
-        if (p == h.n_pairs - 1) {
-            h.tile0[h.n_pairs] = h.row_tile0[h.n_tile_rows] = s_tiles[p];
-            h.group0[h.n_pairs] = s_groups[p];
-        }
+        if (p == h.n_pairs - 1)
+            h.row_tile0[h.n_tile_rows] = s_tiles[p];
     }
     if (mask) {
         int n = 0;
@@ -111,7 +105,7 @@ __global__ __launch_bounds__(1024) void k_quant_scan(const lpv_quant h, const ui
         __syncthreads();
     }
     if (p == 0)
-        *totals = QuantTotals{s_tiles[1023], s_groups[1023], mask ? s_blocks : h.R * h.C};
+        *totals = QuantTotals{s_tiles[1023], mask ? s_blocks : h.R * h.C};
 }
 
 // One workgroup of 4 waves to a pair: wave w its chunks w, w + 4, ...
@@ -126,7 +120,7 @@ __global__ __launch_bounds__(256) void k_quant_fill(const lpv_quant h, const int
         h.scale[n] = n < h.N ? scale[n] : 0.0f;
     }
     const uint32_t* bits = h.bits + (int64_t)pair * h.n_chunks;
-    int tile = h.tile0[pair], group = h.group0[pair];
+    int tile = h.tile0[pair], group = pair * 4 * h.n_chunks;
     int at[2] = {0, 0};  // this pair's entries of either row in list
     if (2 * pair < h.n_tile_rows)
         at[0] = h.row_tile0[2 * pair];
@@ -179,8 +173,28 @@ __global__ __launch_bounds__(256) void k_quant_fill(const lpv_quant h, const int
 
 // ---------------------------------------------------------------- the epilogue's arithmetic
 
-// GELU for float32 outputs, to their own rounding (gelu_erf's 5e-6 would show there).
-__device__ inline float gelu_f32(float v) { return 0.5f * v * erfcf(v * -0.70710678118654752f); }
+// GELU for float32 outputs, as gelu_erf with f of degree 11 (gelu_fit.fit(11)): to 2e-7
+// relative near zero, 2e-6 in the tail, where gelu_erf's 3e-6 to 5e-6 would show in
+// the outputs' own type.
+__device__ inline float gelu_f32(float v)
+{
+    const float a = fabsf(v) * 0.70710678118654752f;
+    float f = 1.137913372e-07f;
+    f = fmaf(f, a, -2.993123871e-06f);
+    f = fmaf(f, a, 3.500672756e-05f);
+    f = fmaf(f, a, -2.377048368e-04f);
+    f = fmaf(f, a, 1.005247817e-03f);
+    f = fmaf(f, a, -2.407329390e-03f);
+    f = fmaf(f, a, 8.043324488e-05f);
+    f = fmaf(f, a, 2.782279439e-02f);
+    f = fmaf(f, a, -1.483810395e-01f);
+    f = fmaf(f, a, -9.184218049e-01f);
+    f = fmaf(f, a, -1.627909422e+00f);
+    f = fmaf(f, a, 3.518289304e-08f - 0.5f);
+    const float e = __builtin_amdgcn_exp2f(f);  // erfc(a) / sqrt 2
+    const float r = fmaxf(v, 0.0f);
+    return a >= 4.0f ? r : fmaf(-a, e, r);
+}
 
 // Four outputs of a token: sums, the token's scale, the outputs' scales and bias.
 template <int OUT, bool GELU> __device__ inline void finish4(const int s[4], float xs, float4 ws, float4 b, float out[4])
@@ -316,8 +330,381 @@ hipError_t launch_few(const lpv_quant* h, const QuantLinearCall& c, hipStream_t 
     return hipGetLastError();
 }
 
+// ---------------------------------------------------------------- many tokens
+
+// A workgroup of 8 waves takes items of 32 TU tokens times 8 pairs of tile rows (512 outputs), a
+// pair to a wave.  X goes by DMA into LDS a chunk (512 columns) at a time, two chunks in
+// turn; the pair's tiles come straight from memory into registers, since no other wave needs
+// them, four columns ahead.  A wave's work is a list of groups of four kept columns, made at
+// pack time: for each column it reads the tokens' codes from LDS, for one tile or both, and
+// has TU products for each.  So dropped tiles cost nothing, a column of X is read from LDS
+// once for two tiles, and waves meet at one barrier a chunk.
+//
+// LDS: panels of 128 columns, a row (token) of 128 bytes, its 16-byte piece c at
+// c ^ xswz(row): the 16 rows that are read at once lie in distinct banks.
+//
+// The wait before a chunk's barrier: the DMA of the next chunk is older than the tiles that
+// the wave has asked for since (8 loads a group, one group a chunk at least), and vector memory
+// comes back in order, so that all but the 8 youngest having come back is enough.
+struct PanelDims {
+    int64_t ldx, M, K, N, ldy;
+    int32_t n_chunks, n_pairs;
+    int32_t n_mt, n_pb;  // token tiles, blocks of 8 pairs
+    int32_t n_items;
+};
+constexpr int PN_WAVES = 8;
+constexpr int PN_MG = 8;             // token tiles that share an XCD's L2 with several blocks of pairs
+constexpr int PN_STAGE = 4096;       // bytes of a wave's staging area
+constexpr int PN_AHEAD = 8;          // loads of tiles that a group asks for
+
+// Global -> LDS DMA of 4 bytes per lane to 256 bytes at a wave-uniform LDS address.
+__device__ inline void dma4(const char* base, uint32_t off, uint32_t lds)
+{
+    asm volatile(
+        "s_nop 0\n"
+        "global_load_lds_dword %0, %1"
+        :
+        : "v"(off), "s"(base), "{m0}"(lds)
+        : "memory");
+}
+
+template <int OUT, bool GELU, int TU>
+__global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
+    const PanelDims a, const char* X, const char* xscale, const char* tiles, const uint2* groups,
+    const char* wscale, const char* bias, char* Y)
+{
+    constexpr int ES = OUT == LPV_F32 ? 4 : 2;
+    constexpr int PANEL = TU * 4096, SLOT = 4 * PANEL;  // bytes
+    __shared__ uint4 smem[(2 * SLOT + PN_WAVES * PN_STAGE) / 16];
+    // (an address that the compiler knows nothing about: loads from it stay on their side of the
+    // DMA and of the waits, which count them)
+    typedef const __attribute__((address_space(1))) char* global;
+    global wt = (global)tiles;
+    asm volatile("" : "+s"(wt));
+
+    const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lds = lds_addr(smem), stage = lds + 2 * SLOT + (uint32_t)wave * PN_STAGE;
+    const uint32_t loff = (uint32_t)lane * 16;
+
+    // Items in order: groups of PN_MG token tiles, in each the blocks of pairs, in each its token
+    // tiles; XCD x (workgroups x, x + 8, ...) has a contiguous eighth of them, which its
+    // workgroups take in turn.
+    const int xcd = (int)(blockIdx.x & 7), C = (int)(gridDim.x >> 3);
+    const int seg = (int)((int64_t)a.n_items * xcd / 8) + (int)(blockIdx.x >> 3);
+    const int seg_end = (int)((int64_t)a.n_items * (xcd + 1) / 8);
+    const int my_items = seg < seg_end ? (seg_end - seg + C - 1) / C : 0;
+    if (my_items == 0)
+        return;
+    auto item = [&](int k, int& mt, int& pb) {
+        const int i = seg + min(k, my_items - 1) * C, per = PN_MG * a.n_pb;
+        const int g = i / per, rest = i - g * per, mg = min(PN_MG, a.n_mt - g * PN_MG);
+        pb = rest / mg;
+        mt = g * PN_MG + rest - pb * mg;
+    };
+    const int per_pair = 4 * a.n_chunks;  // groups of a pair, at most
+    // (the lane made opaque: what only such a part needs is not kept in registers through the
+    // loop; the same below)
+    auto fresh = [](int l) __attribute__((always_inline)) {
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    auto lanes_of = [&](int pb, int from) {  // groups from .. from + 63 of this wave's pair
+        const uint2* g = groups + (int64_t)(pb * PN_WAVES + wave) * per_pair;
+        return g[(uint32_t)min(from + fresh(lane), per_pair - 1)];
+    };
+
+    // ---- the DMA of a chunk: wave w brings the rows 16 TU (w % 2) .. of panel w / 2
+    int d_k = 0, d_c = 0;  // its item and chunk
+    const char* d_base = nullptr;
+    uint32_t d_row[2 * TU];
+    auto set_x = [&]() {
+        int mt, pb;
+        item(d_k, mt, pb);
+        const int64_t m0 = (int64_t)mt * (32 * TU);
+        d_base = X + m0 * a.ldx;
+        const int last = (int)min((int64_t)32 * TU - 1, a.M - 1 - m0);  // rows past M repeat the last
+        const int ln = fresh(lane);
+#pragma unroll
+        for (int i = 0; i < 2 * TU; ++i)
+            d_row[i] = (uint32_t)min(16 * TU * (wave & 1) + 8 * i + (ln >> 3), last) * (uint32_t)a.ldx;
+    };
+    auto dma = [&](int slot) {
+        if (d_k >= my_items)
+            return;
+        const int ln = fresh(lane);
+#pragma unroll
+        for (int i = 0; i < 2 * TU; ++i) {
+            const int row = 8 * i + (ln >> 3);  // (16 TU (wave % 2) more: the same xswz)
+            const int k = d_c * (QUANT_CHUNK * TILE) + (wave >> 1) * 128 + ((ln & 7) ^ xswz(row)) * 16;
+            // (past K the tiles are zero: any codes do, the row's first)
+            dma16(d_base, d_row[i] + (uint32_t)(k < a.K ? k : 0),
+                  smem + (slot * SLOT + (wave >> 1) * PANEL + (wave & 1) * (TU * 2048) + i * 1024) / 16);
+        }
+        if (++d_c == a.n_chunks) {
+            d_c = 0;
+            if (++d_k < my_items)
+                set_x();
+        }
+    };
+    // ---- what the epilogue of an item needs, into the wave's staging area: the outputs' scales
+    // (256 bytes), their bias (256) and the tokens' scales
+    auto dma_params = [&](int k) {
+        int mt, pb;
+        item(k, mt, pb);
+        const int n0 = (pb * PN_WAVES + wave) * 64, ln = fresh(lane);
+        const int64_t m0 = (int64_t)mt * (32 * TU);
+        dma4(wscale + (int64_t)n0 * 4, (uint32_t)ln * 4, stage);
+        if (bias) {
+            const int n = n0 + (OUT == LPV_F32 ? ln : 2 * (ln & 31));
+            dma4(bias, (uint32_t)((n < a.N ? n : 0) * ES), stage + 256);
+        } else {
+            *(__attribute__((address_space(3))) uint32_t*)(uintptr_t)(stage + 256 + ln * 4) = 0;
+        }
+        const int last = (int)min((int64_t)32 * TU - 1, a.M - 1 - m0);
+#pragma unroll
+        for (int i = 0; i < (TU + 1) / 2; ++i)
+            dma4(xscale + m0 * 4, (uint32_t)min(64 * i + ln, last) * 4, stage + 512 + i * 256);
+    };
+
+    set_x();
+    dma(0);
+    dma_params(0);
+    int mt, pb, pb1;
+    item(0, mt, pb);
+    uint2 dl = lanes_of(pb, 0);  // this item's groups, 64 at a time
+    item(1, mt, pb1);
+    uint2 nd = lanes_of(pb1, 0), n2;  // the next item's, and the one's after it
+    asm volatile("" : "+v"(dl.x), "+v"(dl.y), "+v"(nd.x), "+v"(nd.y));
+    int gi = 0, from = 0;  // the group being worked on: lane gi of dl, whose first is `from`
+    uint32_t cur = __builtin_amdgcn_readlane(dl.x, 0);
+
+    // The tiles of four columns: of a column with one tile, that one twice.
+    v4i w[4][2];
+    typedef const __attribute__((address_space(1))) v4i* global4;
+    auto load_w = [&](int i, uint32_t desc, global& p) __attribute__((always_inline)) {
+        const uint32_t ab = desc >> (6 * i + 4) & 3;
+        w[i][0] = *(global4)(p + loff);
+        p += ab == 3 ? 1024 : 0;
+        w[i][1] = *(global4)(p + loff);
+        p += ab ? 1024 : 0;
+    };
+    {
+        global p = wt + (int64_t)__builtin_amdgcn_readlane(dl.y, 0) * 1024;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            load_w(i, cur, p);
+    }
+    // The codes of the tokens at a column of the chunk: lane l has row l % 32 (+ 32 u), pieces 2 c and
+    // 2 c + 1 of the panel by l / 32.
+    const int fr = lane & 31;
+    const uint32_t xbase = lds + fr * 128, xpiece = (uint32_t)(h ^ xswz(fr)) << 4;
+    v4i x[2][TU];
+    auto read_x = [&](v4i(&o)[TU], uint32_t desc, int i, uint32_t slot) __attribute__((always_inline)) {
+        const uint32_t c = desc >> (6 * i) & 15;
+        const uint32_t at = xbase + (xpiece ^ (c & 3) << 5) + (slot + (c >> 2) * PANEL);
+#pragma unroll
+        for (int u = 0; u < TU; ++u)
+            o[u] = *(const __attribute__((address_space(3))) v4i*)(uintptr_t)(at + u * 4096);
+    };
+    i32x16 acc[2][TU];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int u = 0; u < TU; ++u)
+            acc[j][u] = i32x16{};
+
+    auto sync = [&]() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"i"(PN_AHEAD) : "memory");
+    };
+    sync();
+    dma(1);
+    uint32_t slot = 0;
+    for (int k = 0; k < my_items; ++k) {
+        {
+            int mt2, pb2;
+            item(k + 2, mt2, pb2);
+            n2 = lanes_of(pb2, 0);
+        }
+        for (int c = 0; c < a.n_chunks; ++c) {
+            read_x(x[0], cur, 0, slot);
+            for (;;) {  // the chunk's groups
+                const bool last = cur >> 24 & 1;
+                uint32_t next, first;
+                if (cur >> 25 & 1) {
+                    next = __builtin_amdgcn_readlane(nd.x, 0);
+                    first = __builtin_amdgcn_readlane(nd.y, 0);
+                } else {
+                    if (__builtin_expect(++gi == 64, 0)) {
+                        gi = 0;
+                        from += 64;
+                        dl = lanes_of(pb, from);
+                        asm volatile("" : "+v"(dl.x), "+v"(dl.y));
+                    }
+                    next = __builtin_amdgcn_readlane(dl.x, gi);
+                    first = __builtin_amdgcn_readlane(dl.y, gi);
+                }
+                global p = wt + (int64_t)first * 1024;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (i < 3)
+                        read_x(x[(i + 1) & 1], cur, i + 1, slot);
+                    else if (!last)
+                        read_x(x[0], next, 0, slot);
+                    if (cur >> (6 * i + 4) & 1)
+#pragma unroll
+                        for (int u = 0; u < TU; ++u)
+                            acc[0][u] = mma8(w[i][0], x[i & 1][u], acc[0][u]);
+                    if (cur >> (6 * i + 5) & 1)
+#pragma unroll
+                        for (int u = 0; u < TU; ++u)
+                            acc[1][u] = mma8(w[i][1], x[i & 1][u], acc[1][u]);
+                    load_w(i, next, p);
+                }
+                cur = next;
+                if (last)
+                    break;
+            }
+            if (c == 0)
+                asm volatile("" : "+v"(n2.x), "+v"(n2.y));
+            sync();
+            dma(slot ? 1 : 0);
+            slot ^= SLOT;
+        }
+        // ---- the item's outputs
+        item(k, mt, pb);
+        const int64_t m0 = (int64_t)mt * (32 * TU), n0 = (int64_t)(pb * PN_WAVES + wave) * 64;
+        const int ln = fresh(lane), fr = ln & 31, h = ln >> 5;
+        float xs[TU];
+#pragma unroll
+        for (int u = 0; u < TU; ++u)
+            xs[u] = *(const __attribute__((address_space(3))) float*)(uintptr_t)(stage + 512 + (32 * u + fr) * 4);
+        uint2 pk[TU][2][4];    // 16-bit outputs: four to a place
+        float4 pf[OUT == LPV_F32 ? TU : 1][2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = 32 * j + 8 * q + 4 * h;
+                const float4 ws = __builtin_bit_cast(float4, lds_read16<0>(stage + n * 4));
+                float4 b;
+                if constexpr (OUT == LPV_F32) {
+                    b = __builtin_bit_cast(float4, lds_read16<256>(stage + n * 4));
+                } else {
+                    using E = Elem<OUT>;
+                    const uint64_t v = *(const __attribute__((address_space(3))) uint64_t*)(uintptr_t)(stage + 256 + n * 2);
+                    b = float4{E::to_f32((uint16_t)v), E::to_f32((uint16_t)(v >> 16)),
+                               E::to_f32((uint16_t)(v >> 32)), E::to_f32((uint16_t)(v >> 48))};
+                }
+#pragma unroll
+                for (int u = 0; u < TU; ++u) {
+                    const int s[4] = {acc[j][u][4 * q], acc[j][u][4 * q + 1], acc[j][u][4 * q + 2], acc[j][u][4 * q + 3]};
+                    float o[4];
+                    finish4<OUT, GELU>(s, xs[u], ws, b, o);
+                    if constexpr (OUT == LPV_F32)
+                        pf[u][j][q] = float4{o[0], o[1], o[2], o[3]};
+                    else
+                        pk[u][j][q] = uint2{pack2<OUT>(o[0], o[1]), pack2<OUT>(o[2], o[3])};
+                }
+            }
+        // 32 tokens of 128 bytes at a time through the staging area (16-byte piece c of token t at
+        // c ^ xswz(t)), so that whole lines leave; streamed past the caches, which X and the
+        // tiles want
+        const int lt = ln >> 3, lp = ln & 7;
+#pragma unroll
+        for (int u = 0; u < TU; ++u) {
+#pragma unroll
+            for (int half = 0; half < ES / 2; ++half) {
+                const uint32_t at = stage + fr * 128;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (ES == 4 && j != half)
+                        continue;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if constexpr (OUT == LPV_F32)
+                            lds_write16(at + (((2 * q + h) ^ xswz(fr)) << 4), __builtin_bit_cast(v4i, pf[u][j][q]));
+                        else
+                            *(__attribute__((address_space(3))) uint64_t*)(uintptr_t)(
+                                at + (((4 * j + q) ^ xswz(fr)) << 4) + 8 * h) = __builtin_bit_cast(uint64_t, pk[u][j][q]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = 8 * i + lt;
+                    const v4i v = lds_read16<0>(stage + t * 128 + ((lp ^ xswz(t)) << 4));
+                    const int64_t m = m0 + 32 * u + t, n = n0 + 32 * half + lp * (16 / ES);
+                    if (m < a.M && n < a.N)
+                        __builtin_nontemporal_store(v, (v4i*)(Y + (m * a.ldy + n) * ES));
+                }
+            }
+        }
+        if (k + 1 < my_items)
+            dma_params(k + 1);
+        pb = pb1;
+        {
+            int mt2;
+            item(k + 2, mt2, pb1);
+        }
+        dl = nd;
+        nd = n2;
+        gi = from = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int u = 0; u < TU; ++u)
+                acc[j][u] = i32x16{};
+    }
+    // (nothing of this workgroup is in flight when it ends)
+    __builtin_amdgcn_s_waitcnt(0);
+}
+
+template <int OUT, bool GELU, int TU>
+hipError_t launch_panel(const lpv_quant* h, const QuantLinearCall& c, int n_cus, hipStream_t s)
+{
+    PanelDims d = {c.ldx, c.M, h->K, h->N, c.ldy, h->n_chunks, h->n_pairs};
+    // token tiles of one launch: items in 31 bits
+    d.n_pb = h->n_pairs / PN_WAVES;
+    const int64_t most = ((int64_t)1 << 30) / d.n_pb;
+    const int wgs = max(n_cus & ~7, 8) * (TU == 1 ? 2 : 1);
+    for (int64_t m = 0, n_mt = (c.M + 32 * TU - 1) / (32 * TU); n_mt > 0; m += most, n_mt -= most) {
+        d.n_mt = (int32_t)(n_mt < most ? n_mt : most);
+        d.n_items = d.n_mt * d.n_pb;
+        const int64_t m0 = m * (32 * TU);
+        d.M = c.M - m0;
+        const int need = (int)(((int64_t)d.n_items + 7) / 8 * 8);
+        const dim3 grid((unsigned)(need < wgs ? need : wgs)), block(64 * PN_WAVES);
+        hipLaunchKernelGGL((k_quant_panel<OUT, GELU, TU>), grid, block, 0, s, d, (const char*)c.X + m0 * c.ldx,
+                           (const char*)(c.xscale + m0), (const char*)h->tiles, (const uint2*)h->groups,
+                           (const char*)h->scale, (const char*)c.bias,
+                           (char*)c.Y + m0 * c.ldy * (OUT == LPV_F32 ? 4 : 2));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
+}
+
+inline int num_cus()
+{
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess ||
+        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0)
+        n = 256;
+    return n;
+}
+
 template <int OUT, bool GELU> hipError_t launch_as(const lpv_quant* h, const QuantLinearCall& c, hipStream_t s)
 {
+    const int cus = num_cus();
+    const int64_t pbs = h->n_pairs / PN_WAVES;
+    auto items = [&](int t) { return (c.M + t - 1) / t * pbs; };
+    if (items(128) >= cus)
+        return launch_panel<OUT, GELU, 4>(h, c, cus, s);
+    if (items(64) >= cus)
+        return launch_panel<OUT, GELU, 2>(h, c, cus, s);
+    if (items(32) >= cus / 2)
+        return launch_panel<OUT, GELU, 1>(h, c, cus, s);
     if (c.M <= 32)
         return launch_few<OUT, GELU, 1>(h, c, s);
     return launch_few<OUT, GELU, 2>(h, c, s);

@@ -65,7 +65,8 @@ def check(Y, ref, dtype, gelu=False, what=""):
 
 DENSE = [(1, 16, 16), (1, 32, 48), (2, 48, 32), (31, 64, 64), (32, 80, 496), (33, 96, 512), (63, 512, 528),
          (64, 528, 1024), (65, 560, 1040), (127, 64, 2064), (128, 1040, 768), (129, 1024, 80), (197, 2304, 768),
-         (1, 4096, 4096), (5, 176, 8208), (257, 96, 1600), (500, 1536, 384), (1000, 272, 304)]
+         (1, 4096, 4096), (5, 176, 8208), (257, 96, 1600), (500, 1536, 384), (1000, 272, 304),
+         (1100, 8208, 80), (2050, 8208, 80), (8300, 2064, 560), (600, 8208, 1072)]
 
 
 @pytest.mark.parametrize("M,N,K", DENSE)
@@ -80,7 +81,9 @@ def test_dense(M, N, K):
 BLOCKS = [(1, 64, 64, 16, 16, 50), (7, 64, 64, 64, 64, 50), (33, 96, 48, 16, 16, 60), (64, 128, 512, 32, 32, 50),
           (65, 112, 560, 16, 16, 90), (197, 2304, 768, 32, 32, 50), (130, 576, 1088, 64, 64, 80),
           (300, 1536, 384, 16, 16, 75), (1, 1024, 2048, 32, 64, 95), (129, 544, 1056, 32, 16, 30),
-          (77, 640, 1600, 64, 32, 99), (513, 192, 4096, 16, 64, 40), (260, 320, 512, 64, 16, 0)]
+          (77, 640, 1600, 64, 32, 99), (513, 192, 4096, 16, 64, 40), (260, 320, 512, 64, 16, 0),
+         (2050, 8208, 112, 16, 16, 70), (1030, 8192, 1088, 64, 32, 60), (520, 8224, 1072, 32, 16, 85),
+         (17000, 1088, 576, 64, 64, 30)]
 
 
 @pytest.mark.parametrize("M,N,K,b_r,b_c,drop", BLOCKS)
