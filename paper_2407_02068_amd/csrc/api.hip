@@ -1291,6 +1291,8 @@ lpv_status lpv_quant_pack(const int8_t* W, int64_t ldw, int64_t N, int64_t K, co
     hipError_t e = dmalloc(&h->mem, words * 4);
     if (e == hipSuccess)
         e = hipGetDevice(&h->device);
+    if (e == hipSuccess)
+        e = hipDeviceGetAttribute(&h->n_cus, hipDeviceAttributeMultiprocessorCount, h->device);
     if (e != hipSuccess)
         return stop(e, "hipMalloc");
     h->scale = (float*)h->mem;
@@ -1310,7 +1312,7 @@ lpv_status lpv_quant_pack(const int8_t* W, int64_t ldw, int64_t N, int64_t K, co
     h->nnzb = totals.n_blocks;
     // (two tiles more: the kernels ask for a tile ahead of the last)
     const size_t n_tiles = ((size_t)h->n_tiles + 2) * 1024;
-    e = dmalloc(&h->data, n_tiles + ((size_t)h->n_tiles + 1) * sizeof(int2) + 4 * n_bits * sizeof(uint2));
+    e = dmalloc(&h->data, n_tiles + ((size_t)h->n_tiles + 1) * sizeof(int2) + lpv::QUANT_GROUPS * n_bits * sizeof(uint2));
     if (e != hipSuccess)
         return stop(e, "hipMalloc");
     h->tiles = (char*)h->data;

@@ -92,7 +92,7 @@ struct lpv_quant {
     int64_t N, K;
     int32_t b_r, b_c, R, C;  // (dense: blocks of 16 x 16, all kept)
     int64_t nnzb, n_tiles;
-    int32_t device;
+    int32_t device, n_cus;
     int32_t n_tile_rows, n_tile_cols;
     int32_t n_pairs;   // of tile rows, filled up to a multiple of 8 with empty ones
     int32_t n_chunks;
@@ -104,10 +104,12 @@ struct lpv_quant {
     float* scale;        // 64 n_pairs: the outputs' scales, zero past N
     char* tiles;         // n_tiles x 1 KB: lane l's 16 codes of row l % 32, from column 16 (l / 32)
     int2* list;          // n_tiles: by tile row, {tile column, place among the tiles}
-    // up to four columns of a pair's chunk, in order: 6 bits each (column in the chunk, even row
-    // kept << 4, odd row << 5), the chunk's last group << 24, the pair's last << 25; and the
-    // first tile.  A chunk has one at least.  Pair p's follow each other from 4 n_chunks p on.
-    uint2* groups;       // 4 n_chunks n_pairs
+    // Groups of two halves, a half up to two columns of a pair's chunk, in order.  A half is 16
+    // bits: 6 for each column (its place in the chunk, even row kept << 4, odd row << 5), the
+    // chunk's last half << 12, the pair's << 13; a chunk has one at least, a pair an even number.
+    // Then the group's first tile.  Pair p's groups follow each other from QUANT_GROUPS
+    // n_chunks p on.
+    uint2* groups;       // QUANT_GROUPS n_chunks n_pairs
 };
 
 namespace lpv {
@@ -290,7 +292,8 @@ struct QuantRowsCall {
 };
 hipError_t launch_quant_rows(const QuantRowsCall& c, hipStream_t s);
 // quant_linear.hip
-constexpr int QUANT_CHUNK = 16;  // tile columns of a chunk (512 columns)
+constexpr int QUANT_CHUNK = 8;   // tile columns of a chunk (256 columns)
+constexpr int QUANT_GROUPS = 2;  // groups of a chunk, at most
 struct QuantTotals {
     int32_t n_tiles, n_blocks;
 };

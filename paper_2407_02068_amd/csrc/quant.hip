@@ -15,7 +15,6 @@
 #include <math.h>
 
 #include "lpv_device.h"
-#include "lpv_grid.h"
 #include "lpv_internal.h"
 
 namespace lpv {
@@ -24,275 +23,410 @@ namespace {
 struct QuantDims {
     int64_t ldx, ldy, lds, ldq, M;
     int32_t D;
-    double eps;
+    double eps, per;  // 1 / D
 };
 
-// Eight values of an element type, as doubles: 16-byte loads.
-template <int DT> __device__ inline void load8(const char* p, double v[8])
+// CH neighbours of a row as they lie in memory, and their values.
+template <int DT, int CH> struct Raw {
+    static constexpr int WORDS = DT == 0 ? CH : CH / 2;
+    uint32_t w[WORDS];
+    __device__ inline void load(const char* p)
+    {
+        if constexpr (WORDS == 2) {
+            const uint2 v = *(const uint2*)p;
+            w[0] = v.x;
+            w[1] = v.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; i += 4) {
+                const uint4 v = *(const uint4*)(p + 4 * i);
+                w[i] = v.x;
+                w[i + 1] = v.y;
+                w[i + 2] = v.z;
+                w[i + 3] = v.w;
+            }
+        }
+    }
+    // element j alone, from its own address (element by element)
+    __device__ inline void load1(int j, const char* p)
+    {
+        if constexpr (DT == 0)
+            w[j] = *(const uint32_t*)p;
+        else if (j & 1)
+            w[j / 2] |= (uint32_t) * (const uint16_t*)p << 16;
+        else
+            w[j / 2] = *(const uint16_t*)p;
+    }
+    __device__ inline float at(int j) const
+    {
+        if constexpr (DT == 0)
+            return __uint_as_float(w[j]);
+        else
+            return Elem<DT>::to_f32((uint16_t)(w[j / 2] >> (16 * (j & 1))));
+    }
+};
+
+// CH values rounded to the element type, to CH neighbours.
+template <int DT, int CH> __device__ inline void store_sum(char* p, const float v[CH])
 {
-    if constexpr (DT == 0) {
-        const float4 a = *(const float4*)p, b = *(const float4*)(p + 16);
-        const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t w[Raw<DT, CH>::WORDS];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] = f[j];
+    for (int i = 0; i < Raw<DT, CH>::WORDS; ++i) {
+        if constexpr (DT == 0)
+            w[i] = __float_as_uint(v[i]);
+        else
+            w[i] = pack2<DT>(v[2 * i], v[2 * i + 1]);
+    }
+    if constexpr (Raw<DT, CH>::WORDS == 2) {
+        *(uint2*)p = uint2{w[0], w[1]};
     } else {
-        const uint4 a = *(const uint4*)p;
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] = Elem<DT>::to_f32((uint16_t)(w[j / 2] >> (16 * (j & 1))));
+        for (int i = 0; i < Raw<DT, CH>::WORDS; i += 4)
+            *(uint4*)(p + 4 * i) = uint4{w[i], w[i + 1], w[i + 2], w[i + 3]};
     }
 }
 
-template <int DT> __device__ inline double load1(const char* p)
+template <int DT> __device__ inline void store_sum1(char* p, float v)
 {
     if constexpr (DT == 0)
-        return *(const float*)p;
+        *(float*)p = v;
     else
-        return Elem<DT>::to_f32(*(const uint16_t*)p);
+        *(uint16_t*)p = Elem<DT>::from_f32(v);
 }
 
-template <int DT> __device__ inline void store8(char* p, const double v[8])
+// The same value of another lane of the row of 16: row_ror.
+template <int N> __device__ inline double ror16(double v)
 {
-    if constexpr (DT == 0) {
-        *(float4*)p = float4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-        *(float4*)(p + 16) = float4{(float)v[4], (float)v[5], (float)v[6], (float)v[7]};
-    } else {
-        *(uint4*)p = uint4{pack2<DT>((float)v[0], (float)v[1]), pack2<DT>((float)v[2], (float)v[3]),
-                           pack2<DT>((float)v[4], (float)v[5]), pack2<DT>((float)v[6], (float)v[7])};
-    }
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)b, 0x120 + N, 0xf, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(b >> 32), 0x120 + N, 0xf, 0xf, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-template <int DT> __device__ inline void store1(char* p, double v)
+// All-reduce over a wave in registers: rotations in rows of 16 lanes, then the rows change places
+// (every lane adds the same pairs, in one order or the other: the same bits).
+template <typename F> __device__ inline double wave_all(double v, F op)
 {
-    if constexpr (DT == 0)
-        *(float*)p = (float)v;
-    else
-        *(uint16_t*)p = Elem<DT>::from_f32((float)v);
-}
-
-// The row's sums (and its largest value) over its NT threads, the same in every thread:
-// lanes by butterfly, then waves in order.
-template <int NT> __device__ inline void row_reduce(double& a, double& b, double& top, double (*s)[3])
-{
+    v = op(v, ror16<8>(v));
+    v = op(v, ror16<4>(v));
+    v = op(v, ror16<2>(v));
+    v = op(v, ror16<1>(v));
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        a += __shfl_xor(a, o, 64);
-        b += __shfl_xor(b, o, 64);
-        top = fmax(top, __shfl_xor(top, o, 64));
+    for (int half = 16; half <= 32; half *= 2) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, v);
+        const uint32_t l = (uint32_t)b, h = (uint32_t)(b >> 32);
+        const auto lo = half == 16 ? __builtin_amdgcn_permlane16_swap(l, l, false, false)
+                                   : __builtin_amdgcn_permlane32_swap(l, l, false, false);
+        const auto hi = half == 16 ? __builtin_amdgcn_permlane16_swap(h, h, false, false)
+                                   : __builtin_amdgcn_permlane32_swap(h, h, false, false);
+        v = op(__builtin_bit_cast(double, (uint64_t)hi[0] << 32 | lo[0]),
+               __builtin_bit_cast(double, (uint64_t)hi[1] << 32 | lo[1]));
     }
+    return v;
+}
+
+struct Add {
+    __device__ inline double operator()(double a, double b) const { return a + b; }
+};
+struct Max {
+    __device__ inline double operator()(double a, double b) const { return fmax(a, b); }
+};
+
+// Over the NT threads of a row, the same in every thread: lanes, then waves in order.  `s` holds
+// two reductions in turn, so that one barrier each is enough.
+template <int NT, typename F> __device__ inline double row_all(double v, F op, double* s, int& turn)
+{
+    v = wave_all(v, op);
     if constexpr (NT > 64) {
-        const int wave = threadIdx.x >> 6;
-        __syncthreads();  // (a reduction before this one has been read)
+        s += turn * (2 * (NT / 64));
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0)
+            s[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = s[0];
+#pragma unroll
+        for (int w = 1; w < NT / 64; ++w)
+            v = op(v, s[w]);
+    }
+    return v;
+}
+
+// Two sums at once.
+template <int NT> __device__ inline void row_sums(double& a, double& b, double* s, int& turn)
+{
+    a = wave_all(a, Add());
+    b = wave_all(b, Add());
+    if constexpr (NT > 64) {
+        constexpr int N = NT / 64;
+        s += turn * (2 * N);
+        turn ^= 1;
         if ((threadIdx.x & 63) == 0) {
-            s[wave][0] = a;
-            s[wave][1] = b;
-            s[wave][2] = top;
+            s[threadIdx.x >> 6] = a;
+            s[N + (threadIdx.x >> 6)] = b;
         }
         __syncthreads();
-        a = b = top = 0.0;
+        a = s[0];
+        b = s[N];
 #pragma unroll
-        for (int w = 0; w < NT / 64; ++w) {
-            a += s[w][0];
-            b += s[w][1];
-            top = fmax(top, s[w][2]);
+        for (int w = 1; w < N; ++w) {
+            a += s[w];
+            b += s[N + w];
         }
     }
 }
 
-// NT threads to a row (64: four rows to a workgroup), NC chunks of 8 elements to a thread,
-// held in registers: the row is read once.  VEC: a chunk is 8 neighbours, by 16-byte
-// loads; else (odd sizes, strides or addresses) the row's elements go to the threads
-// one by one.
-template <int DT, int KIND, int NT, int NC, bool VEC>
+// The value of a row's first thread, in every thread.
+template <int NT> __device__ inline double first_of(double v, double* s, int& turn)
+{
+    if constexpr (NT > 64) {
+        s += turn * (2 * (NT / 64));
+        turn ^= 1;
+        if (threadIdx.x == 0)
+            s[0] = v;
+        __syncthreads();
+        return s[0];
+    } else {
+        const uint64_t b = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)b);
+        const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    }
+}
+
+// 1 / sqrt(x) and 1 / x to 2^-48 of them: the instructions' estimates (2^-22 at worst) and Newton's
+// steps; an infinity or a NaN for x = 0, as long as nothing takes it.
+__device__ inline double fast_rsqrt(double x)
+{
+    double r = __builtin_amdgcn_rsq(x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const double e = fma(-x * r, r, 1.0);
+        r = fma(r * 0.5, e, r);
+    }
+    return r;
+}
+__device__ inline double fast_rcp(double x)
+{
+    double r = __builtin_amdgcn_rcp(x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        r = fma(fma(-x, r, 1.0), r, r);
+    return r;
+}
+
+// NT threads to a row (64: four rows to a workgroup), NC chunks of CH elements to a thread, held
+// in registers: the row is read once, the next one's loads going out before this one is worked on.
+// VEC: a chunk is CH neighbours; else (odd sizes, strides or addresses) the row's elements go
+// to the threads one by one.
+template <int DT, int KIND, int NT, int NC, int CH, bool VEC>
 __global__ __launch_bounds__(NT == 64 ? 256 : NT) void k_quant_rows(
     const QuantDims d, const char* x, const char* y, const char* __restrict__ gamma,
     const char* __restrict__ beta, char* S, int8_t* __restrict__ q, float* __restrict__ scale)
 {
-    constexpr int ES = DT == 0 ? 4 : 2, E = 8 * NC;
+    constexpr int ES = DT == 0 ? 4 : 2, E = NC * CH;
     constexpr int RPW = NT == 64 ? 4 : 1;  // rows per workgroup
-    __shared__ double s_red[NT / 64][3];
+    constexpr bool KEEP = E <= 16;         // gamma and beta stay in registers
+    __shared__ double s_red[4 * (NT / 64)];
+    int turn = 0;
     const int tid = NT == 64 ? threadIdx.x & 63 : threadIdx.x;
-    const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * RPW +
-                        (NT == 64 ? (int)(threadIdx.x >> 6) : 0);
-    if (row >= d.M)
-        return;  // (whole waves of a row each, or the whole workgroup)
+    const int64_t step = (int64_t)gridDim.x * RPW;
+    int64_t row = (int64_t)blockIdx.x * RPW + (NT == 64 ? (int)(threadIdx.x >> 6) : 0);
     // element of this thread's i-th chunk, j-th place
-    auto at = [&](int i, int j) { return VEC ? (tid + NT * i) * 8 + j : tid + NT * (8 * i + j); };
-    const char* xr = x + row * d.ldx * ES;
-    const char* yr = y ? y + row * d.ldy * ES : nullptr;
-    char* sr = S ? S + row * d.lds * ES : nullptr;
-    double v[E];
-    double sum = 0.0, sq = 0.0, top = 0.0;
+    auto at = [&](int i, int j) { return VEC ? (tid + NT * i) * CH + j : tid + NT * (CH * i + j); };
+    typedef Raw<DT, CH> R;
+    auto load = [&](R(&r)[NC], const char* p) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        double* vi = v + 8 * i;
+        for (int i = 0; i < NC; ++i) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            vi[j] = 0.0;
-        if constexpr (VEC) {
-            const int c = at(i, 0);
-            if (c < d.D) {
-                load8<DT>(xr + (int64_t)c * ES, vi);
-                if (y) {
-                    double t[8];
-                    load8<DT>(yr + (int64_t)c * ES, t);
+            for (int k = 0; k < R::WORDS; ++k)
+                r[i].w[k] = 0;
+            if constexpr (VEC) {
+                if (at(i, 0) < d.D)
+                    r[i].load(p + at(i, 0) * ES);
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        vi[j] += t[j];
-                }
-                if (S)
-                    store8<DT>(sr + (int64_t)c * ES, vi);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = at(i, j);
-                if (c < d.D) {
-                    vi[j] = load1<DT>(xr + (int64_t)c * ES);
-                    if (y)
-                        vi[j] += load1<DT>(yr + (int64_t)c * ES);
-                    if (S)
-                        store1<DT>(sr + (int64_t)c * ES, vi[j]);
-                }
+                for (int j = 0; j < CH; ++j)
+                    if (at(i, j) < d.D)
+                        r[i].load1(j, p + at(i, j) * ES);
             }
         }
-    }
-    double factor = 1.0;
-    if constexpr (KIND == QUANT_LAYER) {
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-            sum += v[i];
-        row_reduce<NT>(sum, sq, top, s_red);
-        const double mean = sum / d.D;
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-            if (at(i / 8, i % 8) < d.D) {
-                v[i] -= mean;
-                sq += v[i] * v[i];
-            }
-        sum = 0.0;
-        row_reduce<NT>(sum, sq, top, s_red);
-        factor = 1.0 / sqrt(sq / d.D + d.eps);
-    }
-    if constexpr (KIND == QUANT_RMS) {
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-            sq += v[i] * v[i];
-    }
-    double poison = 0.0;  // not zero where a value is not finite
-#pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        double g[8], b[8];
-        if constexpr (KIND != QUANT_PLAIN && VEC) {
-            const int c = at(i, 0);
-            if (c < d.D) {
-                load8<DT>(gamma + (int64_t)c * ES, g);
-                if constexpr (KIND == QUANT_LAYER)
-                    load8<DT>(beta + (int64_t)c * ES, b);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = at(i, j);
-            if (c < d.D) {
-                if constexpr (KIND != QUANT_PLAIN && !VEC) {
-                    g[j] = load1<DT>(gamma + (int64_t)c * ES);
-                    if constexpr (KIND == QUANT_LAYER)
-                        b[j] = load1<DT>(beta + (int64_t)c * ES);
-                }
-                double& u = v[8 * i + j];
-                if constexpr (KIND == QUANT_RMS)
-                    u *= g[j];
-                if constexpr (KIND == QUANT_LAYER)
-                    u = u * factor * g[j] + b[j];
-                top = fmax(top, fabs(u));
-                poison += u * 0.0;
-            }
-        }
-    }
-    row_reduce<NT>(sq, poison, top, s_red);
-    if constexpr (KIND == QUANT_RMS) {
-        factor = 1.0 / sqrt(sq / d.D + d.eps);
-        poison += sq * 0.0;
-    }
-    // (the layer norm's factor is in u)
-    const bool bad = !(poison == 0.0);
-    double sc = KIND == QUANT_RMS ? top * factor / 127.0 : top / 127.0;
-    if (top == 0.0)
-        sc = 0.0;
-    if (tid == 0)
-        scale[row] = bad ? __builtin_nanf("") : (float)sc;
-    const double inv = bad || top == 0.0 ? 0.0 : 127.0 / top;
-    int8_t* qr = q + row * d.ldq;
-    auto code = [&](double u) -> uint32_t {
-        if (bad)
-            u = 0.0;
-        constexpr double FINE = 6144.0;              // 1.5 * 2^12
-        constexpr double WHOLE = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the integer
-        const double t = (fma(u, inv, FINE) - FINE) + WHOLE;
-        return (uint32_t)__builtin_bit_cast(uint64_t, t) & 0xff;
     };
+    R g[NC], b[NC], nx[NC], ny[NC];
+    if (KEEP && KIND != QUANT_PLAIN)
+        load(g, gamma);
+    if (KEEP && KIND == QUANT_LAYER)
+        load(b, beta);
+    if (row < d.M) {
+        load(nx, x + row * d.ldx * ES);
+        if (y)
+            load(ny, y + row * d.ldy * ES);
+    }
+    for (; row < d.M; row += step) {  // (the same rows for every thread of a workgroup, or of a wave)
+        double v[E];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        if constexpr (VEC) {
-            const int c = at(i, 0);
-            if (c < d.D) {
-                uint32_t w[2] = {0, 0};
+        for (int i = 0; i < NC; ++i) {
+            float s[CH];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    w[j / 4] |= code(v[8 * i + j]) << (8 * (j & 3));
-                *(uint2*)(qr + c) = uint2{w[0], w[1]};
+            for (int j = 0; j < CH; ++j) {
+                const float a = nx[i].at(j);
+                s[j] = a;
+                v[CH * i + j] = a;
+                if (y) {  // (float32 for S, as lpv_add_layernorm forms it; the codes take the sum itself)
+                    s[j] += ny[i].at(j);
+                    v[CH * i + j] += (double)ny[i].at(j);
+                }
             }
-        } else {
+            if (S) {
+                char* sr = S + row * d.lds * ES;
+                if constexpr (VEC) {
+                    if (at(i, 0) < d.D)
+                        store_sum<DT, CH>(sr + at(i, 0) * ES, s);
+                } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int c = at(i, j);
-                if (c < d.D)
-                    qr[c] = (int8_t)code(v[8 * i + j]);
+                    for (int j = 0; j < CH; ++j)
+                        if (at(i, j) < d.D)
+                            store_sum1<DT>(sr + at(i, j) * ES, s[j]);
+                }
+            }
+        }
+        if (row + step < d.M) {
+            load(nx, x + (row + step) * d.ldx * ES);
+            if (y)
+                load(ny, y + (row + step) * d.ldy * ES);
+        }
+        double sq = 0.0, factor = 1.0;
+        if constexpr (KIND == QUANT_LAYER) {
+            // Both sums in one go, of differences from the row's first element, which is no
+            // further from the mean than sqrt(D) standard deviations: what the difference of
+            // the two loses is at most 2^-52 D of the variance.
+            const double v0 = first_of<NT>(v[0], s_red, turn);
+            double sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (at(i / CH, i % CH) < d.D) {
+                    v[i] -= v0;
+                    sum += v[i];
+                    sq = fma(v[i], v[i], sq);
+                }
+            row_sums<NT>(sum, sq, s_red, turn);
+            const double mean = sum * d.per;
+            const double var = fmax(fma(-mean, mean, sq * d.per), 0.0) + d.eps;
+            factor = var > 0.0 ? fast_rsqrt(var) : __builtin_inf();
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                v[i] -= mean;
+            if (!(sum == sum) || !(sq == sq))  // (a maximum passes over a NaN)
+                factor = __builtin_nan("");
+        }
+        if constexpr (KIND == QUANT_RMS) {
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                sq = fma(v[i], v[i], sq);
+        }
+        if (!KEEP && KIND != QUANT_PLAIN)
+            load(g, gamma);
+        if (!KEEP && KIND == QUANT_LAYER)
+            load(b, beta);
+        double top = 0.0, poison = 0.0;  // (poison: not zero where a value is not finite)
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            if constexpr (KIND == QUANT_RMS)
+                v[i] *= (double)g[i / CH].at(i % CH);
+            if constexpr (KIND == QUANT_LAYER)  // (past the row's end gamma and beta are zero)
+                v[i] = fma(v[i] * factor, (double)g[i / CH].at(i % CH), (double)b[i / CH].at(i % CH));
+            top = fmax(top, fabs(v[i]));
+            poison = fma(v[i], 0.0, poison);
+        }
+        if constexpr (KIND == QUANT_RMS) {
+            sq = row_all<NT>(sq, Add(), s_red, turn);
+            factor = fast_rsqrt(fma(sq, d.per, d.eps));
+            poison = fma(sq, 0.0, poison);
+        }
+        // a row that is not finite has no largest value: a NaN does not pass a maximum, an
+        // infinity does
+        if (!(poison == 0.0))
+            top = __builtin_inf();
+        top = row_all<NT>(top, Max(), s_red, turn);
+        const bool bad = !(top < __builtin_inf());
+        const double sc = (KIND == QUANT_RMS ? top * factor : top) * (1.0 / 127.0);
+        if (tid == 0)
+            scale[row] = bad ? __builtin_nanf("") : top == 0.0 ? 0.0f : (float)sc;
+        const double inv = bad || top == 0.0 ? 0.0 : 127.0 * fast_rcp(top);
+        int8_t* qr = q + row * d.ldq;
+        auto code = [&](double u) -> uint32_t {
+            constexpr double FINE = 6144.0;               // 1.5 * 2^12
+            constexpr double WHOLE = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the integer
+            const double t = (fma(u, inv, FINE) - FINE) + WHOLE;
+            return bad ? 0u : (uint32_t)__builtin_bit_cast(uint64_t, t) & 0xff;
+        };
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            if constexpr (VEC) {
+                if (at(i, 0) < d.D) {
+                    uint32_t w[CH / 4] = {};
+#pragma unroll
+                    for (int j = 0; j < CH; ++j)
+                        w[j / 4] |= code(v[CH * i + j]) << (8 * (j & 3));
+                    if constexpr (CH == 4)
+                        *(uint32_t*)(qr + at(i, 0)) = w[0];
+                    else
+                        *(uint2*)(qr + at(i, 0)) = uint2{w[0], w[1]};
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < CH; ++j)
+                    if (at(i, j) < d.D)
+                        qr[at(i, j)] = (int8_t)code(v[CH * i + j]);
             }
         }
     }
 }
 
+// Workgroups of 256 threads that fill the chip's 256 compute units eight times over: the
+// rows past them follow, each behind its workgroup's last.
+constexpr int QUANT_WGS = 2048;
+
 template <int DT, int KIND> hipError_t launch_kind(const QuantRowsCall& c, hipStream_t s)
 {
-    const QuantDims d = {c.ldx, c.ldy, c.lds, c.ldq, c.M, c.D, c.eps};
-    // 16-byte pieces throughout: the row's length and every stride and address
-    auto even = [](const void* p, int64_t ld, int unit) {
-        return !p || ((uintptr_t)p % unit == 0 && ld % 8 == 0);
-    };
-    const bool vec = c.D % 8 == 0 && even(c.x, c.ldx, 16) && even(c.y, c.ldy, 16) &&
-                     even(c.S, c.lds, 16) && even(c.q, c.ldq, 8) && even(c.gamma, 0, 16) &&
-                     even(c.beta, 0, 16);
-#define LPV_ROWS(NT_, NC_)                                                                          \
+    const QuantDims d = {c.ldx, c.ldy, c.lds, c.ldq, c.M, c.D, c.eps, 1.0 / c.D};
+    // a thread's neighbours by one load throughout: the row's length and every stride and address
+    const int ch = c.D <= 1024 ? 4 : 8, unit = ch * (DT == 0 ? 4 : 2) < 16 ? 8 : 16;
+    auto even = [&](const void* p, int64_t ld, int u) { return !p || ((uintptr_t)p % u == 0 && ld % ch == 0); };
+    const bool vec = c.D % ch == 0 && even(c.x, c.ldx, unit) && even(c.y, c.ldy, unit) &&
+                     even(c.S, c.lds, unit) && even(c.q, c.ldq, ch) && even(c.gamma, 0, unit) &&
+                     even(c.beta, 0, unit);
+#define LPV_ROWS(NT_, NC_, CH_)                                                                     \
     do {                                                                                            \
-        const Grid2 g = grid_of(NT_ == 64 ? (c.M + 3) / 4 : c.M);                                   \
-        const dim3 grid(g.x, g.y), block(NT_ == 64 ? 256 : NT_);                                    \
+        const int64_t wgs = NT_ == 64 ? (c.M + 3) / 4 : c.M, most = NT_ == 1024 ? QUANT_WGS / 4 : QUANT_WGS; \
+        const int64_t rounds = (wgs + most - 1) / most;  /* the same number of rows to each */      \
+        const dim3 grid((unsigned)((wgs + rounds - 1) / rounds)), block(NT_ == 64 ? 256 : NT_);      \
         if (vec)                                                                                    \
-            hipLaunchKernelGGL((k_quant_rows<DT, KIND, NT_, NC_, true>), grid, block, 0, s, d,      \
+            hipLaunchKernelGGL((k_quant_rows<DT, KIND, NT_, NC_, CH_, true>), grid, block, 0, s, d, \
                                (const char*)c.x, (const char*)c.y, (const char*)c.gamma,            \
                                (const char*)c.beta, (char*)c.S, c.q, c.scale);                      \
         else                                                                                        \
-            hipLaunchKernelGGL((k_quant_rows<DT, KIND, NT_, NC_, false>), grid, block, 0, s, d,     \
+            hipLaunchKernelGGL((k_quant_rows<DT, KIND, NT_, NC_, CH_, false>), grid, block, 0, s, d, \
                                (const char*)c.x, (const char*)c.y, (const char*)c.gamma,            \
                                (const char*)c.beta, (char*)c.S, c.q, c.scale);                      \
         return hipGetLastError();                                                                   \
     } while (0)
+    if (c.D <= 256)
+        LPV_ROWS(64, 1, 4);
     if (c.D <= 512)
-        LPV_ROWS(64, 1);
+        LPV_ROWS(64, 2, 4);
+    if (c.D <= 768)
+        LPV_ROWS(64, 3, 4);
     if (c.D <= 1024)
-        LPV_ROWS(64, 2);
+        LPV_ROWS(64, 4, 4);
     if (c.D <= 2048)
-        LPV_ROWS(256, 1);
+        LPV_ROWS(256, 1, 8);
     if (c.D <= 4096)
-        LPV_ROWS(256, 2);
+        LPV_ROWS(256, 2, 8);
     if (c.D <= 8192)
-        LPV_ROWS(256, 4);
+        LPV_ROWS(256, 4, 8);
     if (c.D <= 16384)
-        LPV_ROWS(1024, 2);
-    LPV_ROWS(1024, 4);
+        LPV_ROWS(1024, 2, 8);
+    LPV_ROWS(1024, 4, 8);
 #undef LPV_ROWS
 }
 

@@ -13,7 +13,6 @@
 // output 8 (r / 4) + 4 (l / 32) + r % 4 of that token.  A 0 for a dropped 16 x 16 part of a
 // tile is exact in integers, whatever X holds.
 #include "lpv_device.h"
-#include "lpv_grid.h"
 #include "lpv_internal.h"
 #include "lpv_lds.h"
 
@@ -21,6 +20,11 @@ namespace lpv {
 namespace {
 
 typedef int i32x16 __attribute__((ext_vector_type(16)));
+// (one LDS area holds values of several types in turn: accesses that may alias)
+typedef __attribute__((may_alias)) uint32_t u32a;
+typedef __attribute__((may_alias)) uint64_t u64a;
+typedef __attribute__((address_space(3))) u32a* lds_u32;
+typedef __attribute__((address_space(3))) u64a* lds_u64;
 
 __device__ inline i32x16 mma8(v4i w, v4i x, i32x16 acc)
 {
@@ -45,9 +49,10 @@ __device__ inline bool tile_kept(const lpv_quant& h, const uint8_t* mask, int tr
     return kept;
 }
 
-__device__ inline int groups_of(uint32_t bits)
+// Halves (two columns) of a chunk's groups: one at least.
+__device__ inline int halves_of(uint32_t bits)
 {
-    return max((__popc((bits | bits >> 16) & 0xffff) + 3) / 4, 1);
+    return max((__popc((bits | bits >> 16) & 0xffff) + 1) / 2, 1);
 }
 
 // One wave to a pair of tile rows: the kept columns of its chunks.
@@ -55,7 +60,9 @@ __global__ __launch_bounds__(64) void k_quant_bits(const lpv_quant h, const uint
 {
     const int pair = blockIdx.x, lane = threadIdx.x;
     for (int c = 0; c < h.n_chunks; ++c) {
-        const bool kept = lane < 32 && tile_kept(h, mask, 2 * pair + (lane >> 4), c * QUANT_CHUNK + (lane & 15));
+        const int col = lane & 15;
+        const bool kept = lane < 32 && col < QUANT_CHUNK &&
+                          tile_kept(h, mask, 2 * pair + (lane >> 4), c * QUANT_CHUNK + col);
         const uint32_t bits = (uint32_t)__ballot(kept);
         if (lane == 0)
             h.bits[(int64_t)pair * h.n_chunks + c] = bits;
@@ -120,7 +127,8 @@ __global__ __launch_bounds__(256) void k_quant_fill(const lpv_quant h, const int
         h.scale[n] = n < h.N ? scale[n] : 0.0f;
     }
     const uint32_t* bits = h.bits + (int64_t)pair * h.n_chunks;
-    int tile = h.tile0[pair], group = pair * 4 * h.n_chunks;
+    int tile = h.tile0[pair], half = 0;
+    uint2* groups = h.groups + (int64_t)pair * QUANT_GROUPS * h.n_chunks;
     int at[2] = {0, 0};  // this pair's entries of either row in list
     if (2 * pair < h.n_tile_rows)
         at[0] = h.row_tile0[2 * pair];
@@ -130,44 +138,53 @@ __global__ __launch_bounds__(256) void k_quant_fill(const lpv_quant h, const int
         const uint32_t b = __builtin_amdgcn_readfirstlane(bits[c]);
         const uint32_t e = b & 0xffff, o = b >> 16, any = e | o;
         if ((c & 3) == wave) {
-            uint32_t left = any, desc = 0;
-            const uint32_t last = 1u << 24 | (c == h.n_chunks - 1 ? 1u << 25 : 0u);
-            int t = tile, n = 0, g = group, first = tile;
-            if (any == 0 && lane == 0)
-                h.groups[g] = uint2{last, (uint32_t)first};
-            while (left) {
-                const int col = __builtin_ctz(left);
-                left &= left - 1;
-                const uint32_t kept = (e >> col & 1) | (o >> col & 1) << 1;
-                desc |= (uint32_t)(col | kept << 4) << (6 * n++);
+            uint32_t left = any;
+            int t = tile;
+            for (int n = 0; n < halves_of(b); ++n) {
+                uint32_t desc = 0;
+                const int first = t;
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (kept >> j & 1) {
-                        const int tc = c * QUANT_CHUNK + col;
-                        const int64_t row = (int64_t)(2 * pair + j) * TILE + (lane & 31);
-                        const int64_t k = (int64_t)tc * TILE + 16 * (lane >> 5);
-                        uint4 v = {0, 0, 0, 0};
-                        if (row < h.N && k < h.K && (!mask || mask[row / h.b_r * h.C + k / h.b_c]))
-                            v = *(const uint4*)(W + row * ldw + k);
-                        *(uint4*)(h.tiles + (int64_t)t * 1024 + lane * 16) = v;
-                        if (lane == 0)
-                            h.list[at[j] + __popc((j ? o : e) & ((1u << col) - 1))] = int2{tc, t};
-                        ++t;
-                    }
-                if (n == 4 || left == 0) {
-                    if (lane == 0)
-                        h.groups[g] = uint2{left ? desc : desc | last, (uint32_t)first};
-                    ++g;
-                    n = 0;
-                    desc = 0;
-                    first = t;
+                for (int i = 0; i < 2; ++i) {
+                    if (!left)
+                        break;
+                    const int col = __builtin_ctz(left);
+                    left &= left - 1;
+                    const uint32_t kept = (e >> col & 1) | (o >> col & 1) << 1;
+                    desc |= (uint32_t)(col | kept << 4) << (6 * i);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (kept >> j & 1) {
+                            const int tc = c * QUANT_CHUNK + col;
+                            const int64_t row = (int64_t)(2 * pair + j) * TILE + (lane & 31);
+                            const int64_t k = (int64_t)tc * TILE + 16 * (lane >> 5);
+                            uint4 v = {0, 0, 0, 0};
+                            if (row < h.N && k < h.K && (!mask || mask[row / h.b_r * h.C + k / h.b_c]))
+                                v = *(const uint4*)(W + row * ldw + k);
+                            *(uint4*)(h.tiles + (int64_t)t * 1024 + lane * 16) = v;
+                            if (lane == 0)
+                                h.list[at[j] + __popc((j ? o : e) & ((1u << col) - 1))] = int2{tc, t};
+                            ++t;
+                        }
+                }
+                // (16 bits of the group's word, so that no other wave's half is written)
+                const int at_half = half + n;
+                const bool end = n == halves_of(b) - 1;
+                const bool pad = end && c == h.n_chunks - 1 && (at_half & 1) == 0;  // the pair's last half is empty
+                if (lane == 0) {
+                    uint16_t* w = (uint16_t*)(groups + at_half / 2);
+                    w[at_half & 1] = (uint16_t)(desc | (end && !pad ? 1u << 12 : 0u) |
+                                                (end && !pad && c == h.n_chunks - 1 ? 1u << 13 : 0u));
+                    if ((at_half & 1) == 0)
+                        groups[at_half / 2].y = (uint32_t)first;
+                    if (pad)
+                        w[1] = (uint16_t)(1u << 12 | 1u << 13);
                 }
             }
         }
         tile += __popc(e) + __popc(o);
         at[0] += __popc(e);
         at[1] += __popc(o);
-        group += groups_of(b);
+        half += halves_of(b);
     }
 }
 
@@ -231,80 +248,77 @@ struct QuantDims {
     int64_t n_units;
 };
 
-// 32 TU tokens times one tile row to a workgroup, whose 8 waves share the row's kept tiles, 8
-// neighbours of the list at a time; the partial sums meet in LDS.  Both operands come
-// straight from memory in operand order, so any size will do.
-constexpr int FEW_WAVES = 8;
-
-template <int OUT, bool GELU, int TU>
-__global__ __launch_bounds__(64 * FEW_WAVES) void k_quant_few(
+// 32 tokens times one tile row to a workgroup, whose WV waves share the row's kept tiles, every
+// WV-th of the list, U at a time and the next U already asked for; the partial sums meet in
+// LDS.  Both operands come straight from memory in operand order, so any size will do.
+template <int OUT, bool GELU, int WV, int U>
+__global__ __launch_bounds__(64 * WV) void k_quant_few(
     const QuantDims a, const int8_t* __restrict__ X, const float* __restrict__ xscale,
     const char* __restrict__ tiles, const int2* __restrict__ list, const int32_t* __restrict__ row_tile0,
     const float* __restrict__ wscale, const char* __restrict__ bias, char* __restrict__ Y)
 {
-    constexpr int ES = OUT == LPV_F32 ? 4 : 2, U = 4;  // tiles asked for at a time
-    __shared__ v4i s_part[FEW_WAVES][TU * 4][64];
+    constexpr int ES = OUT == LPV_F32 ? 4 : 2;
+    __shared__ v4i s_part[WV][4][64];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     for (int64_t unit = blockIdx.x; unit < a.n_units; unit += gridDim.x) {
         const int64_t mt = unit / a.n_tile_rows;
         const int row = (int)(unit - mt * a.n_tile_rows);
-        const int64_t m0 = mt * (32 * TU);
-        const int8_t* xr[TU];
-#pragma unroll
-        for (int u = 0; u < TU; ++u)
-            xr[u] = X + min(m0 + 32 * u + (lane & 31), a.M - 1) * a.ldx;
-        i32x16 acc[TU];
-#pragma unroll
-        for (int u = 0; u < TU; ++u)
-            acc[u] = i32x16{};
+        const int64_t m0 = mt * 32;
+        const int8_t* xr = X + min(m0 + (lane & 31), a.M - 1) * a.ldx;
+        i32x16 acc = {};
         const int t0 = row_tile0[row], n = row_tile0[row + 1] - t0;
-        // this wave's tiles: places wave, wave + 8, ... of the row's
-        const int mine = n > wave ? (n - wave + FEW_WAVES - 1) / FEW_WAVES : 0;
+        // this wave's tiles: places wave, wave + WV, ... of the row's
+        const int mine = n > wave ? (n - wave + WV - 1) / WV : 0;
         for (int base = 0; base < mine; base += 64) {
-            const int2 e = list[t0 + wave + FEW_WAVES * min(base + lane, mine - 1)];
+            const int2 e = list[t0 + wave + WV * min(base + lane, mine - 1)];
             const int here = min(mine - base, 64);
-            for (int i0 = 0; i0 < here; i0 += U) {
-                v4i w[U], x[U][TU];
+            v4i w[2][U], x[2][U];
+            auto load = [&](int i0, v4i(&wv)[U], v4i(&xv)[U]) __attribute__((always_inline)) {
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    const int p = min(i0 + i, here - 1);
+                    const int p = min(i0 + i, here - 1);  // (past the last: it again, and no product)
                     const int col = __builtin_amdgcn_readlane(e.x, p), t = __builtin_amdgcn_readlane(e.y, p);
-                    w[i] = *(const v4i*)(tiles + (int64_t)t * 1024 + lane * 16);
+                    wv[i] = *(const v4i*)(tiles + (int64_t)t * 1024 + lane * 16);
                     // (a half past K is zero in the tile: any codes do, the row's first)
                     int k = col * TILE + 16 * h;
                     k = k < a.K ? k : 0;
-#pragma unroll
-                    for (int u = 0; u < TU; ++u)
-                        x[i][u] = *(const v4i*)(xr[u] + k);
+                    xv[i] = *(const v4i*)(xr + k);
                 }
+            };
+            auto mul = [&](int i0, v4i(&wv)[U], v4i(&xv)[U]) __attribute__((always_inline)) {
 #pragma unroll
                 for (int i = 0; i < U; ++i)
                     if (i0 + i < here)
-#pragma unroll
-                        for (int u = 0; u < TU; ++u)
-                            acc[u] = mma8(w[i], x[i][u], acc[u]);
+                        acc = mma8(wv[i], xv[i], acc);
+            };
+            load(0, w[0], x[0]);
+            for (int i0 = 0; i0 < here; i0 += 2 * U) {
+                if (i0 + U < here)
+                    load(i0 + U, w[1], x[1]);
+                mul(i0, w[0], x[0]);
+                if (i0 + U < here) {
+                    if (i0 + 2 * U < here)
+                        load(i0 + 2 * U, w[0], x[0]);
+                    mul(i0 + U, w[1], x[1]);
+                }
             }
         }
 #pragma unroll
-        for (int u = 0; u < TU; ++u)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                s_part[wave][u * 4 + q][lane] = v4i{acc[u][4 * q], acc[u][4 * q + 1], acc[u][4 * q + 2],
-                                                    acc[u][4 * q + 3]};
+        for (int q = 0; q < 4; ++q)
+            s_part[wave][q][lane] = v4i{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
         __syncthreads();
-        for (int i = tid; i < TU * 256; i += 64 * FEW_WAVES) {
-            const int uq = i >> 6, l = i & 63;
+        if (tid < 256) {
+            const int q = tid >> 6;
             int s[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int w = 0; w < FEW_WAVES; ++w) {
-                const v4i v = s_part[w][uq][l];
+            for (int w = 0; w < WV; ++w) {
+                const v4i v = s_part[w][q][lane];
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
                     s[b] += v[b];
             }
-            const int64_t m = m0 + 32 * (uq >> 2) + (l & 31);
-            const int64_t at = (int64_t)row * TILE + 8 * (uq & 3) + 4 * (l >> 5);
+            const int64_t m = m0 + (lane & 31), at = (int64_t)row * TILE + 8 * q + 4 * h;
             if (m < a.M && at < a.N) {
                 float o[4];
                 finish4<OUT, GELU>(s, xscale[m], *(const float4*)(wscale + at), bias4<OUT>(bias, at), o);
@@ -319,43 +333,41 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void k_quant_few(
     }
 }
 
-template <int OUT, bool GELU, int TU>
+template <int OUT, bool GELU, int WV, int U>
 hipError_t launch_few(const lpv_quant* h, const QuantLinearCall& c, hipStream_t s)
 {
     QuantDims d = {c.ldx, c.M, h->K, h->N, c.ldy, h->n_tile_rows, 0};
-    d.n_units = (c.M + 32 * TU - 1) / (32 * TU) * h->n_tile_rows;
-    const dim3 grid((unsigned)(d.n_units < GRID_ROW ? d.n_units : GRID_ROW)), block(64 * FEW_WAVES);
-    hipLaunchKernelGGL((k_quant_few<OUT, GELU, TU>), grid, block, 0, s, d, c.X, c.xscale, h->tiles, h->list,
+    d.n_units = (c.M + 31) / 32 * h->n_tile_rows;
+    const dim3 grid((unsigned)(d.n_units < (1 << 16) ? d.n_units : (1 << 16))), block(64 * WV);
+    hipLaunchKernelGGL((k_quant_few<OUT, GELU, WV, U>), grid, block, 0, s, d, c.X, c.xscale, h->tiles, h->list,
                        h->row_tile0, h->scale, (const char*)c.bias, (char*)c.Y);
     return hipGetLastError();
 }
 
 // ---------------------------------------------------------------- many tokens
 
-// A workgroup of 8 waves takes items of 32 TU tokens times 8 pairs of tile rows (512 outputs), a
-// pair to a wave.  X goes by DMA into LDS a chunk (512 columns) at a time, two chunks in
+// A workgroup of WV waves takes items of 32 TU tokens times WV pairs of tile rows (64 WV outputs), a
+// pair to a wave.  X goes by DMA into LDS a chunk (256 columns) at a time, NS chunks in
 // turn; the pair's tiles come straight from memory into registers, since no other wave needs
-// them, four columns ahead.  A wave's work is a list of groups of four kept columns, made at
-// pack time: for each column it reads the tokens' codes from LDS, for one tile or both, and
-// has TU products for each.  So dropped tiles cost nothing, a column of X is read from LDS
-// once for two tiles, and waves meet at one barrier a chunk.
+// them, four columns ahead.  A wave's work is a list of kept columns, made at pack time: for
+// each it reads the tokens' codes from LDS, for one tile or both, and has TU products for
+// each.  So dropped tiles cost nothing, a column of X is read from LDS once for two tiles, and
+// waves meet at one barrier a chunk.
 //
 // LDS: panels of 128 columns, a row (token) of 128 bytes, its 16-byte piece c at
 // c ^ xswz(row): the 16 rows that are read at once lie in distinct banks.
 //
-// The wait before a chunk's barrier: the DMA of the next chunk is older than the tiles that
-// the wave has asked for since (8 loads a group, one group a chunk at least), and vector memory
-// comes back in order, so that all but the 8 youngest having come back is enough.
+// The waits count: vector memory comes back in order, so that a DMA is there once no more are
+// out than are known to be younger (the compiler's own waits know nothing of the DMA and wait for
+// more than they need).
 struct PanelDims {
     int64_t ldx, M, K, N, ldy;
     int32_t n_chunks, n_pairs;
     int32_t n_mt, n_pb;  // token tiles, blocks of 8 pairs
     int32_t n_items;
 };
-constexpr int PN_WAVES = 8;
 constexpr int PN_MG = 8;             // token tiles that share an XCD's L2 with several blocks of pairs
 constexpr int PN_STAGE = 4096;       // bytes of a wave's staging area
-constexpr int PN_AHEAD = 8;          // loads of tiles that a group asks for
 
 // Global -> LDS DMA of 4 bytes per lane to 256 bytes at a wave-uniform LDS address.
 __device__ inline void dma4(const char* base, uint32_t off, uint32_t lds)
@@ -368,14 +380,16 @@ __device__ inline void dma4(const char* base, uint32_t off, uint32_t lds)
         : "memory");
 }
 
-template <int OUT, bool GELU, int TU>
-__global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
+template <int OUT, bool GELU, int TU, int WV, int NS>
+__global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
     const PanelDims a, const char* X, const char* xscale, const char* tiles, const uint2* groups,
     const char* wscale, const char* bias, char* Y)
 {
     constexpr int ES = OUT == LPV_F32 ? 4 : 2;
-    constexpr int PANEL = TU * 4096, SLOT = 4 * PANEL;  // bytes
-    __shared__ uint4 smem[(2 * SLOT + PN_WAVES * PN_STAGE) / 16];
+    constexpr int PANEL = TU * 4096, SLOT = 2 * PANEL;  // bytes
+    constexpr int IPW = TU * 8 / WV;                    // DMA instructions of a wave and chunk
+    __shared__ uint4 smem[(NS * SLOT + WV * PN_STAGE) / 16];
+    static_assert(IPW * WV == TU * 8 && QUANT_CHUNK == 8, "a chunk is two panels, shared out evenly");
     // (an address that the compiler knows nothing about: loads from it stay on their side of the
     // DMA and of the waits, which count them)
     typedef const __attribute__((address_space(1))) char* global;
@@ -384,7 +398,7 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
 
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t lds = lds_addr(smem), stage = lds + 2 * SLOT + (uint32_t)wave * PN_STAGE;
+    const uint32_t lds = lds_addr(smem), stage = lds + NS * SLOT + (uint32_t)wave * PN_STAGE;
     const uint32_t loff = (uint32_t)lane * 16;
 
     // Items in order: groups of PN_MG token tiles, in each the blocks of pairs, in each its token
@@ -402,7 +416,7 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
         pb = rest / mg;
         mt = g * PN_MG + rest - pb * mg;
     };
-    const int per_pair = 4 * a.n_chunks;  // groups of a pair, at most
+    const int per_pair = QUANT_GROUPS * a.n_chunks;  // groups of a pair, at most
     // (the lane made opaque: what only such a part needs is not kept in registers through the
     // loop; the same below)
     auto fresh = [](int l) __attribute__((always_inline)) {
@@ -410,14 +424,15 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
         return l;
     };
     auto lanes_of = [&](int pb, int from) {  // groups from .. from + 63 of this wave's pair
-        const uint2* g = groups + (int64_t)(pb * PN_WAVES + wave) * per_pair;
+        const uint2* g = groups + (int64_t)(pb * WV + wave) * per_pair;
         return g[(uint32_t)min(from + fresh(lane), per_pair - 1)];
     };
 
-    // ---- the DMA of a chunk: wave w brings the rows 16 TU (w % 2) .. of panel w / 2
-    int d_k = 0, d_c = 0;  // its item and chunk
+    // ---- the DMA of a chunk: half of the waves to a panel, 8 IPW rows to a wave
+    int d_k = 0, d_c = 0, d_slot = 0;  // its item, chunk and slot
     const char* d_base = nullptr;
-    uint32_t d_row[2 * TU];
+    uint32_t d_row[IPW];
+    const int d_panel = wave / (WV / 2), d_first = wave % (WV / 2) * (8 * IPW);
     auto set_x = [&]() {
         int mt, pb;
         item(d_k, mt, pb);
@@ -426,21 +441,22 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
         const int last = (int)min((int64_t)32 * TU - 1, a.M - 1 - m0);  // rows past M repeat the last
         const int ln = fresh(lane);
 #pragma unroll
-        for (int i = 0; i < 2 * TU; ++i)
-            d_row[i] = (uint32_t)min(16 * TU * (wave & 1) + 8 * i + (ln >> 3), last) * (uint32_t)a.ldx;
+        for (int i = 0; i < IPW; ++i)
+            d_row[i] = (uint32_t)min(d_first + 8 * i + (ln >> 3), last) * (uint32_t)a.ldx;
     };
-    auto dma = [&](int slot) {
+    auto dma = [&]() {
         if (d_k >= my_items)
             return;
         const int ln = fresh(lane);
 #pragma unroll
-        for (int i = 0; i < 2 * TU; ++i) {
-            const int row = 8 * i + (ln >> 3);  // (16 TU (wave % 2) more: the same xswz)
-            const int k = d_c * (QUANT_CHUNK * TILE) + (wave >> 1) * 128 + ((ln & 7) ^ xswz(row)) * 16;
+        for (int i = 0; i < IPW; ++i) {
+            const int row = d_first + 8 * i + (ln >> 3);
+            const int k = (2 * d_c + d_panel) * 128 + ((ln & 7) ^ xswz(row)) * 16;
             // (past K the tiles are zero: any codes do, the row's first)
             dma16(d_base, d_row[i] + (uint32_t)(k < a.K ? k : 0),
-                  smem + (slot * SLOT + (wave >> 1) * PANEL + (wave & 1) * (TU * 2048) + i * 1024) / 16);
+                  smem + (d_slot * SLOT + d_panel * PANEL + d_first * 128 + i * 1024) / 16);
         }
+        d_slot = d_slot + 1 == NS ? 0 : d_slot + 1;
         if (++d_c == a.n_chunks) {
             d_c = 0;
             if (++d_k < my_items)
@@ -449,17 +465,15 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
     };
     // ---- what the epilogue of an item needs, into the wave's staging area: the outputs' scales
     // (256 bytes), their bias (256) and the tokens' scales
-    auto dma_params = [&](int k) {
-        int mt, pb;
-        item(k, mt, pb);
-        const int n0 = (pb * PN_WAVES + wave) * 64, ln = fresh(lane);
+    auto dma_params = [&](int mt, int pb) {
+        const int n0 = (pb * WV + wave) * 64, ln = fresh(lane);
         const int64_t m0 = (int64_t)mt * (32 * TU);
         dma4(wscale + (int64_t)n0 * 4, (uint32_t)ln * 4, stage);
         if (bias) {
             const int n = n0 + (OUT == LPV_F32 ? ln : 2 * (ln & 31));
             dma4(bias, (uint32_t)((n < a.N ? n : 0) * ES), stage + 256);
         } else {
-            *(__attribute__((address_space(3))) uint32_t*)(uintptr_t)(stage + 256 + ln * 4) = 0;
+            *(lds_u32)(uintptr_t)(stage + 256 + ln * 4) = 0;
         }
         const int last = (int)min((int64_t)32 * TU - 1, a.M - 1 - m0);
 #pragma unroll
@@ -468,32 +482,33 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
     };
 
     set_x();
-    dma(0);
-    dma_params(0);
-    int mt, pb, pb1;
+    dma();
+    int mt, pb, mt1, pb1, mt2, pb2;  // this item, the next and the one after it
     item(0, mt, pb);
-    uint2 dl = lanes_of(pb, 0);  // this item's groups, 64 at a time
-    item(1, mt, pb1);
+    item(1, mt1, pb1);
+    dma_params(mt, pb);
+    uint2 dl = lanes_of(pb, 0);       // this item's groups, 64 at a time
     uint2 nd = lanes_of(pb1, 0), n2;  // the next item's, and the one's after it
     asm volatile("" : "+v"(dl.x), "+v"(dl.y), "+v"(nd.x), "+v"(nd.y));
     int gi = 0, from = 0;  // the group being worked on: lane gi of dl, whose first is `from`
     uint32_t cur = __builtin_amdgcn_readlane(dl.x, 0);
 
-    // The tiles of four columns: of a column with one tile, that one twice.
+    // The tiles of four columns: of a column with one tile, that one twice.  (At most 2^22 tiles:
+    // byte offsets fit 32 bits.)
     v4i w[4][2];
     typedef const __attribute__((address_space(1))) v4i* global4;
-    auto load_w = [&](int i, uint32_t desc, global& p) __attribute__((always_inline)) {
-        const uint32_t ab = desc >> (6 * i + 4) & 3;
-        w[i][0] = *(global4)(p + loff);
-        p += ab == 3 ? 1024 : 0;
-        w[i][1] = *(global4)(p + loff);
-        p += ab ? 1024 : 0;
+    auto load_w = [&](int i, uint32_t desc, uint32_t& at) __attribute__((always_inline)) {
+        const uint32_t ab = desc >> (16 * (i / 2) + 6 * (i & 1) + 4) & 3;
+        w[i][0] = *(global4)(wt + (at + loff));
+        at += ab == 3 ? 1024 : 0;
+        w[i][1] = *(global4)(wt + (at + loff));
+        at += ab ? 1024 : 0;
     };
     {
-        global p = wt + (int64_t)__builtin_amdgcn_readlane(dl.y, 0) * 1024;
+        uint32_t at = (uint32_t)__builtin_amdgcn_readlane(dl.y, 0) * 1024;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            load_w(i, cur, p);
+            load_w(i, cur, at);
     }
     // The codes of the tokens at a column of the chunk: lane l has row l % 32 (+ 32 u), pieces 2 c and
     // 2 c + 1 of the panel by l / 32.
@@ -501,11 +516,11 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
     const uint32_t xbase = lds + fr * 128, xpiece = (uint32_t)(h ^ xswz(fr)) << 4;
     v4i x[2][TU];
     auto read_x = [&](v4i(&o)[TU], uint32_t desc, int i, uint32_t slot) __attribute__((always_inline)) {
-        const uint32_t c = desc >> (6 * i) & 15;
+        const uint32_t c = desc >> (16 * (i / 2) + 6 * (i & 1)) & 15;
         const uint32_t at = xbase + (xpiece ^ (c & 3) << 5) + (slot + (c >> 2) * PANEL);
 #pragma unroll
         for (int u = 0; u < TU; ++u)
-            o[u] = *(const __attribute__((address_space(3))) v4i*)(uintptr_t)(at + u * 4096);
+            o[u] = lds_read16<0>(at + u * 4096);
     };
     i32x16 acc[2][TU];
 #pragma unroll
@@ -514,71 +529,84 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
         for (int u = 0; u < TU; ++u)
             acc[j][u] = i32x16{};
 
-    auto sync = [&]() {
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"i"(PN_AHEAD) : "memory");
-    };
-    sync();
-    dma(1);
     uint32_t slot = 0;
+    // The end of a chunk: the next one has landed (for every wave, behind the barrier), and every
+    // wave has read this one, whose place the DMA takes.  What is younger than the next one's
+    // DMA: 4 loads of tiles at least in each of the NS - 1 chunks since (fewer before there were
+    // that many); what is younger than an item's scales and bias at its end: 8.
+    int chunks = 0;
+    auto sync = [&](bool at_end) __attribute__((always_inline)) {
+        constexpr int AHEAD = 4 * (NS - 1);
+        if (NS > 2 && chunks >= NS - 1) {
+            if (at_end)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"i"(AHEAD < 8 ? AHEAD : 8) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"i"(AHEAD) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n s_barrier" ::: "memory");
+        }
+        ++chunks;
+    };
+    asm volatile("s_waitcnt vmcnt(8)\n s_barrier" ::: "memory");  // (the tiles' loads are younger)
+#pragma unroll
+    for (int i = 1; i < NS; ++i)
+        dma();
     for (int k = 0; k < my_items; ++k) {
-        {
-            int mt2, pb2;
-            item(k + 2, mt2, pb2);
-            n2 = lanes_of(pb2, 0);
-        }
-        for (int c = 0; c < a.n_chunks; ++c) {
-            read_x(x[0], cur, 0, slot);
-            for (;;) {  // the chunk's groups
-                const bool last = cur >> 24 & 1;
-                uint32_t next, first;
-                if (cur >> 25 & 1) {
-                    next = __builtin_amdgcn_readlane(nd.x, 0);
-                    first = __builtin_amdgcn_readlane(nd.y, 0);
-                } else {
-                    if (__builtin_expect(++gi == 64, 0)) {
-                        gi = 0;
-                        from += 64;
-                        dl = lanes_of(pb, from);
-                        asm volatile("" : "+v"(dl.x), "+v"(dl.y));
-                    }
-                    next = __builtin_amdgcn_readlane(dl.x, gi);
-                    first = __builtin_amdgcn_readlane(dl.y, gi);
+        item(k + 2, mt2, pb2);
+        n2 = lanes_of(pb2, 0);
+        read_x(x[0], cur, 0, slot);
+        bool done;
+        do {  // the pair's groups
+            uint32_t next, first;
+            done = cur >> 29 & 1;
+            if (done) {
+                next = __builtin_amdgcn_readlane(nd.x, 0);
+                first = __builtin_amdgcn_readlane(nd.y, 0);
+            } else {
+                if (__builtin_expect(++gi == 64, 0)) {
+                    gi = 0;
+                    from += 64;
+                    dl = lanes_of(pb, from);
+                    asm volatile("" : "+v"(dl.x), "+v"(dl.y));
                 }
-                global p = wt + (int64_t)first * 1024;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (i < 3)
-                        read_x(x[(i + 1) & 1], cur, i + 1, slot);
-                    else if (!last)
-                        read_x(x[0], next, 0, slot);
-                    if (cur >> (6 * i + 4) & 1)
-#pragma unroll
-                        for (int u = 0; u < TU; ++u)
-                            acc[0][u] = mma8(w[i][0], x[i & 1][u], acc[0][u]);
-                    if (cur >> (6 * i + 5) & 1)
-#pragma unroll
-                        for (int u = 0; u < TU; ++u)
-                            acc[1][u] = mma8(w[i][1], x[i & 1][u], acc[1][u]);
-                    load_w(i, next, p);
-                }
-                cur = next;
-                if (last)
-                    break;
+                next = __builtin_amdgcn_readlane(dl.x, gi);
+                first = __builtin_amdgcn_readlane(dl.y, gi);
             }
-            if (c == 0)
-                asm volatile("" : "+v"(n2.x), "+v"(n2.y));
-            sync();
-            dma(slot ? 1 : 0);
-            slot ^= SLOT;
-        }
+            uint32_t at = first * 1024;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool end = (i & 1) && (cur >> (i == 1 ? 12 : 28) & 1);  // of the chunk
+                if (!end)
+                    read_x(x[(i + 1) & 1], i < 3 ? cur : next, (i + 1) & 3, slot);
+                if (cur >> (16 * (i / 2) + 6 * (i & 1) + 4) & 1)
+#pragma unroll
+                    for (int u = 0; u < TU; ++u)
+                        acc[0][u] = mma8(w[i][0], x[i & 1][u], acc[0][u]);
+                if (cur >> (16 * (i / 2) + 6 * (i & 1) + 5) & 1)
+#pragma unroll
+                    for (int u = 0; u < TU; ++u)
+                        acc[1][u] = mma8(w[i][1], x[i & 1][u], acc[1][u]);
+                load_w(i, next, at);
+                if (end) {
+                    sync(i == 3);
+                    dma();
+                    slot = slot + SLOT == NS * SLOT ? 0 : slot + SLOT;
+                    if (i == 1)
+                        read_x(x[0], cur, 2, slot);
+                    else if (!done)
+                        read_x(x[0], next, 0, slot);
+                }
+            }
+            cur = next;
+        } while (!done);
+        asm volatile("" : "+v"(n2.x), "+v"(n2.y));
         // ---- the item's outputs
-        item(k, mt, pb);
-        const int64_t m0 = (int64_t)mt * (32 * TU), n0 = (int64_t)(pb * PN_WAVES + wave) * 64;
+        const int64_t m0 = (int64_t)mt * (32 * TU), n0 = (int64_t)(pb * WV + wave) * 64;
         const int ln = fresh(lane), fr = ln & 31, h = ln >> 5;
         float xs[TU];
 #pragma unroll
         for (int u = 0; u < TU; ++u)
-            xs[u] = *(const __attribute__((address_space(3))) float*)(uintptr_t)(stage + 512 + (32 * u + fr) * 4);
+            xs[u] = __uint_as_float(*(lds_u32)(uintptr_t)(stage + 512 + (32 * u + fr) * 4));
         uint2 pk[TU][2][4];    // 16-bit outputs: four to a place
         float4 pf[OUT == LPV_F32 ? TU : 1][2][4];
 #pragma unroll
@@ -592,7 +620,7 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
                     b = __builtin_bit_cast(float4, lds_read16<256>(stage + n * 4));
                 } else {
                     using E = Elem<OUT>;
-                    const uint64_t v = *(const __attribute__((address_space(3))) uint64_t*)(uintptr_t)(stage + 256 + n * 2);
+                    const uint64_t v = *(lds_u64)(uintptr_t)(stage + 256 + n * 2);
                     b = float4{E::to_f32((uint16_t)v), E::to_f32((uint16_t)(v >> 16)),
                                E::to_f32((uint16_t)(v >> 32)), E::to_f32((uint16_t)(v >> 48))};
                 }
@@ -611,6 +639,10 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
         // c ^ xswz(t)), so that whole lines leave; streamed past the caches, which X and the
         // tiles want
         const int lt = ln >> 3, lp = ln & 7;
+        const bool inside = m0 + 32 * TU <= a.M && n0 + 64 <= a.N;
+        typedef __attribute__((address_space(1))) char* global_w;
+        // (32 bits: eight rows of a stride of at most 2^22)
+        const uint32_t y_off = ((uint32_t)lt * (uint32_t)a.ldy + (uint32_t)lp * (16 / ES)) * ES;
 #pragma unroll
         for (int u = 0; u < TU; ++u) {
 #pragma unroll
@@ -625,27 +657,40 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
                         if constexpr (OUT == LPV_F32)
                             lds_write16(at + (((2 * q + h) ^ xswz(fr)) << 4), __builtin_bit_cast(v4i, pf[u][j][q]));
                         else
-                            *(__attribute__((address_space(3))) uint64_t*)(uintptr_t)(
-                                at + (((4 * j + q) ^ xswz(fr)) << 4) + 8 * h) = __builtin_bit_cast(uint64_t, pk[u][j][q]);
+                            *(lds_u64)(uintptr_t)(at + (((4 * j + q) ^ xswz(fr)) << 4) + 8 * h) =
+                                __builtin_bit_cast(uint64_t, pk[u][j][q]);
                     }
                 }
+                v4i v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = 8 * i + lt;
-                    const v4i v = lds_read16<0>(stage + t * 128 + ((lp ^ xswz(t)) << 4));
-                    const int64_t m = m0 + 32 * u + t, n = n0 + 32 * half + lp * (16 / ES);
-                    if (m < a.M && n < a.N)
-                        __builtin_nontemporal_store(v, (v4i*)(Y + (m * a.ldy + n) * ES));
+                    v[i] = lds_read16<0>(stage + t * 128 + ((lp ^ xswz(t)) << 4));
+                }
+                global_w y = (global_w)Y + ((m0 + 32 * u) * a.ldy + n0 + 32 * half) * ES;
+                typedef __attribute__((address_space(1))) v4i* out4;
+                if (inside) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i, y += 8 * a.ldy * ES) {
+                        asm volatile("" : "+s"(y));  // (the wave's address: the lane's offset stays 32 bits)
+                        __builtin_nontemporal_store(v[i], (out4)(y + y_off));
+                    }
+                } else {
+                    const int rows = (int)min((int64_t)32, a.M - (m0 + 32 * u));
+                    if (n0 + 32 * half + lp * (16 / ES) < a.N)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (8 * i + lt < rows)
+                                __builtin_nontemporal_store(v[i], (out4)(y + 8 * i * a.ldy * ES + y_off));
                 }
             }
         }
         if (k + 1 < my_items)
-            dma_params(k + 1);
+            dma_params(mt1, pb1);
+        mt = mt1;
         pb = pb1;
-        {
-            int mt2;
-            item(k + 2, mt2, pb1);
-        }
+        mt1 = mt2;
+        pb1 = pb2;
         dl = nd;
         nd = n2;
         gi = from = 0;
@@ -659,22 +704,22 @@ __global__ __launch_bounds__(64 * PN_WAVES, TU == 1 ? 4 : 2) void k_quant_panel(
     __builtin_amdgcn_s_waitcnt(0);
 }
 
-template <int OUT, bool GELU, int TU>
-hipError_t launch_panel(const lpv_quant* h, const QuantLinearCall& c, int n_cus, hipStream_t s)
+template <int OUT, bool GELU, int TU, int WV, int NS>
+hipError_t launch_panel(const lpv_quant* h, const QuantLinearCall& c, int n_cus, int per_cu, hipStream_t s)
 {
     PanelDims d = {c.ldx, c.M, h->K, h->N, c.ldy, h->n_chunks, h->n_pairs};
     // token tiles of one launch: items in 31 bits
-    d.n_pb = h->n_pairs / PN_WAVES;
+    d.n_pb = ((h->n_tile_rows + 1) / 2 + WV - 1) / WV;
     const int64_t most = ((int64_t)1 << 30) / d.n_pb;
-    const int wgs = max(n_cus & ~7, 8) * (TU == 1 ? 2 : 1);
+    const int wgs = max(n_cus & ~7, 8) * per_cu;
     for (int64_t m = 0, n_mt = (c.M + 32 * TU - 1) / (32 * TU); n_mt > 0; m += most, n_mt -= most) {
         d.n_mt = (int32_t)(n_mt < most ? n_mt : most);
         d.n_items = d.n_mt * d.n_pb;
         const int64_t m0 = m * (32 * TU);
         d.M = c.M - m0;
         const int need = (int)(((int64_t)d.n_items + 7) / 8 * 8);
-        const dim3 grid((unsigned)(need < wgs ? need : wgs)), block(64 * PN_WAVES);
-        hipLaunchKernelGGL((k_quant_panel<OUT, GELU, TU>), grid, block, 0, s, d, (const char*)c.X + m0 * c.ldx,
+        const dim3 grid((unsigned)(need < wgs ? need : wgs)), block(64 * WV);
+        hipLaunchKernelGGL((k_quant_panel<OUT, GELU, TU, WV, NS>), grid, block, 0, s, d, (const char*)c.X + m0 * c.ldx,
                            (const char*)(c.xscale + m0), (const char*)h->tiles, (const uint2*)h->groups,
                            (const char*)h->scale, (const char*)c.bias,
                            (char*)c.Y + m0 * c.ldy * (OUT == LPV_F32 ? 4 : 2));
@@ -685,29 +730,23 @@ hipError_t launch_panel(const lpv_quant* h, const QuantLinearCall& c, int n_cus,
     return hipSuccess;
 }
 
-inline int num_cus()
-{
-    int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess ||
-        hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0)
-        n = 256;
-    return n;
-}
-
 template <int OUT, bool GELU> hipError_t launch_as(const lpv_quant* h, const QuantLinearCall& c, hipStream_t s)
 {
-    const int cus = num_cus();
-    const int64_t pbs = h->n_pairs / PN_WAVES;
-    auto items = [&](int t) { return (c.M + t - 1) / t * pbs; };
-    if (items(128) >= cus)
-        return launch_panel<OUT, GELU, 4>(h, c, cus, s);
-    if (items(64) >= cus)
-        return launch_panel<OUT, GELU, 2>(h, c, cus, s);
-    if (items(32) >= cus / 2)
-        return launch_panel<OUT, GELU, 1>(h, c, cus, s);
-    if (c.M <= 32)
-        return launch_few<OUT, GELU, 1>(h, c, s);
-    return launch_few<OUT, GELU, 2>(h, c, s);
+    const int cus = h->n_cus;
+    const int64_t pairs = (h->n_tile_rows + 1) / 2;
+    auto items = [&](int tokens, int wv) { return (c.M + tokens - 1) / tokens * ((pairs + wv - 1) / wv); };
+    if ((c.M + 31) / 32 * h->n_tile_rows <= 1400) {
+        if (h->n_tiles <= 48 * (int64_t)h->n_tile_rows)
+            return launch_few<OUT, GELU, 4, 4>(h, c, s);
+        return launch_few<OUT, GELU, 8, 4>(h, c, s);
+    }
+    if (h->K >= 2048 && items(128, 8) >= cus)
+        return launch_panel<OUT, GELU, 4, 8, 4>(h, c, cus, 1, s);
+    if (items(128, 4) >= 3 * cus)
+        return launch_panel<OUT, GELU, 4, 4, 2>(h, c, cus, 2, s);
+    if (items(64, 4) >= cus)
+        return launch_panel<OUT, GELU, 2, 4, 4>(h, c, cus, 2, s);
+    return launch_panel<OUT, GELU, 1, 4, 4>(h, c, cus, 3, s);
 }
 
 template <int OUT> hipError_t launch_out(const lpv_quant* h, const QuantLinearCall& c, hipStream_t s)

@@ -708,41 +708,73 @@ def distill_grad(logits, ids, teacher, temperature, dloss=None, loss=None, dlogi
     return loss, dlogits
 
 
-def _quant_rows(where, x, y, params, S, q, scale, stream):
+def _device(dev, *tensors):
+    """The current device, if every tensor (name, tensor or None) lives on it; dev: theirs, if
+    the caller has compared them already (it costs less host time than a loop)."""
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        _on_current(*tensors)
+    return dev
+
+
+def _stream_on(dev, stream):
+    """The address of ``stream``, or of the current one of device ``dev``."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+
+
+def _own_stream(stream):
+    """Refuses a stream that is not the current one: torch's allocator orders a new tensor's
+    memory by that."""
+    if _stream(stream).value != _stream(None).value:
+        raise ValueError("a call on a stream that is not the current one takes its outputs")
+
+
+def _quant_rows(call, where, x, y, params, S, q, scale, stream):
     """The arguments that the calls that give rows in 8-bit codes share; params: what comes
     between the element type and S."""
     if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in DTYPES:
         raise ValueError("x must be a 2-D tensor of float32, float16 or bfloat16")
     M, D = x.shape
-    dt, dev = x.dtype, x.device
-    if q is None:
-        q = torch.empty((M, D), dtype=torch.int8, device=dev)
-    if scale is None:
-        scale = torch.empty(M, dtype=torch.float32, device=dev)
-    elif not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or scale.shape != (M,) \
-            or not scale.is_contiguous():
-        raise ValueError("scale must be a contiguous float32 tensor of M elements")
+    dt = x.dtype
     xp, ldx = _rows(x, "x", M, D, dt)
     yp, ldy = _rows(y, "y", M, D, dt) if y is not None else (None, 0)
     sp, lds = _rows(S, "S", M, D, dt) if S is not None else (None, 0)
-    qp, ldq = _rows(q, "q", M, D, torch.int8)
-    _on_current(("x", x), ("y", y), ("S", S), ("q", q), ("scale", scale))
-    _check(getattr(lib(), where)(xp, ldx, yp, ldy, M, D, DTYPES[dt], *params, sp, lds, qp, ldq,
-                                 scale.data_ptr(), _stream(stream)), where)
+    dev = x.get_device()
+    if stream is not None and (q is None or scale is None):
+        _own_stream(stream)
+    if q is None:
+        q = x.new_empty((M, D), dtype=torch.int8)
+        qp, ldq = q.data_ptr(), D
+    else:
+        qp, ldq = _rows(q, "q", M, D, torch.int8)
+        dev = dev if q.get_device() == dev else -1
+    if scale is None:
+        scale = x.new_empty(M, dtype=torch.float32)
+    elif not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or scale.shape != (M,) \
+            or not scale.is_contiguous():
+        raise ValueError("scale must be a contiguous float32 tensor of M elements")
+    if scale.get_device() != dev or (y is not None and y.get_device() != dev) \
+            or (S is not None and S.get_device() != dev):
+        dev = -1
+    dev = _device(dev, ("x", x), ("y", y), ("S", S), ("q", q), ("scale", scale))
+    st = call(xp, ldx, yp, ldy, M, D, DTYPES[dt], *params, sp, lds, qp, ldq, scale.data_ptr(),
+              _stream_on(dev, stream))
+    if st:
+        _check(st, where)
     return q, scale
 
 
 def quant_rows(x, y=None, S=None, q=None, scale=None, stream=None):
     """lpv_quant_rows: (q, scale), the rows of x (+ y) in 8-bit codes (int8 M x D) with a
     scale for each row (M float32); the sum is written to S when given (which may be x or y)."""
-    return _quant_rows("lpv_quant_rows", x, y, (), S, q, scale, stream)
+    return _quant_rows(lib().lpv_quant_rows, "lpv_quant_rows", x, y, (), S, q, scale, stream)
 
 
 def _norm_param(t, name, x):
     if not isinstance(t, torch.Tensor) or t.dtype != x.dtype or t.shape != x.shape[1:] \
             or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of %d elements" % (name, x.dtype, x.shape[1]))
-    _on_current((name, t))
+    if t.get_device() != x.get_device():
+        _on_current((name, t))
     return t.data_ptr()
 
 
@@ -750,16 +782,16 @@ def add_rmsnorm_quant(x, y, gamma, eps, S=None, q=None, scale=None, stream=None)
     """lpv_add_rmsnorm_quant: s = x + y (y may be None), and (q, scale), the rows of
     s / sqrt(mean(s^2) + eps) * gamma in 8-bit codes with a scale for each; s is written to
     S when given (which may be x or y)."""
-    return _quant_rows("lpv_add_rmsnorm_quant", x, y, (_norm_param(gamma, "gamma", x), float(eps)), S, q,
-                       scale, stream)
+    return _quant_rows(lib().lpv_add_rmsnorm_quant, "lpv_add_rmsnorm_quant", x, y,
+                       (_norm_param(gamma, "gamma", x), eps), S, q, scale, stream)
 
 
 def add_layernorm_quant(x, y, gamma, beta, eps, S=None, q=None, scale=None, stream=None):
     """lpv_add_layernorm_quant: as ``add_rmsnorm_quant`` with the layer norm of
     ``add_layernorm``, LN(s) * gamma + beta."""
-    return _quant_rows("lpv_add_layernorm_quant", x, y,
-                       (_norm_param(gamma, "gamma", x), _norm_param(beta, "beta", x), float(eps)), S, q,
-                       scale, stream)
+    return _quant_rows(lib().lpv_add_layernorm_quant, "lpv_add_layernorm_quant", x, y,
+                       (_norm_param(gamma, "gamma", x), _norm_param(beta, "beta", x), eps), S, q, scale,
+                       stream)
 
 
 class QuantWeight:
@@ -819,23 +851,35 @@ def quant_linear(h, X, xscale, bias=None, Y=None, dtype=None, epi=None, stream=N
     without either); allocated if not given."""
     if not isinstance(X, torch.Tensor) or X.dim() != 2:
         raise ValueError("X must be a 2-D int8 tensor")
-    M = X.shape[0]
+    M, N = X.shape[0], h.N
     dt = Y.dtype if Y is not None else dtype if dtype is not None else bias.dtype if bias is not None \
         else torch.bfloat16
-    if dt not in DTYPES or (dtype is not None and dtype != dt):
+    code = DTYPES.get(dt)
+    if code is None or (dtype is not None and dtype != dt):
         raise TypeError("outputs of %s: float32, float16 or bfloat16, the same as Y's" % dt)
-    if bias is not None and (not isinstance(bias, torch.Tensor) or bias.dtype != dt or bias.shape != (h.N,)
-                             or not bias.is_contiguous()):
-        raise ValueError("bias must be a contiguous %s tensor of N = %d elements" % (dt, h.N))
+    bp = None
+    if bias is not None:
+        if not isinstance(bias, torch.Tensor) or bias.dtype != dt or bias.shape != (N,) or not bias.is_contiguous():
+            raise ValueError("bias must be a contiguous %s tensor of N = %d elements" % (dt, N))
+        bp = bias.data_ptr()
     if not isinstance(xscale, torch.Tensor) or xscale.dtype != torch.float32 or xscale.shape != (M,) \
             or not xscale.is_contiguous():
         raise ValueError("xscale must be a contiguous float32 tensor of M elements")
-    if Y is None:
-        Y = torch.empty((M, h.N), dtype=dt, device=X.device)
+    dev = X.get_device()
+    if xscale.get_device() != dev or (bias is not None and bias.get_device() != dev):
+        dev = -1
     xp, ldx = _rows(X, "X", M, h.K, torch.int8)
-    yp, ldy = _rows(Y, "Y", M, h.N, dt)
-    _on_current(("X", X), ("xscale", xscale), ("bias", bias), ("Y", Y))
-    _check(lib().lpv_quant_linear(h.handle, xp, ldx, xscale.data_ptr(), M,
-                                  bias.data_ptr() if bias is not None else None, yp, ldy, DTYPES[dt],
-                                  EPI[epi], _stream(stream)), "lpv_quant_linear")
+    if Y is None:
+        if stream is not None:
+            _own_stream(stream)
+        Y = X.new_empty((M, N), dtype=dt)
+        yp, ldy = Y.data_ptr(), N
+    else:
+        yp, ldy = _rows(Y, "Y", M, N, dt)
+        dev = dev if Y.get_device() == dev else -1
+    dev = _device(dev, ("X", X), ("xscale", xscale), ("bias", bias), ("Y", Y))
+    st = lib().lpv_quant_linear(h._h, xp, ldx, xscale.data_ptr(), M, bp, yp, ldy, code, EPI[epi],
+                                _stream_on(dev, stream))
+    if st:
+        _check(st, "lpv_quant_linear")
     return Y
