@@ -26,10 +26,11 @@
  * - X, W, bias and Y share one element type (lpv_dtype).  Arithmetic inside
  *   the kernels is float32 (bf16/fp16 inputs go to the matrix cores with float32
  *   accumulation); the result is rounded once, to nearest even, to the element
- *   type.
+ *   type.  (The calls on rows in 8-bit codes name their types themselves: the codes
+ *   are int8, the scales float32, the sums of products 32-bit integers.)
  * - `stream` is a hipStream_t (NULL = the default stream).  Every call only
- *   enqueues work on it and returns, except lpv_bsr_pack, which waits once for
- *   its own work (see there).
+ *   enqueues work on it and returns, except lpv_bsr_pack and lpv_quant_pack, which
+ *   wait for their own work (see there).
  * - Every argument is checked before any HIP call; a bad argument returns a
  *   negative lpv_status and changes nothing.  lpv_last_error() then gives a
  *   message for the calling thread.  No exception crosses the ABI.
@@ -640,7 +641,8 @@ lpv_status lpv_quant_info_get(const lpv_quant* h, lpv_quant_info* out);
  * bias    device, N elements of type dt, or NULL for no bias.
  * Y       device, M x N of type dt (each of lpv_dtype), row stride N <= ldy <= 2^22, a multiple of 16
  *         bytes; must not overlap X, xscale or bias.
- * epi     LPV_EPI_NONE or LPV_EPI_GELU, as lpv_bsr_linear (float32 outputs: to 1e-6 relative).
+ * epi     LPV_EPI_NONE or LPV_EPI_GELU, as lpv_bsr_linear (float32 outputs: positive ones to 3e-7
+ *         relative, negative ones to 1e-7).
  * The sums are 32-bit integers and exact; they, the scales and the bias meet in float32, and
  * the result is rounded once, so a row's bits depend on neither the other rows nor M.
  * No allocation, no host synchronisation.  M = 0 is a no-op.

@@ -190,9 +190,10 @@ __global__ __launch_bounds__(256) void k_quant_fill(const lpv_quant h, const int
 
 // ---------------------------------------------------------------- the epilogue's arithmetic
 
-// GELU for float32 outputs, as gelu_erf with f of degree 11 (gelu_fit.fit(11)): to 2e-7
-// relative near zero, 2e-6 in the tail, where gelu_erf's 3e-6 to 5e-6 would show in
-// the outputs' own type.
+// GELU for float32 outputs, as gelu_erf with f of degree 11 (gelu_fit.fit(11)): positive
+// outputs to 3e-7 relative, negative ones to 1e-7 (4e-6 relative at -5.5, where the
+// rounding of the exponent itself shows), where gelu_erf's 3e-6 to 5e-6 would show in the
+// outputs' own type.
 __device__ inline float gelu_f32(float v)
 {
     const float a = fabsf(v) * 0.70710678118654752f;
@@ -245,7 +246,6 @@ template <int OUT> __device__ inline float4 bias4(const char* bias, int64_t n)
 struct QuantDims {
     int64_t ldx, M, K, N, ldy;
     int32_t n_tile_rows;
-    int64_t n_units;
 };
 
 // 32 tokens times one tile row to a workgroup, whose WV waves share the row's kept tiles, every
@@ -261,84 +261,79 @@ __global__ __launch_bounds__(64 * WV) void k_quant_few(
     __shared__ v4i s_part[WV][4][64];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    for (int64_t unit = blockIdx.x; unit < a.n_units; unit += gridDim.x) {
-        const int64_t mt = unit / a.n_tile_rows;
-        const int row = (int)(unit - mt * a.n_tile_rows);
-        const int64_t m0 = mt * 32;
-        const int8_t* xr = X + min(m0 + (lane & 31), a.M - 1) * a.ldx;
-        i32x16 acc = {};
-        const int t0 = row_tile0[row], n = row_tile0[row + 1] - t0;
-        // this wave's tiles: places wave, wave + WV, ... of the row's
-        const int mine = n > wave ? (n - wave + WV - 1) / WV : 0;
-        for (int base = 0; base < mine; base += 64) {
-            const int2 e = list[t0 + wave + WV * min(base + lane, mine - 1)];
-            const int here = min(mine - base, 64);
-            v4i w[2][U], x[2][U];
-            auto load = [&](int i0, v4i(&wv)[U], v4i(&xv)[U]) __attribute__((always_inline)) {
+    const int row = (int)(blockIdx.x % (unsigned)a.n_tile_rows);
+    const int64_t m0 = (int64_t)(blockIdx.x / (unsigned)a.n_tile_rows) * 32;
+    const int8_t* xr = X + min(m0 + (lane & 31), a.M - 1) * a.ldx;
+    i32x16 acc = {};
+    const int t0 = row_tile0[row], n = row_tile0[row + 1] - t0;
+    // this wave's tiles: places wave, wave + WV, ... of the row's
+    const int mine = n > wave ? (n - wave + WV - 1) / WV : 0;
+    for (int base = 0; base < mine; base += 64) {
+        const int2 e = list[t0 + wave + WV * min(base + lane, mine - 1)];
+        const int here = min(mine - base, 64);
+        v4i w[2][U], x[2][U];
+        auto load = [&](int i0, v4i(&wv)[U], v4i(&xv)[U]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < U; ++i) {
-                    const int p = min(i0 + i, here - 1);  // (past the last: it again, and no product)
-                    const int col = __builtin_amdgcn_readlane(e.x, p), t = __builtin_amdgcn_readlane(e.y, p);
-                    wv[i] = *(const v4i*)(tiles + (int64_t)t * 1024 + lane * 16);
-                    // (a half past K is zero in the tile: any codes do, the row's first)
-                    int k = col * TILE + 16 * h;
-                    k = k < a.K ? k : 0;
-                    xv[i] = *(const v4i*)(xr + k);
-                }
-            };
-            auto mul = [&](int i0, v4i(&wv)[U], v4i(&xv)[U]) __attribute__((always_inline)) {
+            for (int i = 0; i < U; ++i) {
+                const int p = min(i0 + i, here - 1);  // (past the last: it again, and no product)
+                const int col = __builtin_amdgcn_readlane(e.x, p), t = __builtin_amdgcn_readlane(e.y, p);
+                wv[i] = *(const v4i*)(tiles + (int64_t)t * 1024 + lane * 16);
+                // (a half past K is zero in the tile: any codes do, the row's first)
+                int k = col * TILE + 16 * h;
+                k = k < a.K ? k : 0;
+                xv[i] = *(const v4i*)(xr + k);
+            }
+        };
+        auto mul = [&](int i0, v4i(&wv)[U], v4i(&xv)[U]) __attribute__((always_inline)) {
 #pragma unroll
-                for (int i = 0; i < U; ++i)
-                    if (i0 + i < here)
-                        acc = mma8(wv[i], xv[i], acc);
-            };
-            load(0, w[0], x[0]);
-            for (int i0 = 0; i0 < here; i0 += 2 * U) {
-                if (i0 + U < here)
-                    load(i0 + U, w[1], x[1]);
-                mul(i0, w[0], x[0]);
-                if (i0 + U < here) {
-                    if (i0 + 2 * U < here)
-                        load(i0 + 2 * U, w[0], x[0]);
-                    mul(i0 + U, w[1], x[1]);
-                }
+            for (int i = 0; i < U; ++i)
+                if (i0 + i < here)
+                    acc = mma8(wv[i], xv[i], acc);
+        };
+        load(0, w[0], x[0]);
+        for (int i0 = 0; i0 < here; i0 += 2 * U) {
+            if (i0 + U < here)
+                load(i0 + U, w[1], x[1]);
+            mul(i0, w[0], x[0]);
+            if (i0 + U < here) {
+                if (i0 + 2 * U < here)
+                    load(i0 + 2 * U, w[0], x[0]);
+                mul(i0 + U, w[1], x[1]);
             }
         }
+    }
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            s_part[wave][q][lane] = v4i{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
-        __syncthreads();
-        if (tid < 256) {
-            const int q = tid >> 6;
-            int s[4] = {0, 0, 0, 0};
+    for (int q = 0; q < 4; ++q)
+        s_part[wave][q][lane] = v4i{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    __syncthreads();
+    if (tid < 256) {
+        const int q = tid >> 6;
+        int s[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int w = 0; w < WV; ++w) {
-                const v4i v = s_part[w][q][lane];
+        for (int w = 0; w < WV; ++w) {
+            const v4i v = s_part[w][q][lane];
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    s[b] += v[b];
-            }
-            const int64_t m = m0 + (lane & 31), at = (int64_t)row * TILE + 8 * q + 4 * h;
-            if (m < a.M && at < a.N) {
-                float o[4];
-                finish4<OUT, GELU>(s, xscale[m], *(const float4*)(wscale + at), bias4<OUT>(bias, at), o);
-                char* y = Y + (m * a.ldy + at) * ES;
-                if constexpr (OUT == LPV_F32)
-                    *(float4*)y = float4{o[0], o[1], o[2], o[3]};
-                else
-                    *(uint2*)y = uint2{pack2<OUT>(o[0], o[1]), pack2<OUT>(o[2], o[3])};
-            }
+            for (int b = 0; b < 4; ++b)
+                s[b] += v[b];
         }
-        __syncthreads();  // (the sums are read: the next unit's may be written)
+        const int64_t m = m0 + (lane & 31), at = (int64_t)row * TILE + 8 * q + 4 * h;
+        if (m < a.M && at < a.N) {
+            float o[4];
+            finish4<OUT, GELU>(s, xscale[m], *(const float4*)(wscale + at), bias4<OUT>(bias, at), o);
+            char* y = Y + (m * a.ldy + at) * ES;
+            if constexpr (OUT == LPV_F32)
+                *(float4*)y = float4{o[0], o[1], o[2], o[3]};
+            else
+                *(uint2*)y = uint2{pack2<OUT>(o[0], o[1]), pack2<OUT>(o[2], o[3])};
+        }
     }
 }
 
 template <int OUT, bool GELU, int WV, int U>
 hipError_t launch_few(const lpv_quant* h, const QuantLinearCall& c, hipStream_t s)
 {
-    QuantDims d = {c.ldx, c.M, h->K, h->N, c.ldy, h->n_tile_rows, 0};
-    d.n_units = (c.M + 31) / 32 * h->n_tile_rows;
-    const dim3 grid((unsigned)(d.n_units < (1 << 16) ? d.n_units : (1 << 16))), block(64 * WV);
+    const QuantDims d = {c.ldx, c.M, h->K, h->N, c.ldy, h->n_tile_rows};
+    const dim3 grid((unsigned)((c.M + 31) / 32 * h->n_tile_rows)), block(64 * WV);
     hipLaunchKernelGGL((k_quant_few<OUT, GELU, WV, U>), grid, block, 0, s, d, c.X, c.xscale, h->tiles, h->list,
                        h->row_tile0, h->scale, (const char*)c.bias, (char*)c.Y);
     return hipGetLastError();
@@ -363,8 +358,9 @@ hipError_t launch_few(const lpv_quant* h, const QuantLinearCall& c, hipStream_t 
 struct PanelDims {
     int64_t ldx, M, K, N, ldy;
     int32_t n_chunks, n_pairs;
-    int32_t n_mt, n_pb;  // token tiles, blocks of 8 pairs
+    int32_t n_mt, n_pb;  // token tiles, blocks of WV pairs
     int32_t n_items;
+    uint32_t per_inv, last_inv;  // 2^32 / d rounded up for the divisors of item(): PN_MG n_pb and n_mt % PN_MG
 };
 constexpr int PN_MG = 8;             // token tiles that share an XCD's L2 with several blocks of pairs
 constexpr int PN_STAGE = 4096;       // bytes of a wave's staging area
@@ -380,12 +376,143 @@ __device__ inline void dma4(const char* base, uint32_t off, uint32_t lds)
         : "memory");
 }
 
+// The lane number made opaque: what only a rare part needs is not kept in registers through the
+// loop.
+__device__ inline int fresh(int l)
+{
+    asm volatile("" : "+v"(l));
+    return l;
+}
+
+// What the outputs of a pair need, into the wave's staging area: the outputs' scales (256 bytes),
+// their bias (256) and the tokens' scales.
+template <int OUT, int TU>
+__device__ inline void params_dma(const PanelDims& a, uint32_t stage, int lane, int64_t m0, int64_t n0,
+                                  const char* xscale, const char* wscale, const char* bias)
+{
+    constexpr int ES = OUT == LPV_F32 ? 4 : 2;
+    const int ln = fresh(lane);
+    dma4(wscale + n0 * 4, (uint32_t)ln * 4, stage);
+    if (bias) {
+        const int n = (int)n0 + (OUT == LPV_F32 ? ln : 2 * (ln & 31));
+        dma4(bias, (uint32_t)((n < a.N ? n : 0) * ES), stage + 256);
+    } else {
+        *(lds_u32)(uintptr_t)(stage + 256 + ln * 4) = 0;
+    }
+    const int last = (int)min((int64_t)32 * TU - 1, a.M - 1 - m0);
+#pragma unroll
+    for (int i = 0; i < (TU + 1) / 2; ++i)
+        dma4(xscale + m0 * 4, (uint32_t)min(64 * i + ln, last) * 4, stage + 512 + i * 256);
+}
+
+// The outputs of 32 TU tokens (from m0) and a pair's 64 outputs (from n0); the sums are left at 0.
+template <int OUT, bool GELU, int TU>
+__device__ inline void panel_outputs(const PanelDims& a, i32x16 (&acc)[2][TU], uint32_t stage, int lane,
+                                     int64_t m0, int64_t n0, char* Y)
+{
+    constexpr int ES = OUT == LPV_F32 ? 4 : 2;
+    const int ln = fresh(lane), fr = ln & 31, h = ln >> 5;
+    float xs[TU];
+#pragma unroll
+    for (int u = 0; u < TU; ++u)
+        xs[u] = __uint_as_float(*(lds_u32)(uintptr_t)(stage + 512 + (32 * u + fr) * 4));
+    uint2 pk[TU][2][4];    // 16-bit outputs: four to a place
+    float4 pf[OUT == LPV_F32 ? TU : 1][2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = 32 * j + 8 * q + 4 * h;
+            const float4 ws = __builtin_bit_cast(float4, lds_read16<0>(stage + n * 4));
+            float4 b;
+            if constexpr (OUT == LPV_F32) {
+                b = __builtin_bit_cast(float4, lds_read16<256>(stage + n * 4));
+            } else {
+                using E = Elem<OUT>;
+                const uint64_t v = *(lds_u64)(uintptr_t)(stage + 256 + n * 2);
+                b = float4{E::to_f32((uint16_t)v), E::to_f32((uint16_t)(v >> 16)),
+                           E::to_f32((uint16_t)(v >> 32)), E::to_f32((uint16_t)(v >> 48))};
+            }
+#pragma unroll
+            for (int u = 0; u < TU; ++u) {
+                const int s[4] = {acc[j][u][4 * q], acc[j][u][4 * q + 1], acc[j][u][4 * q + 2], acc[j][u][4 * q + 3]};
+                float o[4];
+                finish4<OUT, GELU>(s, xs[u], ws, b, o);
+                if constexpr (OUT == LPV_F32)
+                    pf[u][j][q] = float4{o[0], o[1], o[2], o[3]};
+                else
+                    pk[u][j][q] = uint2{pack2<OUT>(o[0], o[1]), pack2<OUT>(o[2], o[3])};
+            }
+        }
+    // 32 tokens of 128 bytes at a time through the staging area (16-byte piece c of token t at
+    // c ^ xswz(t)), so that whole lines leave; streamed past the caches, which X and the
+    // tiles want
+    const int lt = ln >> 3, lp = ln & 7;
+    const bool inside = m0 + 32 * TU <= a.M && n0 + 64 <= a.N;
+    typedef __attribute__((address_space(1))) char* global_w;
+    // (32 bits: eight rows of a stride of at most 2^22)
+    const uint32_t y_off = ((uint32_t)lt * (uint32_t)a.ldy + (uint32_t)lp * (16 / ES)) * ES;
+#pragma unroll
+    for (int u = 0; u < TU; ++u) {
+#pragma unroll
+        for (int half = 0; half < ES / 2; ++half) {
+            const uint32_t at = stage + fr * 128;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (ES == 4 && j != half)
+                    continue;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if constexpr (OUT == LPV_F32)
+                        lds_write16(at + (((2 * q + h) ^ xswz(fr)) << 4), __builtin_bit_cast(v4i, pf[u][j][q]));
+                    else
+                        *(lds_u64)(uintptr_t)(at + (((4 * j + q) ^ xswz(fr)) << 4) + 8 * h) =
+                            __builtin_bit_cast(uint64_t, pk[u][j][q]);
+                }
+            }
+            v4i v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = 8 * i + lt;
+                v[i] = lds_read16<0>(stage + t * 128 + ((lp ^ xswz(t)) << 4));
+            }
+            global_w y = (global_w)Y + ((m0 + 32 * u) * a.ldy + n0 + 32 * half) * ES;
+            typedef __attribute__((address_space(1))) v4i* out4;
+            if (inside) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i, y += 8 * a.ldy * ES) {
+                    asm volatile("" : "+s"(y));  // (the wave's address: the lane's offset stays 32 bits)
+                    __builtin_nontemporal_store(v[i], (out4)(y + y_off));
+                }
+            } else {
+                const int rows = (int)min((int64_t)32, a.M - (m0 + 32 * u));
+                if (n0 + 32 * half + lp * (16 / ES) < a.N)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (8 * i + lt < rows)
+                            __builtin_nontemporal_store(v[i], (out4)(y + 8 * i * a.ldy * ES + y_off));
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int u = 0; u < TU; ++u)
+            acc[j][u] = i32x16{};
+}
+
+// The four columns of a group: place in the chunk, and which of the pair's tiles are kept.
+__device__ inline uint32_t col_of(uint32_t desc, int i) { return desc >> (16 * (i / 2) + 6 * (i & 1)) & 15; }
+__device__ inline uint32_t kept_of(uint32_t desc, int i) { return desc >> (16 * (i / 2) + 6 * (i & 1) + 4) & 3; }
+// A half's end of the chunk (i = 1 or 3), and the group's of the pair.
+__device__ inline bool chunk_end(uint32_t desc, int i) { return desc >> (i == 1 ? 12 : 28) & 1; }
+__device__ inline bool pair_end(uint32_t desc) { return desc >> 29 & 1; }
+
 template <int OUT, bool GELU, int TU, int WV, int NS>
 __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
     const PanelDims a, const char* X, const char* xscale, const char* tiles, const uint2* groups,
     const char* wscale, const char* bias, char* Y)
 {
-    constexpr int ES = OUT == LPV_F32 ? 4 : 2;
     constexpr int PANEL = TU * 4096, SLOT = 2 * PANEL;  // bytes
     constexpr int IPW = TU * 8 / WV;                    // DMA instructions of a wave and chunk
     __shared__ uint4 smem[(NS * SLOT + WV * PN_STAGE) / 16];
@@ -411,18 +538,18 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
     if (my_items == 0)
         return;
     auto item = [&](int k, int& mt, int& pb) {
+        // (below 2^30: the estimate of a quotient is right or one too many)
         const int i = seg + min(k, my_items - 1) * C, per = PN_MG * a.n_pb;
-        const int g = i / per, rest = i - g * per, mg = min(PN_MG, a.n_mt - g * PN_MG);
-        pb = rest / mg;
+        int g = (int)__umulhi((uint32_t)i, a.per_inv), rest = i - g * per;
+        if (rest < 0) {
+            --g;
+            rest += per;
+        }
+        const int mg = min(PN_MG, a.n_mt - g * PN_MG);
+        pb = mg == PN_MG ? rest / PN_MG : mg == 1 ? rest : (int)__umulhi((uint32_t)rest, a.last_inv);
         mt = g * PN_MG + rest - pb * mg;
     };
     const int per_pair = QUANT_GROUPS * a.n_chunks;  // groups of a pair, at most
-    // (the lane made opaque: what only such a part needs is not kept in registers through the
-    // loop; the same below)
-    auto fresh = [](int l) __attribute__((always_inline)) {
-        asm volatile("" : "+v"(l));
-        return l;
-    };
     auto lanes_of = [&](int pb, int from) {  // groups from .. from + 63 of this wave's pair
         const uint2* g = groups + (int64_t)(pb * WV + wave) * per_pair;
         return g[(uint32_t)min(from + fresh(lane), per_pair - 1)];
@@ -463,22 +590,8 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
                 set_x();
         }
     };
-    // ---- what the epilogue of an item needs, into the wave's staging area: the outputs' scales
-    // (256 bytes), their bias (256) and the tokens' scales
-    auto dma_params = [&](int mt, int pb) {
-        const int n0 = (pb * WV + wave) * 64, ln = fresh(lane);
-        const int64_t m0 = (int64_t)mt * (32 * TU);
-        dma4(wscale + (int64_t)n0 * 4, (uint32_t)ln * 4, stage);
-        if (bias) {
-            const int n = n0 + (OUT == LPV_F32 ? ln : 2 * (ln & 31));
-            dma4(bias, (uint32_t)((n < a.N ? n : 0) * ES), stage + 256);
-        } else {
-            *(lds_u32)(uintptr_t)(stage + 256 + ln * 4) = 0;
-        }
-        const int last = (int)min((int64_t)32 * TU - 1, a.M - 1 - m0);
-#pragma unroll
-        for (int i = 0; i < (TU + 1) / 2; ++i)
-            dma4(xscale + m0 * 4, (uint32_t)min(64 * i + ln, last) * 4, stage + 512 + i * 256);
+    auto params = [&](int mt, int pb) {
+        params_dma<OUT, TU>(a, stage, lane, (int64_t)mt * (32 * TU), (int64_t)(pb * WV + wave) * 64, xscale, wscale, bias);
     };
 
     set_x();
@@ -486,7 +599,7 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
     int mt, pb, mt1, pb1, mt2, pb2;  // this item, the next and the one after it
     item(0, mt, pb);
     item(1, mt1, pb1);
-    dma_params(mt, pb);
+    params(mt, pb);
     uint2 dl = lanes_of(pb, 0);       // this item's groups, 64 at a time
     uint2 nd = lanes_of(pb1, 0), n2;  // the next item's, and the one's after it
     asm volatile("" : "+v"(dl.x), "+v"(dl.y), "+v"(nd.x), "+v"(nd.y));
@@ -498,7 +611,7 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
     v4i w[4][2];
     typedef const __attribute__((address_space(1))) v4i* global4;
     auto load_w = [&](int i, uint32_t desc, uint32_t& at) __attribute__((always_inline)) {
-        const uint32_t ab = desc >> (16 * (i / 2) + 6 * (i & 1) + 4) & 3;
+        const uint32_t ab = kept_of(desc, i);
         w[i][0] = *(global4)(wt + (at + loff));
         at += ab == 3 ? 1024 : 0;
         w[i][1] = *(global4)(wt + (at + loff));
@@ -516,7 +629,7 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
     const uint32_t xbase = lds + fr * 128, xpiece = (uint32_t)(h ^ xswz(fr)) << 4;
     v4i x[2][TU];
     auto read_x = [&](v4i(&o)[TU], uint32_t desc, int i, uint32_t slot) __attribute__((always_inline)) {
-        const uint32_t c = desc >> (16 * (i / 2) + 6 * (i & 1)) & 15;
+        const uint32_t c = col_of(desc, i);
         const uint32_t at = xbase + (xpiece ^ (c & 3) << 5) + (slot + (c >> 2) * PANEL);
 #pragma unroll
         for (int u = 0; u < TU; ++u)
@@ -558,7 +671,7 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
         bool done;
         do {  // the pair's groups
             uint32_t next, first;
-            done = cur >> 29 & 1;
+            done = pair_end(cur);
             if (done) {
                 next = __builtin_amdgcn_readlane(nd.x, 0);
                 first = __builtin_amdgcn_readlane(nd.y, 0);
@@ -575,14 +688,14 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
             uint32_t at = first * 1024;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool end = (i & 1) && (cur >> (i == 1 ? 12 : 28) & 1);  // of the chunk
+                const bool end = (i & 1) && chunk_end(cur, i);
                 if (!end)
                     read_x(x[(i + 1) & 1], i < 3 ? cur : next, (i + 1) & 3, slot);
-                if (cur >> (16 * (i / 2) + 6 * (i & 1) + 4) & 1)
+                if (kept_of(cur, i) & 1)
 #pragma unroll
                     for (int u = 0; u < TU; ++u)
                         acc[0][u] = mma8(w[i][0], x[i & 1][u], acc[0][u]);
-                if (cur >> (16 * (i / 2) + 6 * (i & 1) + 5) & 1)
+                if (kept_of(cur, i) & 2)
 #pragma unroll
                     for (int u = 0; u < TU; ++u)
                         acc[1][u] = mma8(w[i][1], x[i & 1][u], acc[1][u]);
@@ -600,93 +713,9 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
             cur = next;
         } while (!done);
         asm volatile("" : "+v"(n2.x), "+v"(n2.y));
-        // ---- the item's outputs
-        const int64_t m0 = (int64_t)mt * (32 * TU), n0 = (int64_t)(pb * WV + wave) * 64;
-        const int ln = fresh(lane), fr = ln & 31, h = ln >> 5;
-        float xs[TU];
-#pragma unroll
-        for (int u = 0; u < TU; ++u)
-            xs[u] = __uint_as_float(*(lds_u32)(uintptr_t)(stage + 512 + (32 * u + fr) * 4));
-        uint2 pk[TU][2][4];    // 16-bit outputs: four to a place
-        float4 pf[OUT == LPV_F32 ? TU : 1][2][4];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = 32 * j + 8 * q + 4 * h;
-                const float4 ws = __builtin_bit_cast(float4, lds_read16<0>(stage + n * 4));
-                float4 b;
-                if constexpr (OUT == LPV_F32) {
-                    b = __builtin_bit_cast(float4, lds_read16<256>(stage + n * 4));
-                } else {
-                    using E = Elem<OUT>;
-                    const uint64_t v = *(lds_u64)(uintptr_t)(stage + 256 + n * 2);
-                    b = float4{E::to_f32((uint16_t)v), E::to_f32((uint16_t)(v >> 16)),
-                               E::to_f32((uint16_t)(v >> 32)), E::to_f32((uint16_t)(v >> 48))};
-                }
-#pragma unroll
-                for (int u = 0; u < TU; ++u) {
-                    const int s[4] = {acc[j][u][4 * q], acc[j][u][4 * q + 1], acc[j][u][4 * q + 2], acc[j][u][4 * q + 3]};
-                    float o[4];
-                    finish4<OUT, GELU>(s, xs[u], ws, b, o);
-                    if constexpr (OUT == LPV_F32)
-                        pf[u][j][q] = float4{o[0], o[1], o[2], o[3]};
-                    else
-                        pk[u][j][q] = uint2{pack2<OUT>(o[0], o[1]), pack2<OUT>(o[2], o[3])};
-                }
-            }
-        // 32 tokens of 128 bytes at a time through the staging area (16-byte piece c of token t at
-        // c ^ xswz(t)), so that whole lines leave; streamed past the caches, which X and the
-        // tiles want
-        const int lt = ln >> 3, lp = ln & 7;
-        const bool inside = m0 + 32 * TU <= a.M && n0 + 64 <= a.N;
-        typedef __attribute__((address_space(1))) char* global_w;
-        // (32 bits: eight rows of a stride of at most 2^22)
-        const uint32_t y_off = ((uint32_t)lt * (uint32_t)a.ldy + (uint32_t)lp * (16 / ES)) * ES;
-#pragma unroll
-        for (int u = 0; u < TU; ++u) {
-#pragma unroll
-            for (int half = 0; half < ES / 2; ++half) {
-                const uint32_t at = stage + fr * 128;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if (ES == 4 && j != half)
-                        continue;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if constexpr (OUT == LPV_F32)
-                            lds_write16(at + (((2 * q + h) ^ xswz(fr)) << 4), __builtin_bit_cast(v4i, pf[u][j][q]));
-                        else
-                            *(lds_u64)(uintptr_t)(at + (((4 * j + q) ^ xswz(fr)) << 4) + 8 * h) =
-                                __builtin_bit_cast(uint64_t, pk[u][j][q]);
-                    }
-                }
-                v4i v[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = 8 * i + lt;
-                    v[i] = lds_read16<0>(stage + t * 128 + ((lp ^ xswz(t)) << 4));
-                }
-                global_w y = (global_w)Y + ((m0 + 32 * u) * a.ldy + n0 + 32 * half) * ES;
-                typedef __attribute__((address_space(1))) v4i* out4;
-                if (inside) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i, y += 8 * a.ldy * ES) {
-                        asm volatile("" : "+s"(y));  // (the wave's address: the lane's offset stays 32 bits)
-                        __builtin_nontemporal_store(v[i], (out4)(y + y_off));
-                    }
-                } else {
-                    const int rows = (int)min((int64_t)32, a.M - (m0 + 32 * u));
-                    if (n0 + 32 * half + lp * (16 / ES) < a.N)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (8 * i + lt < rows)
-                                __builtin_nontemporal_store(v[i], (out4)(y + 8 * i * a.ldy * ES + y_off));
-                }
-            }
-        }
+        panel_outputs<OUT, GELU, TU>(a, acc, stage, lane, (int64_t)mt * (32 * TU), (int64_t)(pb * WV + wave) * 64, Y);
         if (k + 1 < my_items)
-            dma_params(mt1, pb1);
+            params(mt1, pb1);
         mt = mt1;
         pb = pb1;
         mt1 = mt2;
@@ -694,11 +723,6 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
         dl = nd;
         nd = n2;
         gi = from = 0;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int u = 0; u < TU; ++u)
-                acc[j][u] = i32x16{};
     }
     // (nothing of this workgroup is in flight when it ends)
     __builtin_amdgcn_s_waitcnt(0);
@@ -715,6 +739,9 @@ hipError_t launch_panel(const lpv_quant* h, const QuantLinearCall& c, int n_cus,
     for (int64_t m = 0, n_mt = (c.M + 32 * TU - 1) / (32 * TU); n_mt > 0; m += most, n_mt -= most) {
         d.n_mt = (int32_t)(n_mt < most ? n_mt : most);
         d.n_items = d.n_mt * d.n_pb;
+        auto inverse = [](int32_t n) { return (uint32_t)((((uint64_t)1 << 32) + n - 1) / n); };
+        d.per_inv = inverse(PN_MG * d.n_pb);
+        d.last_inv = d.n_mt % PN_MG > 1 ? inverse(d.n_mt % PN_MG) : 0;
         const int64_t m0 = m * (32 * TU);
         d.M = c.M - m0;
         const int need = (int)(((int64_t)d.n_items + 7) / 8 * 8);
@@ -730,6 +757,19 @@ hipError_t launch_panel(const lpv_quant* h, const QuantLinearCall& c, int n_cus,
     return hipSuccess;
 }
 
+// The kernel by the work there is, GPU us on 256 compute units.
+// - k_quant_few up to 1400 units of 32 tokens and a tile row (1380 units of 640 x 832 6.8, items of 32
+//   tokens 7.0; 1600 of 656 x 688 9.5 / 7.5; 6400 of 5504 x 128 14.6 / 9.0), with 4 waves to a unit, or
+//   8 where a tile row keeps more than 48 tiles (12: 4.7 / 5.5, 57: 4.7 / 4.6, 128: 7.0 / 6.1).
+// - Items of 128 tokens x 8 pairs with four chunks on their way for a long reduction, if every
+//   compute unit gets one (16384 x 4096 x 8192: 467, four pairs 480, 64 tokens 560), from 4096
+//   columns on if half of them do (5832 x 7376 x 1424: 79 / 90 / 95).
+// - Two workgroups of 128 tokens x 4 pairs to a compute unit, one's outputs beside the other's
+//   products, if there are three items for each compute unit (50432 x 768 -> 2304 at 50%: 80, 8 pairs
+//   84, 64 tokens 96; 594 items 20.8, 64 tokens 19.8).  Float32 outputs, which take twice the
+//   registers there, go 64 tokens at a time (5506 x 640 -> 6848: 41 / 37).
+// - 64 tokens if every compute unit gets an item (9933 x 528 x 528: 9.9, 32 tokens 11.7), else 32
+//   (2353 x 2112 -> 896: 10.1 / 10.5).
 template <int OUT, bool GELU> hipError_t launch_as(const lpv_quant* h, const QuantLinearCall& c, hipStream_t s)
 {
     const int cus = h->n_cus;
@@ -740,10 +780,12 @@ template <int OUT, bool GELU> hipError_t launch_as(const lpv_quant* h, const Qua
             return launch_few<OUT, GELU, 4, 4>(h, c, s);
         return launch_few<OUT, GELU, 8, 4>(h, c, s);
     }
-    if (h->K >= 2048 && items(128, 8) >= cus)
+    if (h->K >= 2048 && items(128, 8) >= (h->K >= 4096 ? cus / 2 : cus))
         return launch_panel<OUT, GELU, 4, 8, 4>(h, c, cus, 1, s);
-    if (items(128, 4) >= 3 * cus)
-        return launch_panel<OUT, GELU, 4, 4, 2>(h, c, cus, 2, s);
+    if constexpr (OUT != LPV_F32) {
+        if (items(128, 4) >= 3 * cus)
+            return launch_panel<OUT, GELU, 4, 4, 2>(h, c, cus, 2, s);
+    }
     if (items(64, 4) >= cus)
         return launch_panel<OUT, GELU, 2, 4, 4>(h, c, cus, 2, s);
     return launch_panel<OUT, GELU, 1, 4, 4>(h, c, cus, 3, s);

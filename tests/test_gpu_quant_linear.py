@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import quant
-from gpu_util import TORCH, f64, say
+from gpu_util import TORCH, f64, kernels, say
 
 pytestmark = pytest.mark.gpu
 
@@ -94,6 +94,33 @@ def test_blocks(M, N, K, b_r, b_c, drop):
         assert h.info["nnzb"] == int(c.mask.sum()) and (h.info["R"], h.info["C"]) == tuple(c.mask.shape)
         Y = lpv().quant_linear(h, c.X, c.xs, c.bias, epi="gelu" if gelu else None)
         check(Y, c.want(gelu), dtype, gelu, "%d x %d x %d, %d x %d blocks %s" % (M, N, K, b_r, b_c, dtype))
+
+
+@pytest.mark.parametrize("M,N,K,b,kernel", [
+    (33, 96, 512, 0, "few<%d, %s, 4, 4>"), (1, 256, 4096, 0, "few<%d, %s, 8, 4>"),
+    (1000, 1600, 80, 16, "panel<%d, %s, 1, 4, 4>"), (1500, 8208, 336, 16, "panel<%d, %s, 2, 4, 4>"),
+    (5000, 8208, 592, 16, "panel<%d, %s, 4, 4, 2>"), (2050, 8208, 2064, 16, "panel<%d, %s, 4, 8, 4>")])
+def test_every_kernel(M, N, K, b, kernel):
+    # the size that reaches it, in every type, with and without GELU: the ends against the oracle, the
+    # rows between against the same rows in a call of their own
+    for dtype, code in (("bf16", 2), ("f16", 1), ("f32", 0)):
+        if dtype == "f32" and "4, 4, 2" in kernel:
+            continue
+        for gelu in (False, True):
+            c = Case(M, N, K, dtype, b, b, 45)
+            h = c.pack()
+            epi = "gelu" if gelu else None
+            Y = lpv().quant_linear(h, c.X, c.xs, c.bias, epi=epi)
+            assert kernels(lambda: lpv().quant_linear(h, c.X, c.xs, c.bias, epi=epi), args=True) == {
+                "k_quant_" + kernel % (code, str(gelu).lower())}
+            for at in ([slice(0, 70), slice(max(0, M - 70), M)] if M > 140 else [slice(0, M)]):
+                part = Case(M, N, K, dtype, b, b, 45)
+                part.X, part.xs = c.X[at], c.xs[at]
+                check(Y[at], part.want(gelu), dtype, gelu, "%s rows %s" % (kernel % (code, gelu), at))
+            if M > 64:
+                for i in range(0, M - 32, max(32, (M // 8) & ~15)):
+                    few = lpv().quant_linear(h, c.X[i:i + 32], c.xs[i:i + 32], c.bias, epi=epi)
+                    assert torch.equal(Y[i:i + 32], few), i
 
 
 @pytest.mark.parametrize("M", [1, 40, 300, 5000])
@@ -256,3 +283,14 @@ def test_refusals_of_the_binding():
     with pytest.raises(m.LpvError, match="LPV_ERR_INVALID_ARG"):
         m.quant_linear(h, c.X, c.xs)
     h.close()
+
+
+def test_a_stream_that_is_not_current_takes_its_output():
+    m = lpv()
+    c = Case(5, 64, 96)
+    h = c.pack()
+    side = torch.cuda.Stream()
+    with pytest.raises(ValueError, match="takes its outputs"):
+        m.quant_linear(h, c.X, c.xs, c.bias, stream=side)
+    assert torch.equal(m.quant_linear(h, c.X, c.xs, c.bias, stream=torch.cuda.current_stream()),
+                       m.quant_linear(h, c.X, c.xs, c.bias))

@@ -230,3 +230,21 @@ def test_another_stream_and_a_captured_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(q, want_q) and torch.equal(scale, want_s) and torch.equal(S, sum_of(x, y)), k
+
+
+@pytest.mark.parametrize("kind", ["plain", "rms", "layer"])
+def test_a_stream_that_is_not_current_takes_its_outputs(kind):
+    """New outputs come from the current stream's memory: a call on another one is refused without
+    its outputs, one of them missing or both."""
+    x, y, g, b = make(4, 64, "bf16", 3)
+    side = torch.cuda.Stream()
+    q, scale = torch.empty((4, 64), dtype=torch.int8, device="cuda"), torch.empty(4, device="cuda")
+    for kw in ({}, {"q": q}, {"scale": scale}):
+        with pytest.raises(ValueError, match="takes its outputs"):
+            call(kind, x, y, g, b, stream=side, **kw)
+    got = call(kind, x, y, g, b, stream=torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.default_stream())
+        again = call(kind, x, y, g, b, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
