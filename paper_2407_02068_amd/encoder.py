@@ -16,6 +16,10 @@ this chains the standard pre-norm block around them:
 
 With a position bias (one table of buckets per block) the attention is the
 position-biased one, in windows or over regions of tokens if labels are given.
+In 8 bits (``quantize``, then ``run(..., quant=True)``) every linear layer takes 8-bit
+codes with a scale for each token, from its own weight in 8-bit codes: the layer norms
+give them in place of A, and O and Hd are quantised row by row.
+
 Every layer norm uses the same gamma / beta.  The residual stream alternates
 between two buffers, so a run never overwrites its own input and every run
 computes the same function of ``x0``.
@@ -33,6 +37,13 @@ class Linear:
         self.name, self.W, self.mask, self.bias = name, W, mask, bias
         self.b_r, self.b_c, self.gelu = b_r, b_c, gelu
         self.h = lpv.bsr_pack(W, mask, b_r, b_c)
+        self.q = None
+
+    def quantize(self):
+        """Packs the kept blocks in 8-bit codes with a scale for each output."""
+        keep = self.mask.repeat_interleave(self.b_r, 0).repeat_interleave(self.b_c, 1) != 0
+        codes, scale = lpv.quant_rows(torch.where(keep, self.W, 0))
+        self.q = lpv.quant_pack(codes, scale, self.mask, self.b_r, self.b_c)
 
     def __call__(self, x, y, sparse):
         epi = "gelu" if self.gelu else None
@@ -40,8 +51,13 @@ class Linear:
             return lpv.bsr_linear(self.h, x, self.bias, y, epi=epi)
         return lpv.dense_linear(self.W, x, self.bias, y, epi=epi)
 
+    def quant(self, codes, scale, y):
+        return lpv.quant_linear(self.q, codes, scale, self.bias, y, epi="gelu" if self.gelu else None)
+
     def close(self):
         self.h.close()
+        if self.q is not None:
+            self.q.close()
 
 
 class EncoderChain:
@@ -76,6 +92,7 @@ class EncoderChain:
         self.A, self.O, self.P = new(D), new(D), new(D)
         self.qkv, self.Hd = new(linears[0].W.shape[0]), new(linears[2].W.shape[0])
         self.R = [new(D), new(D)]
+        self.codes = None
         self.relpos, self.tables, self.region = relpos, tables, region
         self.relpos_ws = None
         if relpos is not None:
@@ -86,14 +103,83 @@ class EncoderChain:
     def blocks(self):
         return len(self.linears) // 4
 
-    def run(self, x0, sparse=True, trace=None, linear_events=None):
+    def quantize(self):
+        """Gets the chain ready for ``run(..., quant=True)``: every linear layer's weight in 8-bit
+        codes, and the buffers of the activations' codes and scales."""
+        new = lambda cols: (torch.empty((self.M, cols), dtype=torch.int8, device=self.A.device),
+                            torch.empty(self.M, dtype=torch.float32, device=self.A.device))
+        for layer in self.linears:
+            layer.quantize()
+        self.codes = {"A": new(self.D), "O": new(self.D), "Hd": new(self.Hd.shape[1])}
+
+    def _attention(self, blk, qkv, out):
+        if self.relpos is None:
+            return lpv.attention(qkv, self.n_seq, self.T, self.H, out=out)
+        region = self.region[blk] if isinstance(self.region, (list, tuple)) else self.region
+        return lpv.relpos_attention(self.relpos, self.tables[blk], qkv, self.n_seq, self.H,
+                                    region=region, out=out, workspace=self.relpos_ws,
+                                    hd=self.D // self.H)
+
+    def _run_quant(self, x0, trace=None):
+        """``run`` with 8-bit codes into every linear layer.  trace: as there; the codes and scales of
+        a layer's input are its "q" and "scale"."""
+        if self.codes is None:
+            raise ValueError("quantize() first")
+        g, b, eps = self.gamma, self.beta, self.eps
+        O, P, qkv, Hd, R = self.O, self.P, self.qkv, self.Hd, self.R
+        A8, O8, Hd8 = self.codes["A"], self.codes["O"], self.codes["Hd"]
+
+        def lin(layer, x8, y):
+            layer.quant(*x8, y)
+            if trace:
+                trace(layer.name, {"q": x8[0], "scale": x8[1]}, y)
+
+        def norm(name, x, y, S):
+            lpv.add_layernorm_quant(x, y, g, b, eps, S=S, q=A8[0], scale=A8[1])
+            if trace:
+                trace(name, {"x": x, "y": y, "s": S}, A8)
+
+        def rows(name, x, x8):
+            lpv.quant_rows(x, q=x8[0], scale=x8[1])
+            if trace:
+                trace(name, {"x": x}, x8)
+
+        x, nxt = x0, 0
+        norm("ln.in", x, None, None)
+        for blk in range(self.blocks):
+            q, pr, f1, f2 = self.linears[4 * blk:4 * blk + 4]
+            lin(q, A8, qkv)
+            self._attention(blk, qkv, O)
+            if trace:
+                trace("%d.attention" % blk, {"qkv": qkv}, O)
+            rows("%d.o" % blk, O, O8)
+            lin(pr, O8, P)
+            norm("%d.add_ln1" % blk, x, P, R[nxt])
+            x, nxt = R[nxt], 1 - nxt
+            lin(f1, A8, Hd)
+            rows("%d.hd" % blk, Hd, Hd8)
+            lin(f2, Hd8, P)
+            if blk + 1 < self.blocks:
+                norm("%d.add_ln2" % blk, x, P, R[nxt])
+            else:  # (the result: no layer takes it)
+                lpv.add_layernorm(x, P, g, b, eps, S=R[nxt], out=self.A)
+            x, nxt = R[nxt], 1 - nxt
+        return x, self.A
+
+    def run(self, x0, sparse=True, trace=None, linear_events=None, quant=False):
         """One forward pass from the token activations x0 (M x D).  Returns
         (x, A): the residual stream after the last block and its layer norm.
+        quant: every linear layer in 8 bits, over its kept blocks (after ``quantize``; it takes
+        neither sparse=False nor linear_events).
 
         trace(name, inputs, output), if given, is called after every step with
         the step's input tensors (a dict) and its output, for checking a link
         at a time.  linear_events, if a list, receives a (start, end) pair of
         timing events recorded around every linear launch."""
+        if quant:
+            if not sparse or linear_events is not None:
+                raise ValueError("in 8 bits the chain is sparse, and records no events")
+            return self._run_quant(x0, trace)
         g, b, eps = self.gamma, self.beta, self.eps
         A, O, P, qkv, Hd, R = self.A, self.O, self.P, self.qkv, self.Hd, self.R
 
@@ -116,13 +202,7 @@ class EncoderChain:
         for blk in range(self.blocks):
             q, pr, f1, f2 = self.linears[4 * blk:4 * blk + 4]
             lin(q, A, qkv)
-            if self.relpos is None:
-                lpv.attention(qkv, self.n_seq, self.T, self.H, out=O)
-            else:
-                region = self.region[blk] if isinstance(self.region, (list, tuple)) else self.region
-                lpv.relpos_attention(self.relpos, self.tables[blk], qkv, self.n_seq, self.H,
-                                     region=region, out=O, workspace=self.relpos_ws,
-                                     hd=self.D // self.H)
+            self._attention(blk, qkv, O)
             if trace:
                 trace("%d.attention" % blk, {"qkv": qkv}, O)
             lin(pr, O, P)
@@ -138,18 +218,18 @@ class EncoderChain:
             x, nxt = R[nxt], 1 - nxt
         return x, A
 
-    def capture(self, x0, sparse=True):
+    def capture(self, x0, sparse=True, quant=False):
         """The forward pass from x0 captured once into a HIP graph (through
-        torch.cuda.CUDAGraph): replaying it relaunches the same 1 + 6 * blocks
-        calls' kernels on the same buffers with no host work per launch.  Every call
+        torch.cuda.CUDAGraph): replaying it relaunches the same 1 + 6 * blocks (in 8
+        bits 1 + 8 * blocks) calls' kernels on the same buffers with no host work per launch.  Every call
         of the chain is capturable (no allocation, no host synchronisation, no
         memset); one eager pass first settles the kernels' one-time set-up.
         Returns (graph, (x, A)): the outputs the replays rewrite."""
-        self.run(x0, sparse)
+        self.run(x0, sparse, quant=quant)
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
-            out = self.run(x0, sparse)
+            out = self.run(x0, sparse, quant=quant)
         torch.cuda.synchronize()
         return graph, out
 
