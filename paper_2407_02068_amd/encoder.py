@@ -105,7 +105,10 @@ class EncoderChain:
 
     def quantize(self):
         """Gets the chain ready for ``run(..., quant=True)``: every linear layer's weight in 8-bit
-        codes, and the buffers of the activations' codes and scales."""
+        codes, and the buffers of the activations' codes and scales.  Once only: captured
+        graphs hold their addresses."""
+        if self.codes is not None:
+            raise ValueError("the chain is in 8 bits already")
         new = lambda cols: (torch.empty((self.M, cols), dtype=torch.int8, device=self.A.device),
                             torch.empty(self.M, dtype=torch.float32, device=self.A.device))
         for layer in self.linears:

@@ -38,6 +38,8 @@ def test_encoder_chain_in_8_bits(n_seq, T, biased):
         chain.run(x0, quant=True)
     chain.quantize()
     with pytest.raises(ValueError):
+        chain.quantize()
+    with pytest.raises(ValueError):
         chain.run(x0, sparse=False, quant=True)
     with pytest.raises(ValueError):
         chain.run(x0, quant=True, linear_events=[])

@@ -226,6 +226,22 @@ def test_many_rows_past_32_bit_offsets():
     assert torch.equal(Y[M - M % 64:], part[:M % 64])
 
 
+def test_the_largest_weight():
+    # 2^22 tiles, 4 GiB: tokens of one column each find theirs at either end
+    n = 65536
+    g = torch.Generator(device="cuda").manual_seed(3)
+    W = torch.randint(-128, 128, (n, n), generator=g, device="cuda", dtype=torch.int8)
+    ws, xs = torch.rand(n, generator=g, device="cuda"), torch.ones(300, device="cuda")
+    h = lpv().quant_pack(W, ws)
+    ks = torch.arange(300, device="cuda") * 219  # 0 ... 65481
+    ks[-1] = n - 1
+    X = torch.zeros((300, n), dtype=torch.int8, device="cuda")
+    X[torch.arange(300, device="cuda"), ks] = 1
+    for M in (3, 300):
+        Y = lpv().quant_linear(h, X[-M:], xs[:M], dtype=torch.float32)
+        assert torch.equal(Y, W[:, ks[-M:]].t().float() * ws), M
+
+
 def test_streams_graph_and_two_weights():
     m = lpv()
     a, b = Case(333, 528, 768, "bf16", 16, 32), Case(333, 768, 528, "f16")
