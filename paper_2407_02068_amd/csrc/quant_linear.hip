@@ -363,14 +363,14 @@ hipError_t launch_few(const lpv_quant* h, const QuantLinearCall& c, hipStream_t 
 // waves' waiting (a chunk has 0.8 kept blocks a pair, on average, and the wave with the most is waited
 // for), 44 without the DMA, 35 without both.  Behind GELU its 16 instructions for every
 // 64 outputs: 12608 x 384 -> 1536 at 75% 19 us (8.4), of its cycles 30% that, and 14% before the first
-// product; a workgroup has two or three items, 2.3 on average.  With one wave a SIMD (777 x 1296
-// -> 5136 float32 with GELU, 16 us) a group of four columns takes 1580 cycles, 512 of them products; without
-// loads, waits, LDS reads and products together its control still takes 1100, and DMA, waits or
-// products alone can be left out at no more than 4% gain.  Chunks of 512 columns, tiles eight columns ahead, X two columns ahead and
-// over a chunk's end, places for all of a column's tiles (fewer instructions for their addresses),
-// three workgroups a compute unit and wave priorities were measured and are within 3%, one way here
-// and the other there; X of all K resident in LDS takes 5 us from the first of these and adds to
-// the others.
+// product; a workgroup has two or three items, 2.3 on average.  With one wave a SIMD (777 x 1296 ->
+// 5136 float32 with GELU, 16 us) a group of four columns takes 1580 cycles, 512 of them products;
+// without loads, waits, LDS reads and products together its control still takes 1100, and DMA,
+// waits or products alone can be left out at no more than 4% gain.  Chunks of 512 columns, tiles
+// eight columns ahead, X two columns ahead and over a chunk's end, places for all of a column's
+// tiles (fewer instructions for their addresses), three workgroups a compute unit and wave
+// priorities were measured and are within 5%, one way here and the other there; X of all K resident
+// in LDS takes 5 us from the first of these and adds to the others.
 //
 // The waits count: vector memory comes back in order, so that a DMA is there once no more are
 // out than are known to be younger (the compiler's own waits know nothing of the DMA and wait for

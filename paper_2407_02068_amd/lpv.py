@@ -849,6 +849,8 @@ def quant_linear(h, X, xscale, bias=None, Y=None, dtype=None, epi=None, stream=N
     """lpv_quant_linear: Y = g(xscale scale (X Wq^T) + b) from 8-bit codes X (int8 M x K) with a
     scale for each token (M float32).  Y has the type of the bias or ``dtype`` (bfloat16
     without either); allocated if not given."""
+    if not isinstance(h, QuantWeight):
+        raise ValueError("h must be a QuantWeight")
     if not isinstance(X, torch.Tensor) or X.dim() != 2:
         raise ValueError("X must be a 2-D int8 tensor")
     M, N = X.shape[0], h.N

@@ -289,6 +289,10 @@ def test_refusals_of_the_binding():
                 lambda: m.quant_pack(c.W, c.ws, c.mask[:1], 32, 32), lambda: m.quant_pack(c.W, c.ws, c.mask.bool(), 32, 32)):
         with pytest.raises((ValueError, TypeError, KeyError)):
             bad()
+    other = m.bsr_pack(torch.zeros((64, 96), dtype=torch.bfloat16, device="cuda"), c.mask, 32, 32)
+    for bad in (other, None, h.handle):  # (a handle of another kind is no weight in 8-bit codes)
+        with pytest.raises(ValueError):
+            m.quant_linear(bad, c.X, c.xs)
     with pytest.raises(m.LpvError, match="LPV_ERR_BLOCK"):
         m.quant_pack(c.W, c.ws, torch.ones((8, 12), dtype=torch.uint8, device="cuda"), 8, 8)
     with pytest.raises(m.LpvError, match="LPV_ERR_SHAPE"):
