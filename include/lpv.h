@@ -558,8 +558,9 @@ lpv_status lpv_distill_workspace_size(int64_t M, int64_t V, int32_t k, lpv_dtype
  * lpv_quant_rows -- rows in 8-bit codes: per row of M rows of D elements, u = x + y (y may be
  * NULL: u = x), and
  *   m = max_j |u_j|,  scale = m / 127,  q_j = rint(127 u_j / m)   (ties to even),
- * codes of -127 .. 127 of which u_j is q_j scale to half a step.  In float64 inside: the
- * codes are those of the exact quotient, the scale is rounded once to float32.  A row of zeros
+ * codes of -127 .. 127 of which u_j is q_j scale to half a step.  u is a float64 (x + y is
+ * exact in it up to magnitudes 2^28 apart); the codes are those of its exact quotient, however
+ * near to halfway between two of them, and the scale is rounded once to float32.  A row of zeros
  * has scale 0 and codes 0; a row with a NaN or an infinity has scale NaN and codes 0.
  * x, y   device, M x D, row strides ldx, ldy.
  * S      device, M x D, row stride lds, or NULL: receives u, rounded to dt.  May be x or y
@@ -581,7 +582,7 @@ lpv_status lpv_quant_rows(const void* x, int64_t ldx, const void* y, int64_t ldy
  * codes: s = x + y,
  *   u = s / sqrt(mean(s^2) + eps) * gamma,
  * then codes and scale of u as lpv_quant_rows gives them (the norm's factor divides out of the
- * codes, which are those of s * gamma).  S receives s.  gamma: device, D elements of
+ * codes, which are those of s * gamma, a float64).  S receives s.  gamma: device, D elements of
  * type dt; eps finite and >= 0.  The rest, and the errors, as lpv_quant_rows.
  */
 lpv_status lpv_add_rmsnorm_quant(const void* x, int64_t ldx, const void* y, int64_t ldy, int64_t M,
@@ -591,8 +592,10 @@ lpv_status lpv_add_rmsnorm_quant(const void* x, int64_t ldx, const void* y, int6
 /*
  * lpv_add_layernorm_quant -- lpv_add_layernorm in 8-bit codes: s = x + y,
  *   u = (s - mean(s)) / sqrt(var(s) + eps) * gamma + beta,
- * var the biased variance, then codes and scale of u as lpv_quant_rows gives them.  S
- * receives s.  The rest, and the errors, as lpv_add_rmsnorm_quant.
+ * var the biased variance, then codes and scale of u as lpv_quant_rows gives them, with a u
+ * that the norm's own float64 arithmetic gives: a quotient within 2^-41 of halfway counts as
+ * halfway, and has the even code.  S receives s.  The rest, and the errors, as
+ * lpv_add_rmsnorm_quant.
  */
 lpv_status lpv_add_layernorm_quant(const void* x, int64_t ldx, const void* y, int64_t ldy, int64_t M,
                                    int64_t D, lpv_dtype dt, const void* gamma, const void* beta,

@@ -3,17 +3,19 @@ addition and a norm, and the linear layer over 8-bit codes, as their definitions
 
 Arrays are float64 values (decode the element type first) and integer codes.
 """
+from fractions import Fraction
+
 import numpy as np
 from scipy.special import erfc
 
 
-def codes(u):
+def codes(u, exact=False):
     """(q, scale) of the rows of u: q = rint(127 u / max|u|), ties to even, scale = max|u| / 127.
     A row of zeros has scale 0, one with a value that is not finite scale NaN, both codes 0.
-    Values that a norm's float64 arithmetic gave are off by some 2^-52, and a quotient that
-    is halfway between two codes by some 2^-45 then: quotients go to the nearest multiple of
-    2^-40 first, which leaves every one that is exact (of values of up to 46 bits) where it is to
-    the same bits."""
+    exact: u is what it is, as elements, their sums and products are: next to halfway between two
+    codes rational arithmetic decides.  Else u is off by some 2^-52, as what a norm's float64
+    arithmetic gave, and a quotient that is halfway by some 2^-45: quotients go to the nearest
+    multiple of 2^-40 first, which puts them back there."""
     u = np.asarray(u, np.float64)
     m = np.abs(u).max(1)
     ok = np.isfinite(u).all(1)
@@ -21,13 +23,17 @@ def codes(u):
     q = np.zeros(u.shape, np.int64)
     t = 127 * u[live] / m[live, None]
     q[live] = np.rint(np.rint(t * 2.0 ** 40) * 2.0 ** -40).astype(np.int64)
+    if exact:
+        rows = np.flatnonzero(live)
+        for i, j in np.argwhere(np.abs(t - np.floor(t) - 0.5) <= 2.0 ** -39):
+            q[rows[i], j] = round(127 * Fraction(u[rows[i], j]) / Fraction(m[rows[i]]))
     return q, np.where(ok, m / 127, np.nan)
 
 
 def rms(s, gamma, eps):
     """(q, scale) of s / sqrt(mean(s^2) + eps) * gamma: the codes are those of s * gamma."""
     s = np.asarray(s, np.float64)
-    q, scale = codes(s * gamma)
+    q, scale = codes(s * gamma, exact=True)
     with np.errstate(divide="ignore", invalid="ignore"):
         r = 1 / np.sqrt((s * s).mean(1) + eps)
         return q, np.where(scale == 0, 0.0, scale * r)

@@ -10,8 +10,12 @@
 // of two codes would else take one or the other by the order of a sum.  It costs nothing that
 // shows: this card's float64 add, multiply and fma run at the rate of the (unpacked) float32
 // ones, and the kernel waits for memory.  127 u / max|u| comes by a reciprocal, an error
-// under 2^-45; adding and subtracting 1.5 * 2^12 rounds it to a multiple of 2^-40 first, so
-// that a quotient exactly between two codes stays there and goes to the even one.
+// under 2^-44; in the sum with 6144.5 it is rounded to a multiple of 2^-40.  Where
+// that is halfway between two codes, 127 u and that multiple of max|u| are compared as they
+// are (settle): a float64 quotient that is past a border by 2^-50 takes its own code, and one that
+// is on it the even one.  Elements themselves are never that near a border without being
+// on it (24 bits each: 2^-33 at least); sums x + y and products with gamma are.  A layer
+// norm's values have roundings of their own, and its quotients next to halfway go to the even code.
 #include <math.h>
 
 #include "lpv_device.h"
@@ -214,6 +218,16 @@ __device__ inline double fast_rcp(double x)
     return r;
 }
 
+// The code of u whose quotient 127 u / top is nearest to t, halfway between two codes: the sign of
+// 127 u - t top decides.  The product's rounding error is exact in float64 (p and e), and so is
+// 127 u - p, of two numbers that agree in 40 bits; the last difference has the right sign.
+__device__ inline int settle(double u, double top, double t)
+{
+    const double p = t * top, e = fma(t, top, -p);
+    const double d = fma(127.0, u, -p) - e;
+    return (int)(d > 0.0 ? ceil(t) : d < 0.0 ? floor(t) : rint(t));
+}
+
 // NT threads to a row (64: four rows to a workgroup), NC chunks of CH elements to a thread, held
 // in registers: the row is read once, the next one's loads going out before this one is worked on.
 // Bound by memory: 8192 x 4096 bf16 with its sum and a root-mean-square norm 37 us, 6.4 TB/s (two
@@ -358,20 +372,61 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void k_quant_rows(
             scale[row] = bad ? __builtin_nanf("") : top == 0.0 ? 0.0f : (float)sc;
         const double inv = bad || top == 0.0 ? 0.0 : 127.0 * fast_rcp(top);
         int8_t* qr = q + row * d.ldq;
-        auto code = [&](double u) -> uint32_t {
-            constexpr double FINE = 6144.0;               // 1.5 * 2^12
+        // 24 * 2^8 + 1/2 + t, for the quotient t: its whole part's low byte is the code of t rounded half
+        // up, and of its 40 bits of fraction none is set where t is halfway.
+        constexpr double BIAS = 6144.5;
+        auto quotient = [&](double u, double by, uint32_t& hi) {
+            const uint64_t b = __builtin_bit_cast(uint64_t, fma(u, by, BIAS));
+            hi = (uint32_t)(b >> 32);
+            return (uint32_t)b | (hi & 0xff);  // zero: halfway
+        };
+        // The same to the even code at once: for a layer norm, which has nothing to settle (with the other
+        // form 4% more time at 768 elements).
+        auto even = [&](double u) {
             constexpr double WHOLE = 6755399441055744.0;  // 1.5 * 2^52: the sum's low bits are the integer
-            const double t = (fma(u, inv, FINE) - FINE) + WHOLE;
-            return bad ? 0u : (uint32_t)__builtin_bit_cast(uint64_t, t) & 0xff;
+            return (uint32_t)__builtin_bit_cast(uint64_t, (fma(u, inv, 6144.0) - 6144.0) + WHOLE) & 0xff;
         };
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
+            uint32_t w[CH / 4] = {}, off = ~0u;
+#pragma unroll
+            for (int j = 0; j < CH; j += 4) {
+                if constexpr (KIND == QUANT_LAYER) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        w[j / 4] |= even(v[CH * i + j + k]) << (8 * k);
+                    continue;
+                }
+                uint32_t hi[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    off = min(off, quotient(v[CH * i + j + k], inv, hi[k]));
+                // byte 1 of each
+                w[j / 4] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(hi[3], hi[2], 0x0c0c0501),
+                                                 __builtin_amdgcn_perm(hi[1], hi[0], 0x0c0c0501), 0x05040100);
+            }
+            if (KIND != QUANT_LAYER && __builtin_expect(off == 0, 0)) {
+                double again = inv;  // (opaque, so that the quotients above need not be kept)
+                asm volatile("" : "+v"(again));
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    uint32_t hi;
+                    if (quotient(v[CH * i + j], again, hi) != 0)
+                        continue;
+                    if (KIND == QUANT_RMS || y) {
+                        const int c = settle(v[CH * i + j], top, fma(v[CH * i + j], again, BIAS) - BIAS);
+                        w[j / 4] = (w[j / 4] & ~(0xffu << (8 * (j & 3)))) | (uint32_t)(c & 0xff) << (8 * (j & 3));
+                    } else {
+                        w[j / 4] &= ~(1u << (8 * (j & 3)));  // (of the two codes the even one)
+                    }
+                }
+            }
+            if (bad)  // (the quotients of a NaN)
+#pragma unroll
+                for (int k = 0; k < CH / 4; ++k)
+                    w[k] = 0;
             if constexpr (VEC) {
                 if (at(i, 0) < d.D) {
-                    uint32_t w[CH / 4] = {};
-#pragma unroll
-                    for (int j = 0; j < CH; ++j)
-                        w[j / 4] |= code(v[CH * i + j]) << (8 * (j & 3));
                     if constexpr (CH == 4)
                         *(uint32_t*)(qr + at(i, 0)) = w[0];
                     else
@@ -381,7 +436,7 @@ __global__ __launch_bounds__(NT == 64 ? 256 : NT) void k_quant_rows(
 #pragma unroll
                 for (int j = 0; j < CH; ++j)
                     if (at(i, j) < d.D)
-                        qr[at(i, j)] = (int8_t)code(v[CH * i + j]);
+                        qr[at(i, j)] = (int8_t)(w[j / 4] >> (8 * (j & 3)));
             }
         }
     }
