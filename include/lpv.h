@@ -646,8 +646,9 @@ lpv_status lpv_quant_info_get(const lpv_quant* h, lpv_quant_info* out);
  *         bytes; must not overlap X, xscale or bias.
  * epi     LPV_EPI_NONE or LPV_EPI_GELU, as lpv_bsr_linear (float32 outputs: positive ones to 3e-7
  *         relative, negative ones to 1e-7).
- * The sums are 32-bit integers and exact; they, the scales and the bias meet in float32, and
- * the result is rounded once, so a row's bits depend on neither the other rows nor M.
+ * The sums are 32-bit integers and exact; they, the scales and the bias meet in float32, where
+ * a scale of any finite size does not overflow before the output does, and the result is
+ * rounded once, so a row's bits depend on neither the other rows nor M.
  * No allocation, no host synchronisation.  M = 0 is a no-op.
  * Errors: INVALID_ARG, SHAPE, DTYPE, ALIAS, HIP.
  */

@@ -214,6 +214,13 @@ __device__ inline float gelu_f32(float v)
     return a >= 4.0f ? r : fmaf(-a, e, r);
 }
 
+// A token's scale above 2^96: its product with a sum (below 2^31) may pass the largest float32 where
+// the output does not (a row that holds a type's lowest value, say).  2^-32 of the scale and 2^32 times
+// the outputs' scales give the same bits without that.  (An output's scale above 2^95 stays: there a
+// sum that is not 0 is infinite either way, and a sum of 0 stays 0.)
+__device__ inline bool is_far(float xs) { return fabsf(xs) > 0x1p96f && fabsf(xs) < __builtin_inff(); }
+__device__ inline float lift(float ws) { return fabsf(ws) <= 0x1p95f ? ws * 0x1p32f : ws; }
+
 // Four outputs of a token: sums, the token's scale, the outputs' scales and bias.
 template <int OUT, bool GELU> __device__ inline void finish4(const int s[4], float xs, float4 ws, float4 b, float out[4])
 {
@@ -239,6 +246,15 @@ template <int OUT> __device__ inline float4 bias4(const char* bias, int64_t n)
         return float4{E::to_f32((uint16_t)v.x), E::to_f32((uint16_t)(v.x >> 16)),
                       E::to_f32((uint16_t)v.y), E::to_f32((uint16_t)(v.y >> 16))};
     }
+}
+
+// Four neighbouring outputs, to memory.
+template <int OUT> __device__ inline void store4(char* y, const float o[4])
+{
+    if constexpr (OUT == LPV_F32)
+        *(float4*)y = float4{o[0], o[1], o[2], o[3]};
+    else
+        *(uint2*)y = uint2{pack2<OUT>(o[0], o[1]), pack2<OUT>(o[2], o[3])};
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -321,13 +337,14 @@ __global__ __launch_bounds__(64 * WV) void k_quant_few(
         }
         const int64_t m = m0 + (lane & 31), at = (int64_t)row * TILE + 8 * q + 4 * h;
         if (m < a.M && at < a.N) {
-            float o[4];
-            finish4<OUT, GELU>(s, xscale[m], *(const float4*)(wscale + at), bias4<OUT>(bias, at), o);
-            char* y = Y + (m * a.ldy + at) * ES;
-            if constexpr (OUT == LPV_F32)
-                *(float4*)y = float4{o[0], o[1], o[2], o[3]};
-            else
-                *(uint2*)y = uint2{pack2<OUT>(o[0], o[1]), pack2<OUT>(o[2], o[3])};
+            float o[4], xs = xscale[m];
+            float4 ws = *(const float4*)(wscale + at);
+            if (__builtin_expect(is_far(xs), 0)) {
+                xs *= 0x1p-32f;
+                ws = float4{lift(ws.x), lift(ws.y), lift(ws.z), lift(ws.w)};
+            }
+            finish4<OUT, GELU>(s, xs, ws, bias4<OUT>(bias, at), o);
+            store4<OUT>(Y + (m * a.ldy + at) * ES, o);
         }
     }
 }
@@ -425,6 +442,53 @@ __device__ inline void params_dma(const PanelDims& a, uint32_t stage, int lane, 
         dma4(xscale + m0 * 4, (uint32_t)min(64 * i + ln, last) * 4, stage + 512 + i * 256);
 }
 
+// Four neighbours of the bias in the staging area, from the pair's output n on.
+template <int OUT> __device__ inline float4 stage_bias4(uint32_t stage, int n)
+{
+    if constexpr (OUT == LPV_F32) {
+        return __builtin_bit_cast(float4, lds_read16<256>(stage + n * 4));
+    } else {
+        using E = Elem<OUT>;
+        const uint64_t v = *(lds_u64)(uintptr_t)(stage + 256 + n * 2);
+        return float4{E::to_f32((uint16_t)v), E::to_f32((uint16_t)(v >> 16)),
+                      E::to_f32((uint16_t)(v >> 32)), E::to_f32((uint16_t)(v >> 48))};
+    }
+}
+
+// The outputs as panel_outputs gives them, for a wave with a far token: each lane stores its own.
+template <int OUT, bool GELU, int TU>
+__device__ inline void far_outputs(const PanelDims& a, i32x16 (&acc)[2][TU], const float (&xs)[TU], uint32_t stage,
+                                   int lane, int64_t m0, int64_t n0, char* Y)
+{
+    constexpr int ES = OUT == LPV_F32 ? 4 : 2;
+    const int fr = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = 32 * j + 8 * q + 4 * h;
+            const float4 ws = __builtin_bit_cast(float4, lds_read16<0>(stage + n * 4));
+            const float4 b = stage_bias4<OUT>(stage, n);
+#pragma unroll
+            for (int u = 0; u < TU; ++u) {
+                const int s[4] = {acc[j][u][4 * q], acc[j][u][4 * q + 1], acc[j][u][4 * q + 2], acc[j][u][4 * q + 3]};
+                const bool far = is_far(xs[u]);
+                const float4 wl = {far ? lift(ws.x) : ws.x, far ? lift(ws.y) : ws.y, far ? lift(ws.z) : ws.z,
+                                   far ? lift(ws.w) : ws.w};
+                float o[4];
+                finish4<OUT, GELU>(s, far ? xs[u] * 0x1p-32f : xs[u], wl, b, o);
+                const int64_t m = m0 + 32 * u + fr;
+                if (m < a.M && n0 + n < a.N)
+                    store4<OUT>(Y + (m * a.ldy + n0 + n) * ES, o);
+            }
+        }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int u = 0; u < TU; ++u)
+            acc[j][u] = i32x16{};
+}
+
 // The outputs of 32 TU tokens (from m0) and a pair's 64 outputs (from n0); the sums are left at 0.
 template <int OUT, bool GELU, int TU>
 __device__ inline void panel_outputs(const PanelDims& a, i32x16 (&acc)[2][TU], uint32_t stage, int lane,
@@ -436,6 +500,14 @@ __device__ inline void panel_outputs(const PanelDims& a, i32x16 (&acc)[2][TU], u
 #pragma unroll
     for (int u = 0; u < TU; ++u)
         xs[u] = __uint_as_float(*(lds_u32)(uintptr_t)(stage + 512 + (32 * u + fr) * 4));
+    bool any_far = false;
+#pragma unroll
+    for (int u = 0; u < TU; ++u)
+        any_far |= is_far(xs[u]);
+    if (__builtin_expect(__any(any_far), 0)) {
+        far_outputs<OUT, GELU, TU>(a, acc, xs, stage, ln, m0, n0, Y);
+        return;
+    }
     uint2 pk[TU][2][4];    // 16-bit outputs: four to a place
     float4 pf[OUT == LPV_F32 ? TU : 1][2][4];
 #pragma unroll
@@ -444,15 +516,7 @@ __device__ inline void panel_outputs(const PanelDims& a, i32x16 (&acc)[2][TU], u
         for (int q = 0; q < 4; ++q) {
             const int n = 32 * j + 8 * q + 4 * h;
             const float4 ws = __builtin_bit_cast(float4, lds_read16<0>(stage + n * 4));
-            float4 b;
-            if constexpr (OUT == LPV_F32) {
-                b = __builtin_bit_cast(float4, lds_read16<256>(stage + n * 4));
-            } else {
-                using E = Elem<OUT>;
-                const uint64_t v = *(lds_u64)(uintptr_t)(stage + 256 + n * 2);
-                b = float4{E::to_f32((uint16_t)v), E::to_f32((uint16_t)(v >> 16)),
-                           E::to_f32((uint16_t)(v >> 32)), E::to_f32((uint16_t)(v >> 48))};
-            }
+            const float4 b = stage_bias4<OUT>(stage, n);
 #pragma unroll
             for (int u = 0; u < TU; ++u) {
                 const int s[4] = {acc[j][u][4 * q], acc[j][u][4 * q + 1], acc[j][u][4 * q + 2], acc[j][u][4 * q + 3]};
