@@ -822,8 +822,8 @@ class QuantWeight:
 
 def quant_pack(W, scale, mask=None, b_r=16, b_c=16, stream=None):
     """lpv_quant_pack: a weight in 8-bit codes (int8 N x K) with a scale for each output (N
-    float32), and a uint8 block mask (N/b_r x K/b_c; None: dense) -> QuantWeight.  Waits for
-    the pack to finish."""
+    float32), and a uint8 block mask (N/b_r x K/b_c, or its entries row by row; None: dense) ->
+    QuantWeight.  Waits for the pack to finish."""
     if not isinstance(W, torch.Tensor) or W.dim() != 2:
         raise ValueError("W must be a 2-D int8 tensor")
     N, K = W.shape
@@ -834,9 +834,10 @@ def quant_pack(W, scale, mask=None, b_r=16, b_c=16, stream=None):
     if mask is not None:
         if not isinstance(mask, torch.Tensor) or mask.dtype != torch.uint8 or not mask.is_contiguous():
             raise ValueError("mask must be a contiguous uint8 tensor")
-        if b_r > 0 and b_c > 0 and N % b_r == 0 and K % b_c == 0 \
-                and mask.numel() != (N // b_r) * (K // b_c):
-            raise ValueError("mask has %d entries, expected %d" % (mask.numel(), (N // b_r) * (K // b_c)))
+        if b_r > 0 and b_c > 0 and N % b_r == 0 and K % b_c == 0:
+            R, C = N // b_r, K // b_c
+            if mask.shape != (R, C) and mask.shape != (R * C,):
+                raise ValueError("mask is %s, expected %d x %d" % (" x ".join(map(str, mask.shape)), R, C))
     _on_current(("W", W), ("scale", scale), ("mask", mask))
     out = ctypes.c_void_p()
     _check(lib().lpv_quant_pack(wp, ldw, N, K, scale.data_ptr(), b_r, b_c,
