@@ -41,9 +41,11 @@ class Linear:
 
     def quantize(self):
         """Packs the kept blocks in 8-bit codes with a scale for each output."""
-        keep = self.mask.repeat_interleave(self.b_r, 0).repeat_interleave(self.b_c, 1) != 0
+        N, K = self.W.shape
+        mask = self.mask.view(N // self.b_r, K // self.b_c)  # (bsr_pack takes its entries in any shape)
+        keep = mask.repeat_interleave(self.b_r, 0).repeat_interleave(self.b_c, 1) != 0
         codes, scale = lpv.quant_rows(torch.where(keep, self.W, 0))
-        self.q = lpv.quant_pack(codes, scale, self.mask, self.b_r, self.b_c)
+        self.q = lpv.quant_pack(codes, scale, mask, self.b_r, self.b_c)
 
     def __call__(self, x, y, sparse):
         epi = "gelu" if self.gelu else None

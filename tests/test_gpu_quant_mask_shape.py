@@ -1,6 +1,9 @@
-"""The block mask of a weight in 8-bit codes: its shape."""
+"""The block mask of a weight in 8-bit codes: its shape, and a flat one through the encoder chain."""
 import pytest
 import torch
+
+import workloads as wl
+from gpu_util import dev
 
 pytestmark = pytest.mark.gpu
 
@@ -26,3 +29,25 @@ def test_a_mask_of_another_shape_is_refused():
     want = m.quant_linear(m.quant_pack(W, ws, mask, 16, 32), X, xs)
     flat = m.quant_linear(m.quant_pack(W, ws, mask.view(-1), 16, 32), X, xs)  # (row by row)
     assert torch.equal(want, flat)
+
+
+def test_a_chain_of_flat_masks():
+    # the 16-bit chain takes them; so does the one in 8 bits
+    from paper_2407_02068_amd.encoder import EncoderChain, Linear
+    n_seq, T, H = 1, 50, 12
+    layers = wl.b_stack(M=n_seq * T, layers=1)
+    outs = []
+    for flat in (False, True):
+        lins = []
+        for w in layers:
+            mask = dev(w.mask)
+            lins.append(Linear(w.name, dev(w.W, "bf16"), mask.view(-1) if flat else mask, dev(w.bias, "bf16"),
+                               w.b_r, w.b_c, w.gelu))
+        one = torch.ones(768, dtype=torch.bfloat16, device="cuda")
+        chain = EncoderChain(lins, n_seq, T, H, one, torch.zeros_like(one))
+        x0 = dev(layers[0].X, "bf16")
+        a = [t.clone() for t in chain.run(x0)]
+        chain.quantize()
+        outs.append(a + [t.clone() for t in chain.run(x0, quant=True)])
+        chain.close()
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
