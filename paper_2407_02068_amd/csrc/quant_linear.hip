@@ -731,6 +731,8 @@ __global__ __launch_bounds__(64 * WV, TU == 1 ? 3 : 2) void k_quant_panel(
     // wave has read this one, whose place the DMA takes.  What is younger than the next one's
     // DMA: 4 loads of tiles at least in each of the NS - 1 chunks since (fewer before there were
     // that many); what is younger than an item's scales and bias at its end: 8.
+    // (At least: a count that is too low waits for more than it needs.  So any other load or store
+    // in between, a spilled register's among them, leaves the waits right.)
     int chunks = 0;
     auto sync = [&](bool at_end) __attribute__((always_inline)) {
         constexpr int AHEAD = 4 * (NS - 1);
