@@ -272,7 +272,7 @@ struct DistillCall {
 size_t distill_workspace_bytes(int64_t M, int64_t V, int32_t k, int dtype);
 hipError_t launch_distill(const DistillCall& c, hipStream_t s);
 // quant.hip
-constexpr int32_t QUANT_MAX_D = 32768;  // the longest row (it stays in registers)
+constexpr int32_t QUANT_MAX_D = 32768;  // the longest row (32 elements to each of 1024 threads)
 constexpr int QUANT_PLAIN = 0, QUANT_RMS = 1, QUANT_LAYER = 2;
 struct QuantRowsCall {
     int kind;

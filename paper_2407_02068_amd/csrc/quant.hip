@@ -229,12 +229,18 @@ __device__ inline int settle(double u, double top, double t)
 }
 
 // NT threads to a row (64: four rows to a workgroup), NC chunks of CH elements to a thread, held
-// in registers: the row is read once, the next one's loads going out before this one is worked on.
-// Bound by memory: 8192 x 4096 bf16 with its sum and a root-mean-square norm 37 us, 6.4 TB/s (two
-// rows in, the sum and the codes out), 60 before reductions in registers and the row ahead;
-// 12608 x 768 fp16 with a layer norm 17.6 us, 3.9 TB/s (25.8), where a wave has a row of 12
-// elements a lane and the reductions' chain shows; 1777 x 5120 float32 10.3 us (14.8); one row of 4096
-// 3.3 us, a launch.
+// in registers up to 8192 elements: the row is read once, the next one's loads going out before this
+// one is worked on.  Bound by memory: 8192 x 4096 bf16 with its sum and a root-mean-square norm (two
+// rows in, the sum and the codes out) 44 us, 5.3 TB/s, or 37, 6.4 TB/s, where the last-level cache
+// still has the rows (60 before reductions in registers and the row ahead); 12608 x 768 fp16 with a
+// layer norm 17.6 us, 3.9 TB/s (25.8), where a wave has a row of 12 elements a lane and the
+// reductions' chain shows, bf16 as they are 8.5 us; 1777 x 5120 float32 10.4 us (14.8); one row of
+// 4096 3.3 us, a launch.
+// Past 8192 elements a row has 1024 threads, with 128 registers each.  They hold rows as they are (float32
+// to 16384) and root-mean-square rows to 16384; the rest spills (bytes a lane, vectors / element by element):
+// layer norms 184 to 252 up to 16384 and 384 to 956 / 892 to 1412 beyond, root-mean-square norms 36 to
+// 352 / 336 to 576, float32 rows 120 / 128.  1024 x 32768 bf16 takes 39 us as a sum (6.0 TB/s with the
+// cache's help), 90 behind a root-mean-square norm, 224 behind a layer norm.
 // VEC: a chunk is CH neighbours; else (odd sizes, strides or addresses) the row's elements go
 // to the threads one by one.
 template <int DT, int KIND, int NT, int NC, int CH, bool VEC>

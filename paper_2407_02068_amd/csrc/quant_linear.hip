@@ -372,9 +372,10 @@ hipError_t launch_few(const lpv_quant* h, const QuantLinearCall& c, hipStream_t 
 // LDS: panels of 128 columns, a row (token) of 128 bytes, its 16-byte piece c at
 // c ^ xswz(row): the 16 rows that are read at once lie in distinct banks.
 //
-// What bounds it.  Dense and large, the matrix cores at the clock that their power leaves: 16384 x
-// 4096 -> 8192 453 us, 2.43 POP/s, a library's 8192^3 int8 product 2.49.  Pruned, no one thing:
-// 50432 x 768 -> 2304 at 50% takes 79 us (a copy of its bytes 52), 74 if the waves did not wait for each
+// What bounds it.  Dense and large, the matrix cores: 16384 x 4096 -> 8192 453 to 465 us, 2.36 to 2.43
+// POP/s, a library's 8192^3 int8 product 2.49 (525 to 566 us in the tens of launches after a rest, while
+// the clock settles, as the library's is slower there).  Pruned, no one thing:
+// 50432 x 768 -> 2304 at 50% takes 78 us (a copy of its bytes 52), 74 if the waves did not wait for each
 // other at a chunk's end, 71 without the chunks' DMA (the tiles' loads come back behind it), 66
 // without the outputs' stores; 8192 x 4096 -> 4096 in blocks of 64 at 80% 48 us (22), 41 without the
 // waves' waiting (a chunk has 0.8 kept blocks a pair, on average, and the wave with the most is waited
@@ -843,7 +844,8 @@ hipError_t launch_panel(const lpv_quant* h, const QuantLinearCall& c, int n_cus,
     return hipSuccess;
 }
 
-// The kernel by the work there is, GPU us on 256 compute units.
+// The kernel by the work there is, GPU us on 256 compute units (at up to 8192 outputs; wider ones follow
+// the same rule untimed).
 // - k_quant_few up to 1400 units of 32 tokens and a tile row (1380 units of 640 x 832 6.8, items of 32
 //   tokens 7.0; 1600 of 656 x 688 9.5 / 7.5; 6400 of 5504 x 128 14.6 / 9.0), with 4 waves to a unit, or
 //   8 where a tile row keeps more than 48 tiles (12: 4.7 / 5.5, 57: 4.7 / 4.6, 128: 7.0 / 6.1).

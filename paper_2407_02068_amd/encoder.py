@@ -225,8 +225,8 @@ class EncoderChain:
 
     def capture(self, x0, sparse=True, quant=False):
         """The forward pass from x0 captured once into a HIP graph (through
-        torch.cuda.CUDAGraph): replaying it relaunches the same 1 + 6 * blocks (in 8
-        bits 1 + 8 * blocks) calls' kernels on the same buffers with no host work per launch.  Every call
+        torch.cuda.CUDAGraph): replaying it relaunches the same 1 + 7 * blocks (in 8
+        bits 1 + 9 * blocks) calls' kernels on the same buffers with no host work per launch.  Every call
         of the chain is capturable (no allocation, no host synchronisation, no
         memset); one eager pass first settles the kernels' one-time set-up.
         Returns (graph, (x, A)): the outputs the replays rewrite."""
